@@ -175,7 +175,7 @@ def prepare(case, seed):
         inside = inside_r & inside_c                                                       # one flag per 32-wide group
         code = code * inside.repeat_interleave(16, dim=3).to(torch.uint8)
         byte = byte * inside.to(torch.uint8)
-        # inside a tile: [half, row % 8, eighth (8 codes), group] words of four bytes, then [row, group] scale bytes
+        # inside a tile: [half, row % 8, quarter of a group, group] words of eight codes, then [row, group] scale bytes
         code = code.reshape(e, -1, code.shape[2], 2, 8, 4, 4, 4).permute(0, 1, 2, 3, 4, 6, 5, 7).reshape(*code.shape[:3], 1024)
         st["packed"] = torch.cat([code, byte.reshape(*code.shape[:3], 64)], dim=3).contiguous()
         st["y"] = empty(n * k, r, dtype=DTYPE[case["out"]])
@@ -280,16 +280,22 @@ def _plain_combine_grad(st):
     return d_y.to(st["y"].dtype), d_weights
 
 
+# Where the codes of a word's eight columns lie: even columns in its low half, odd ones in its high half
+SIGN_BIT, VALUE_BITS = (15, 12, 14, 13), (6, 3, 0, 9)
+
+
 def _decoded(packed, rows, cols):
     """[matrices, rows, cols] values of packed E2M1 tiles in 32 bits."""
     e, rb, kb, _ = packed.shape
-    code = packed[..., :1024].reshape(e, rb, kb, 2, 8, 4, 4, 4).permute(0, 1, 3, 4, 2, 6, 5, 7).reshape(e, rb * 16, kb * 64)
+    word = packed[..., :1024].contiguous().view(torch.int32).reshape(e, rb, kb, 2, 8, 4, 4)    # half, row % 8, quarter, group
+    word = word.permute(0, 1, 3, 4, 2, 6, 5).reshape(e, rb * 16, kb * 16)
     scale = packed[..., 1024:].reshape(e, rb, kb, 16, 4).permute(0, 1, 3, 2, 4).reshape(e, rb * 16, kb * 4)
-    code = torch.stack([code & 15, code >> 4], dim=3).reshape(e, rb * 16, kb * 128)
-    # sign, two exponent bits, one mantissa bit: m / 2 below the smallest exponent, (1 + m / 2) 2^(e - 1) above
-    exponent, half = (code >> 1) & 3, 0.5 * (code & 1).float()
-    value = torch.where(exponent == 0, half, (1 + half) * ((exponent.int() + 126) << 23).view(torch.float32))
-    value = value * (1 - 2 * (code >> 3).float())
+    sign = torch.stack([word >> (SIGN_BIT[i // 2] + 16 * (i % 2)) for i in range(8)], dim=3) & 1
+    code = torch.stack([word >> (VALUE_BITS[i // 2] + 16 * (i % 2)) for i in range(8)], dim=3) & 7
+    # two exponent bits, one mantissa bit: m / 2 below the smallest exponent, (1 + m / 2) 2^(e - 1) above
+    exponent, half = code >> 1, 0.5 * (code & 1).float()
+    value = torch.where(exponent == 0, half, (1 + half) * ((exponent + 126) << 23).view(torch.float32))
+    value = (value * (1 - 2 * sign.float())).reshape(e, rb * 16, kb * 128)
     return (value * (scale.int() << 23).view(torch.float32).repeat_interleave(32, dim=2))[:, :rows, :cols]
 
 
@@ -368,7 +374,7 @@ def _exact_codes(v, axis, rule, elem):
     return _fp8_grid(blocks * _two(-exponent), mantissa, least, largest).reshape(v.shape)
 
 
-E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)       # by the three value bits
 
 
 def _exact_products(st):
@@ -377,16 +383,19 @@ def _exact_products(st):
     if case["tokens"] * k * r * c > (15e8 if case["chosen"] else 15e9):
         return None
     flat = st["packed"].reshape(e, -1)
-    table = torch.tensor(E2M1 + tuple(-v for v in E2M1), dtype=torch.float64, device="cuda")
+    table = torch.tensor(E2M1, dtype=torch.float64, device="cuda")
     row, col = torch.arange(r, device="cuda").unsqueeze(1), torch.arange(c, device="cuda").unsqueeze(0)
     tile = ((row // 16) * ((c + 127) // 128) + col // 128) * 1088
-    byte = tile + row % 16 // 8 * 512 + row % 8 * 64 + col % 32 // 8 * 16 + col % 128 // 32 * 4 + col % 8 // 2
+    word = (tile + row % 16 // 8 * 512 + row % 8 * 64 + col % 32 // 8 * 16 + col % 128 // 32 * 4) // 4
     group = tile + 1024 + row % 16 * 4 + col % 128 // 32
+    pair, high = col % 8 // 2, 16 * (col % 2)
+    sign_at = torch.tensor(SIGN_BIT, device="cuda")[pair] + high
+    value_at = torch.tensor(VALUE_BITS, device="cuda")[pair] + high
     out = torch.empty(case["tokens"] * k, r, dtype=torch.float64, device="cuda")
     ids = st["ids"].reshape(-1) if case["chosen"] else torch.zeros(case["tokens"], dtype=torch.int32, device="cuda")
     for m in ids.unique().tolist():
-        code = (flat[m][byte] >> (4 * (col % 2))) & 15
-        w = table[code.long()] * _two(flat[m][group].int() - 127)
+        bits = flat[m].view(torch.int32)[word].long()
+        w = table[(bits >> value_at) & 7] * (1 - 2 * ((bits >> sign_at) & 1)) * _two(flat[m][group].int() - 127)
         slots = torch.nonzero(ids == m).reshape(-1)
         out[slots] = st["x"].double()[slots // k] @ w.t()
     return out
