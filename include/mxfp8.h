@@ -361,6 +361,92 @@ int mxfp8_grouped_gemm(const void* Aq, const void* As, const void* Bq, const voi
                        void* D, int out_dtype, void* stream);
 
 /*
+ * Moving the tokens of a mixture-of-experts layer (App. A.4) into and out of the order that mxfp8_grouped_gemm reads.
+ * A SLOT is one (token, choice) pair, numbered token * top_k + choice.  The sorted tensor has one row per slot that has
+ * an expert: rows of expert e from group_offsets[e], in slot order, every segment padded with rows without a slot to a
+ * multiple of 128.  (The paper trains such a model with the recipe and says nothing of its routing; these calls are what
+ * the grouped products ask of their caller.)  All pointers are device pointers.  No tokens (tokens = 0) is a valid batch.
+ *
+ * mxfp8_moe_rows -- rows that hold every possible routing of this size: the `rows` to allocate sorted tensors with (a
+ * multiple of 128).  The rows in use, group_offsets[num_experts], stay on the device; every call below reads them there
+ * and leaves the rows behind them as they were.
+ *
+ * mxfp8_moe_sort -- stable counting sort of the slots by expert.
+ *   expert_ids     [tokens, top_k] int32; a number outside 0 .. num_experts - 1 (-1, say) is a slot without an expert
+ *                  (dropped).  The same expert may appear twice in a token.
+ *   group_offsets  [num_experts + 1]: starts of the segments and the end of the last, as mxfp8_grouped_gemm takes them.
+ *   row_of         [tokens, top_k]: row of every slot, -1 for a slot without an expert.
+ *   slot_of        [rows]: slot of every row, -1 for a row without one (padding, and all rows behind the last segment).
+ *   ws             mxfp8_moe_sort_ws_bytes() bytes (0 for small batches); calls that may overlap need their own.
+ *   The result is the same every time (no atomic decides an order).  num_experts <= 256 (ERR_UNSUPPORTED);
+ *   rows < mxfp8_moe_rows() is ERR_SHAPE.
+ *
+ * mxfp8_moe_dispatch_quantize -- gathers tokens into the sorted order and converts them in the same pass (no sorted
+ * tensor is written in between):
+ *     y[r, :] = weights[slot_of[r]] * src[slot_of[r] / top_k, :]   one FP32 product, rounded once to the source dtype
+ *             = src[slot_of[r] / top_k, :]                         without weights
+ *             = 0                                                  for a row without a slot
+ *   then exactly mxfp8_quantize(y) of the rows in use, y being [rows, cols] (scale layouts and output sizes are those of
+ *   [rows, cols]).  Without weights: the experts' input, forward (ROW) and for WGRAD (COL).  With the router's weights and
+ *   the layer's output gradient as src: the gradient of mxfp8_moe_combine with respect to the experts' outputs, converted
+ *   for DGRAD (ROW) and WGRAD (COL).
+ *   rows a multiple of 128; cols a multiple of 32 for ROW blocks and of 16 otherwise; slot_of 16-byte aligned; the
+ *   other arguments and errors as mxfp8_quantize.
+ *
+ * mxfp8_moe_combine -- dst[t, :] = sum over j of weights[t, j] * src[row_of[t, j], :], FP32 in the order of j, rounded once
+ * to dst's type; slots without a row are left out (a token without any gets zeros).  weights NULL: a plain sum, which is
+ * the gradient of an unweighted mxfp8_moe_dispatch_quantize with respect to its source.  src [rows, cols], dst [tokens, cols],
+ * each FP32 or BF16, any cols, aligned to their elements (16-byte rows are read in larger pieces).
+ *
+ * mxfp8_moe_combine_grad -- the gradients of that sum, dy read once:
+ *     d_src[row_of[t, j], :] = weights[t, j] * dy[t, :]                one FP32 product, rounded to src's type; 0 in padding rows
+ *     d_weights[t, j]        = sum over c of dy[t, c] * src[row_of[t, j], c]    FP32 in a fixed order; 0 without a row
+ *   d_src (with slot_of, group_offsets) or d_weights (with src) may be NULL.  weights NULL: all ones.
+ *
+ * Entries of row_of / slot_of that are neither -1 nor a row / slot of the tensors, or a group_offsets[num_groups] that is
+ * no possible end, leave MXFP8_ERR_DEVICE_ARGS in the device status word; such an entry counts as -1, and with such an end
+ * nothing is stored into rows.  Two slots must not share a row.
+ */
+int64_t mxfp8_moe_rows(int64_t tokens, int top_k, int num_experts);
+size_t mxfp8_moe_sort_ws_bytes(int64_t tokens, int top_k, int num_experts);
+int mxfp8_moe_sort(const int32_t* expert_ids, int64_t tokens, int top_k, int num_experts,
+                   int32_t* group_offsets, int32_t* row_of, int32_t* slot_of, int64_t rows,
+                   void* ws, size_t ws_bytes, void* stream);
+int mxfp8_moe_dispatch_quantize(const void* src, int src_dtype, int64_t tokens, int64_t cols,
+                                const int32_t* slot_of, int64_t rows, int top_k, const float* weights,
+                                const int32_t* group_offsets, int num_groups,
+                                int orientation, int scale_rule, int elem,
+                                void* q_row, void* s_row, void* q_col, void* s_col,
+                                int sf_layout, void* stream);
+int mxfp8_moe_combine(const void* src, int src_dtype, int64_t rows, int64_t cols, const int32_t* row_of,
+                      const float* weights, int64_t tokens, int top_k, void* dst, int dst_dtype, void* stream);
+int mxfp8_moe_combine_grad(const void* dy, int dy_dtype, int64_t tokens, int64_t cols, const void* src, int src_dtype, int64_t rows,
+                           const int32_t* row_of, const int32_t* slot_of, int top_k, const float* weights,
+                           const int32_t* group_offsets, int num_groups, void* d_src, float* d_weights, void* stream);
+
+/*
+ * Products of a few tokens with E2M1 (MXFP4, Table 1) matrices: what a layer computes when it answers one or a few
+ * sequences token by token, where a product is bound by the bytes of its weights.  Weights are stored as the conversion
+ * makes them (4-bit codes, one UE8M0 scale per 32 columns of a row), activations stay BF16.
+ *
+ * mxfp8_e2m1_pack -- lays matrices out for mxfp8_e2m1_matvec, once: `q` [num_matrices * rows, cols] and `s` are what
+ * mxfp8_quantize(elem E2M1, ROW, MXFP8_SF_LINEAR) wrote; `packed` receives mxfp8_e2m1_packed_bytes() bytes (17/32 byte per
+ * weight, rows padded to 16 and columns to 128).  cols % 32 == 0; q and packed 16-byte aligned.
+ *
+ * mxfp8_e2m1_matvec --
+ *     y[s, n] = sum over groups g of 2^(b[n, g] - 127) * sum_{k in g} code[n, k] * x[s / slots_per_token, k]
+ *   with the codes and scale bytes of matrix matrix_ids[s] (slot s = token * slots_per_token + choice), or of the only
+ *   matrix when matrix_ids is NULL (num_matrices and slots_per_token are 1 then).  A slot whose number is outside
+ *   0 .. num_matrices - 1 gets zeros.  x [tokens, cols] BF16, 16-byte aligned; y [tokens * slots_per_token, rows] FP32 or BF16.
+ *   Products are exact, each group's sum is FP32, the groups are added in FP32 in a fixed order; scale byte 0xFF gives NaN.
+ *   At most 1024 slots and 65535 matrices (ERR_UNSUPPORTED): beyond that mxfp8_gemm / mxfp8_grouped_gemm are the tools.
+ */
+size_t mxfp8_e2m1_packed_bytes(int64_t num_matrices, int64_t rows, int64_t cols);
+int mxfp8_e2m1_pack(const void* q, const void* s, int64_t num_matrices, int64_t rows, int64_t cols, void* packed, void* stream);
+int mxfp8_e2m1_matvec(const void* x, int64_t tokens, int64_t cols, const void* packed, int64_t num_matrices, int64_t rows,
+                      const int32_t* matrix_ids, int slots_per_token, void* y, int y_dtype, void* stream);
+
+/*
  * Data-parallel exchange.  The recipe casts weights, activations and output gradients (Sec. 3.2); when
  * the tokens of a step are split over GPUs and every GPU owns a row range of each weight, two exchanges
  * follow from that arithmetic: the MXFP8 copies of the weight shards are gathered (1 + 1/32 bytes per

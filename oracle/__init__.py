@@ -12,4 +12,5 @@ from .mxfp8_oracle import (  # noqa: F401
     swizzle_scales, gemm_f64, quantize_threads, grouped_gemm_f64, code_bits, pack_codes16, unpack_codes16,
     ACT_NONE, ACT_RELU, ACT_RELU2, ACT_SILU, ACT_GELU_TANH, activation, rmsnorm, glu, layernorm, activation_grad,
     concat_swizzled_scales_k, data_parallel_linear_f64,
+    moe_sort, moe_dispatch, moe_combine_f64, moe_combine_grad_f64, e2m1_packed, matvec_f64,
 )

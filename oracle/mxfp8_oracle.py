@@ -475,3 +475,111 @@ def glu(x: np.ndarray, act: int, dst: str = "f32") -> np.ndarray:
     y64 = np.ascontiguousarray(y32, dtype=np.float64)
     _load().orc_round_to_bf16(_ptr(y64), y64.size, _ptr(out))
     return out
+
+
+def moe_sort(ids: np.ndarray, experts: int, rows: int):
+    """Sorts the (token, choice) slots of `ids` [tokens, top_k] by expert, in slot order inside an expert, every expert's
+    segment padded to whole 128 rows.  Returns (group_offsets [experts + 1], row_of [tokens, top_k], slot_of [rows]) as
+    int32; -1 where a slot has no expert (its number is outside 0 .. experts - 1) or a row no slot."""
+    flat = ids.reshape(-1)
+    offsets = [0]
+    row_of = np.full(flat.size, -1, np.int32)
+    slot_of = np.full(rows, -1, np.int32)
+    for e in range(experts):
+        mine = np.flatnonzero(flat == e)
+        row_of[mine] = offsets[-1] + np.arange(mine.size)
+        slot_of[row_of[mine]] = mine
+        offsets.append(offsets[-1] + -(-mine.size // 128) * 128)
+    return np.array(offsets, np.int32), row_of.reshape(ids.shape), slot_of
+
+
+def moe_dispatch(x: np.ndarray, slot_of: np.ndarray, top_k: int, weights=None, dst: str = "f32") -> np.ndarray:
+    """Row r = weights[slot_of[r]] * x[slot_of[r] // top_k]: one binary32 product, rounded once more to bfloat16 for dst
+    "bf16" (returned as the float32 values), without weights the row itself, zeros where slot_of[r] is -1."""
+    y = np.zeros((slot_of.size, x.shape[1]), np.float32)
+    for r, slot in enumerate(slot_of):
+        if slot < 0:
+            continue
+        y[r] = x[slot // top_k]
+        if weights is not None:
+            with np.errstate(over="ignore", invalid="ignore"):
+                y[r] = y[r] * np.float32(weights.reshape(-1)[slot])
+    if dst == "bf16" and weights is not None:
+        bits = np.empty(y.shape, dtype=np.uint16)
+        y64 = np.ascontiguousarray(y, dtype=np.float64)
+        _load().orc_round_to_bf16(_ptr(y64), y64.size, _ptr(bits))
+        y = bf16_bits_to_f32(bits)
+    return y
+
+
+def moe_combine_f64(src: np.ndarray, row_of: np.ndarray, weights=None):
+    """dst[t] = sum_j weights[t, j] * src[row_of[t, j]] over the slots with a row, in binary64, and the sum of the
+    terms' magnitudes."""
+    out = np.zeros((row_of.shape[0], src.shape[1]))
+    mag = np.zeros_like(out)
+    for t in range(row_of.shape[0]):
+        for j in range(row_of.shape[1]):
+            if row_of[t, j] >= 0:
+                term = src[row_of[t, j]].astype(np.float64) * (1.0 if weights is None else np.float64(weights[t, j]))
+                out[t] += term
+                mag[t] += np.abs(term)
+    return out, mag
+
+
+def moe_combine_grad_f64(dy: np.ndarray, src: np.ndarray, row_of: np.ndarray, weights, rows: int):
+    """Gradients of moe_combine_f64 for the output gradient dy: (d_src [rows, cols], zero in rows without a slot,
+    d_weights [tokens, top_k], sum of the magnitudes of d_weights' terms), binary64."""
+    d_src = np.zeros((rows, dy.shape[1]))
+    d_w, mag = np.zeros(row_of.shape), np.zeros(row_of.shape)
+    for t in range(row_of.shape[0]):
+        g = dy[t].astype(np.float64)
+        for j in range(row_of.shape[1]):
+            r = row_of[t, j]
+            if r >= 0:
+                d_src[r] = g * np.float64(weights[t, j])
+                terms = g * src[r].astype(np.float64)
+                d_w[t, j], mag[t, j] = terms.sum(), np.abs(terms).sum()
+    return d_src, d_w, mag
+
+
+def e2m1_packed(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
+    """The tile layout of the 4-bit product (an index / bit permutation): codes [rows, cols] one per byte, scales
+    [rows, cols / 32]; tiles of 16 rows x 128 columns, column tiles innermost, 1024 bytes of codes and 64 of scales each,
+    padded with zeros.  Inside a tile the code of (row, col) lies in the little-endian 32-bit word
+    ((row / 8 * 8 + row % 8) * 4 + col % 32 / 8) * 4 + col / 32, low half for an even column, its sign at bit 15, 12, 14, 13
+    and its value bits from bit 6, 3, 0, 9 for col % 8 / 2 = 0, 1, 2, 3; the scale of (row, group) is byte 1024 + 4 row + group."""
+    rows, cols = codes.shape
+    rt, kt = -(-rows // 16), -(-cols // 128)
+    out = np.zeros((rt, kt, 1088), np.uint8)
+    words = np.zeros((rt, kt, 256), np.uint32)
+    for r in range(rows):
+        for c in range(cols):
+            rr, cc = r % 16, c % 128
+            code = int(codes[r, c])
+            sign, value = ((15, 6), (12, 3), (14, 0), (13, 9))[cc % 8 // 2]
+            half = 16 * (cc % 2)
+            words[r // 16, c // 128, (rr * 4 + cc % 32 // 8) * 4 + cc // 32] |= np.uint32(((code >> 3) << (sign + half)) | ((code & 7) << (value + half)))
+        for g in range(cols // 32):
+            out[r // 16, g // 4, 1024 + 4 * (r % 16) + g % 4] = scales[r, g]
+    out[:, :, :1024] = words.astype("<u4").view(np.uint8).reshape(rt, kt, 1024)
+    return out.reshape(-1)
+
+
+def matvec_f64(x: np.ndarray, codes: np.ndarray, scales: np.ndarray, ids=None):
+    """y[s] = decoded(matrix of slot s) @ x[token of s] in binary64 and the sums of the terms' magnitudes.  codes
+    [matrices, rows, cols] E2M1 codes one per byte, scales [matrices, rows, cols / 32] bytes, ids [tokens, choices] or None
+    (matrix 0).  A number that names no matrix gives zeros."""
+    tokens = x.shape[0]
+    flat = np.zeros(tokens, np.int64) if ids is None else ids.reshape(-1)
+    per = 1 if ids is None else ids.shape[1]
+    table = np.array([fp8_decode(c, E2M1) for c in range(16)])
+    y, mag = np.zeros((flat.size, codes.shape[1])), np.zeros((flat.size, codes.shape[1]))
+    for m in np.unique(flat):
+        if not 0 <= m < codes.shape[0]:
+            continue
+        s = scales[m].astype(np.float64)
+        w = table[codes[m]] * np.repeat(np.where(s == 255, np.nan, np.exp2(s - 127)), 32, axis=1)
+        at = np.flatnonzero(flat == m)
+        xs = x[at // per].astype(np.float64)
+        y[at], mag[at] = xs @ w.T, np.abs(xs) @ np.abs(w).T
+    return y, mag

@@ -32,6 +32,8 @@ EXPORTS = (
     "mxfp8_linear", "mxfp8_grouped_gemm", "mxfp8_quantize_multi", "mxfp8_gemm_multi", "mxfp8_act_quantize", "mxfp8_rmsnorm_quantize",
     "mxfp8_rmsnorm_quantize_static", "mxfp8_rmsnorm_quantize_static_max_rows", "mxfp8_glu_quantize",
     "mxfp8_sf_concat_k", "mxfp8_gemm_reduce_scatter", "mxfp8_enable_peer_access", "mxfp8_gemm_last_clock", "mxfp8_layernorm_quantize", "mxfp8_act_grad_quantize",
+    "mxfp8_moe_rows", "mxfp8_moe_sort_ws_bytes", "mxfp8_moe_sort", "mxfp8_moe_dispatch_quantize", "mxfp8_moe_combine", "mxfp8_moe_combine_grad",
+    "mxfp8_e2m1_packed_bytes", "mxfp8_e2m1_pack", "mxfp8_e2m1_matvec",
 )
 
 
@@ -124,6 +126,24 @@ def load_library(path: str) -> ctypes.CDLL:
     L.mxfp8_quantize_multi.argtypes = [ctypes.POINTER(_QuantizeItem), i, i, i, i, i, i, p]
     L.mxfp8_grouped_gemm.restype = i
     L.mxfp8_grouped_gemm.argtypes = [p, p, p, p, p, i, i, i64, i64, i64, i, i, i, p, i, p]
+    L.mxfp8_moe_rows.restype = i64
+    L.mxfp8_moe_rows.argtypes = [i64, i, i]
+    L.mxfp8_moe_sort_ws_bytes.restype = sz
+    L.mxfp8_moe_sort_ws_bytes.argtypes = [i64, i, i]
+    L.mxfp8_moe_sort.restype = i
+    L.mxfp8_moe_sort.argtypes = [p, i64, i, i, p, p, p, i64, p, sz, p]
+    L.mxfp8_moe_dispatch_quantize.restype = i
+    L.mxfp8_moe_dispatch_quantize.argtypes = [p, i, i64, i64, p, i64, i, p, p, i, i, i, i, p, p, p, p, i, p]
+    L.mxfp8_moe_combine.restype = i
+    L.mxfp8_moe_combine.argtypes = [p, i, i64, i64, p, p, i64, i, p, i, p]
+    L.mxfp8_moe_combine_grad.restype = i
+    L.mxfp8_moe_combine_grad.argtypes = [p, i, i64, i64, p, i, i64, p, p, i, p, p, i, p, p, p]
+    L.mxfp8_e2m1_packed_bytes.restype = sz
+    L.mxfp8_e2m1_packed_bytes.argtypes = [i64, i64, i64]
+    L.mxfp8_e2m1_pack.restype = i
+    L.mxfp8_e2m1_pack.argtypes = [p, p, i64, i64, i64, p, p]
+    L.mxfp8_e2m1_matvec.restype = i
+    L.mxfp8_e2m1_matvec.argtypes = [p, i64, i64, p, i64, i64, p, i, p, i, p]
     L.mxfp8_gemm_last_clock.restype = i
     L.mxfp8_gemm_last_clock.argtypes = [p, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
     L.mxfp8_enable_peer_access.restype = i
@@ -426,3 +446,125 @@ def mxfp8_glu_quantize(src: torch.Tensor, act: int, orientation: int, scale_rule
     _check(lib().mxfp8_glu_quantize(_ptr(src), _dtype_code(src), rows, two_cols // 2, act, orientation, scale_rule, elem,
                                     _ptr(q_row), _ptr(s_row), _ptr(q_col), _ptr(s_col), sf_layout,
                                     _stream(stream)), "mxfp8_glu_quantize")
+
+
+def _on_device(stream, **tensors) -> None:
+    """Every tensor lies on the device that the call's stream belongs to (a launch elsewhere would read foreign addresses)."""
+    device = torch.cuda.current_device() if stream is None else stream.device.index
+    for name, t in tensors.items():
+        if t is not None and not (t.is_cuda and t.device.index == device):
+            raise ValueError("%s is on %s, the call runs on cuda:%d" % (name, t.device, device))
+    if device != torch.cuda.current_device():
+        raise ValueError("the call runs on the current device, cuda:%d: its stream belongs to cuda:%d" % (torch.cuda.current_device(), device))
+
+
+def _int32(**tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and t.dtype != torch.int32:
+            raise TypeError("%s must be int32" % name)
+
+
+def mxfp8_moe_rows(tokens: int, top_k: int, num_experts: int) -> int:
+    return int(lib().mxfp8_moe_rows(tokens, top_k, num_experts))
+
+
+def mxfp8_moe_sort_ws_bytes(tokens: int, top_k: int, num_experts: int) -> int:
+    return int(lib().mxfp8_moe_sort_ws_bytes(tokens, top_k, num_experts))
+
+
+def mxfp8_moe_sort(expert_ids: torch.Tensor, num_experts: int, group_offsets: torch.Tensor, row_of: torch.Tensor, slot_of: torch.Tensor,
+                   ws=None, stream=None) -> None:
+    """expert_ids, row_of: [tokens, top_k]; group_offsets: [num_experts + 1]; slot_of: [rows], rows >= mxfp8_moe_rows(...)."""
+    tokens, top_k = expert_ids.shape
+    _int32(expert_ids=expert_ids, group_offsets=group_offsets, row_of=row_of, slot_of=slot_of)
+    _on_device(stream, expert_ids=expert_ids, group_offsets=group_offsets, row_of=row_of, slot_of=slot_of, ws=ws)
+    if group_offsets.numel() != num_experts + 1 or row_of.shape != expert_ids.shape:
+        raise ValueError("group_offsets holds num_experts + 1 numbers, row_of has the shape of expert_ids")
+    _check(lib().mxfp8_moe_sort(_ptr(expert_ids), tokens, top_k, num_experts, _ptr(group_offsets), _ptr(row_of), _ptr(slot_of), slot_of.numel(),
+                                _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "mxfp8_moe_sort")
+
+
+def mxfp8_moe_dispatch_quantize(src: torch.Tensor, slot_of: torch.Tensor, top_k: int, weights, group_offsets: torch.Tensor,
+                                orientation: int, scale_rule: int, elem: int, q_row, s_row, q_col, s_col, sf_layout: int, stream=None) -> None:
+    """src: [tokens, cols]; slot_of: [rows]; weights: None or FP32 [tokens, top_k]; outputs as mxfp8_quantize of [rows, cols]."""
+    tokens, cols = src.shape
+    rows = slot_of.numel()
+    _int32(slot_of=slot_of, group_offsets=group_offsets)
+    _on_device(stream, src=src, slot_of=slot_of, weights=weights, group_offsets=group_offsets, q_row=q_row, s_row=s_row, q_col=q_col, s_col=s_col)
+    _float_weights(weights, tokens, top_k)
+    for o, q, s in ((ROW, q_row, s_row), (COL, q_col, s_col)):
+        if orientation & o and q is not None and s is not None and rows % 128 == 0:
+            if q.numel() * q.element_size() < rows * cols or s.numel() * s.element_size() < mxfp8_scale_bytes(rows, cols, o, sf_layout):
+                raise ValueError("an output is smaller than [%d, %d] needs" % (rows, cols))
+    _check(lib().mxfp8_moe_dispatch_quantize(_ptr(src), _dtype_code(src), tokens, cols, _ptr(slot_of), rows, top_k, _ptr(weights),
+                                             _ptr(group_offsets), group_offsets.numel() - 1, orientation, scale_rule, elem,
+                                             _ptr(q_row), _ptr(s_row), _ptr(q_col), _ptr(s_col), sf_layout, _stream(stream)),
+           "mxfp8_moe_dispatch_quantize")
+
+
+def _float_weights(weights, tokens: int, top_k: int) -> None:
+    if weights is not None and (weights.dtype != torch.float32 or tuple(weights.shape) != (tokens, top_k)):
+        raise TypeError("weights must be float32 [tokens, top_k]")
+
+
+def mxfp8_moe_combine(src: torch.Tensor, row_of: torch.Tensor, weights, dst: torch.Tensor, stream=None) -> None:
+    """src: [rows, cols]; row_of: [tokens, top_k]; weights: None or FP32 [tokens, top_k]; dst: [tokens, cols]."""
+    rows, cols = src.shape
+    tokens, top_k = row_of.shape
+    _int32(row_of=row_of)
+    _on_device(stream, src=src, row_of=row_of, weights=weights, dst=dst)
+    _float_weights(weights, tokens, top_k)
+    if tuple(dst.shape) != (tokens, cols):
+        raise ValueError("dst must be [tokens, cols]")
+    _check(lib().mxfp8_moe_combine(_ptr(src), _dtype_code(src), rows, cols, _ptr(row_of), _ptr(weights), tokens, top_k, _ptr(dst),
+                                   _dtype_code(dst), _stream(stream)), "mxfp8_moe_combine")
+
+
+def mxfp8_moe_combine_grad(dy: torch.Tensor, src: torch.Tensor, row_of: torch.Tensor, slot_of: torch.Tensor, weights, group_offsets: torch.Tensor,
+                           d_src, d_weights, stream=None) -> None:
+    """dy: [tokens, cols]; src, d_src: [rows, cols]; row_of, weights, d_weights: [tokens, top_k]; d_src or d_weights may be None."""
+    tokens, cols = dy.shape
+    rows = src.shape[0]
+    _int32(row_of=row_of, slot_of=slot_of, group_offsets=group_offsets)
+    _on_device(stream, dy=dy, src=src, row_of=row_of, slot_of=slot_of, weights=weights, group_offsets=group_offsets, d_src=d_src, d_weights=d_weights)
+    top_k = row_of.shape[1]
+    _float_weights(weights, tokens, top_k)
+    _float_weights(d_weights, tokens, top_k)
+    if row_of.shape[0] != tokens or src.shape[1] != cols or slot_of.numel() != rows or (d_src is not None and (d_src.shape != src.shape or d_src.dtype != src.dtype)):
+        raise ValueError("shapes or types of dy, src, d_src, row_of and slot_of do not agree")
+    _check(lib().mxfp8_moe_combine_grad(_ptr(dy), _dtype_code(dy), tokens, cols, _ptr(src), _dtype_code(src), rows, _ptr(row_of), _ptr(slot_of), top_k,
+                                        _ptr(weights), _ptr(group_offsets), group_offsets.numel() - 1, _ptr(d_src), _ptr(d_weights),
+                                        _stream(stream)), "mxfp8_moe_combine_grad")
+
+
+def mxfp8_e2m1_packed_bytes(num_matrices: int, rows: int, cols: int) -> int:
+    return int(lib().mxfp8_e2m1_packed_bytes(num_matrices, rows, cols))
+
+
+def mxfp8_e2m1_pack(q: torch.Tensor, s: torch.Tensor, num_matrices: int, packed: torch.Tensor, stream=None) -> None:
+    """q: [num_matrices * rows, cols] E2M1 slots and s: their linear ROW scales, as mxfp8_quantize writes them."""
+    all_rows, cols = q.shape
+    _on_device(stream, q=q, s=s, packed=packed)
+    if num_matrices < 1 or all_rows % num_matrices:
+        raise ValueError("q holds num_matrices matrices of the same number of rows")
+    rows = all_rows // num_matrices
+    if s.numel() * s.element_size() < all_rows * (cols // 32) or packed.numel() * packed.element_size() < mxfp8_e2m1_packed_bytes(num_matrices, rows, cols):
+        raise ValueError("s or packed is too small")
+    _check(lib().mxfp8_e2m1_pack(_ptr(q), _ptr(s), num_matrices, rows, cols, _ptr(packed), _stream(stream)), "mxfp8_e2m1_pack")
+
+
+def mxfp8_e2m1_matvec(x: torch.Tensor, packed: torch.Tensor, num_matrices: int, matrix_ids, y: torch.Tensor, stream=None) -> None:
+    """x: BF16 [tokens, cols]; matrix_ids: None (one matrix) or int32 [tokens, choices]; y: [tokens * choices, rows]."""
+    tokens, cols = x.shape
+    if x.dtype != torch.bfloat16:
+        raise TypeError("x must be bfloat16")
+    _int32(matrix_ids=matrix_ids)
+    _on_device(stream, x=x, packed=packed, matrix_ids=matrix_ids, y=y)
+    per_token = 1 if matrix_ids is None else matrix_ids.shape[1]
+    if (matrix_ids is not None and matrix_ids.shape[0] != tokens) or y.shape[0] != tokens * per_token:
+        raise ValueError("y holds one row per token and choice")
+    rows = y.shape[1]
+    if packed.numel() * packed.element_size() < mxfp8_e2m1_packed_bytes(num_matrices, rows, cols):
+        raise ValueError("packed is smaller than num_matrices matrices of [%d, %d]" % (rows, cols))
+    _check(lib().mxfp8_e2m1_matvec(_ptr(x), tokens, cols, _ptr(packed), num_matrices, rows, _ptr(matrix_ids), per_token, _ptr(y),
+                                   _dtype_code(y), _stream(stream)), "mxfp8_e2m1_matvec")

@@ -115,6 +115,13 @@ bool gemm_device(GemmDevice& out)
     });
 }
 }  // namespace gemm
+
+int* device_status_word()
+{
+    GemmDevice d;
+    return gemm_device(d) ? d.status : nullptr;
+}
+
 namespace {
 
 // D can be stored straight from registers when every row segment of 32 bytes is aligned (see GemmParams::d_direct);
