@@ -26,30 +26,30 @@ namespace {
 
 constexpr int TILE_ROWS = 16, TILE_COLS = 128, TILE_CODES = 1024, TILE_BYTES = 1088;
 constexpr int MV_WARPS = 8, MV_THREADS = 32 * MV_WARPS;
-constexpr int MV_MAX_SLOTS = 1024;       // (token, choice) pairs of one call
+constexpr int MV_MAX_SLOTS = 1024;              // (token, choice) pairs of one call
 
 struct MatvecArgs {
     const __nv_bfloat16* x;      // [tokens, cols]
     const uint8_t* packed;       // [matrices][row tiles][column tiles][1088]
     const int32_t* ids;          // [slots] or null: matrix 0 for all
     void* y;                     // [slots, rows]
-    int slots, per_token, matrices;
+    int slots, per_token, matrices, by_matrix;
     int64_t rows, cols;
     int row_tiles, col_tiles;
+    int split;                   // warps that share a row group and split its columns (1, 2, 4 or 8)
 };
 
-// Code pairs p = 0 .. 3 of a word as BF16 pairs (column 2p in the low half).
-__device__ __forceinline__ void decode_word(uint32_t w, uint32_t (&out)[4])
+// Code pairs p = 0 .. 3 of a word as BF16 pairs (column 2p in the low half), times `scale` (both halves: 2^126 X).
+__device__ __forceinline__ void decode_word(uint32_t w, uint32_t scale, uint32_t (&out)[4])
 {
     constexpr uint32_t V = 0x01C001C0u, S = 0x80008000u;
     out[0] = w & (V | S);
     out[1] = (w << 3) & (V | S);
     out[2] = ((w << 6) & V) | ((w << 1) & S);
     out[3] = ((w >> 3) & V) | ((w << 2) & S);
-    const __nv_bfloat162 up = __halves2bfloat162(__ushort_as_bfloat16(0x7E80), __ushort_as_bfloat16(0x7E80));      // 2^126
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-        const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&out[p]), up);
+        const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&out[p]), *reinterpret_cast<const __nv_bfloat162*>(&scale));
         out[p] = *reinterpret_cast<const uint32_t*>(&v);
     }
 }
@@ -65,96 +65,275 @@ __device__ __forceinline__ float scale_value(uint32_t b)
 {
     return __uint_as_float(b == 0u ? 0x00400000u : (b == 255u ? 0x7FC00000u : b << 23));
 }
+// 2^126 * 2^(b - 127) as BF16, for b <= 127: exponent field b + 126.  Two words hold a row's four factors, one per half, and
+// the product names the half that it takes.
+template <int G>
+__device__ __forceinline__ __nv_bfloat162 half_of(const uint32_t (&f)[2])
+{
+    const __nv_bfloat162 v = *reinterpret_cast<const __nv_bfloat162*>(&f[G & 1]);
+    return (G >> 1) ? __high2bfloat162(v) : __low2bfloat162(v);
+}
+__device__ __forceinline__ void factors(uint32_t bytes, uint32_t (&f)[2])
+{
+    f[0] = (bytes & 0x00FF00FFu) * 128u + 0x3F003F00u;              // groups 0 and 2
+    f[1] = ((bytes >> 8) & 0x00FF00FFu) * 128u + 0x3F003F00u;       // groups 1 and 3
+}
+// One lane's share of R row tiles and of the activations under them.
+template <int R, int NT>
+struct Operands {
+    uint4 lo[R], hi[R];           // rows (lane / 4) and (lane / 4) + 8: a word of eight codes per group
+    uint32_t s_lo[R], s_hi[R];    // their scale bytes, one per group
+    uint4 x[NT][4];               // token lane / 4 of every block: eight columns per group
+    __device__ __forceinline__ void load(const uint8_t* const (&tile)[R], int64_t w_at, const __nv_bfloat16* const (&from)[NT], const bool (&has)[NT], int64_t x_at, int lane)
+    {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            lo[r] = __ldcs(reinterpret_cast<const uint4*>(tile[r] + w_at));
+            hi[r] = __ldcs(reinterpret_cast<const uint4*>(tile[r] + w_at + 512));
+            s_lo[r] = __ldcs(reinterpret_cast<const uint32_t*>(tile[r] + w_at + TILE_CODES - lane * 16 + (lane >> 2) * 4));
+            s_hi[r] = __ldcs(reinterpret_cast<const uint32_t*>(tile[r] + w_at + TILE_CODES - lane * 16 + (lane >> 2) * 4 + 32));
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+            if (has[t])
+#pragma unroll
+                for (int g = 0; g < 4; ++g) x[t][g] = *reinterpret_cast<const uint4*>(from[t] + x_at + g * 32);
+    }
+};
+
+template <int R, int NT>
+__device__ __forceinline__ void product(const Operands<R, NT>& o, float (&acc)[R][NT][4])
+{
+    uint32_t any = 0u, all = 0xFFFFFFFFu;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        any |= o.s_lo[r] | o.s_hi[r];
+        all &= o.s_lo[r] & o.s_hi[r];
+    }
+    const bool wide = ((any & 0x80808080u) | (~all & 0x40404040u)) != 0u;             // a byte outside 64 .. 127
+    if (!__any_sync(0xFFFFFFFFu, wide)) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint32_t wl[4] = {o.lo[r].x, o.lo[r].y, o.lo[r].z, o.lo[r].w}, wh[4] = {o.hi[r].x, o.hi[r].y, o.hi[r].z, o.hi[r].w};
+            float d[NT][4];
+            uint32_t fl[2], fh[2];
+            factors(o.s_lo[r], fl);
+            factors(o.s_hi[r], fh);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) d[t][i] = 0.f;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                uint32_t al[4], ah[4];
+                const __nv_bfloat162 sl = g == 0 ? half_of<0>(fl) : (g == 1 ? half_of<1>(fl) : (g == 2 ? half_of<2>(fl) : half_of<3>(fl)));
+                const __nv_bfloat162 sh = g == 0 ? half_of<0>(fh) : (g == 1 ? half_of<1>(fh) : (g == 2 ? half_of<2>(fh) : half_of<3>(fh)));
+                decode_word(wl[g], *reinterpret_cast<const uint32_t*>(&sl), al);
+                decode_word(wh[g], *reinterpret_cast<const uint32_t*>(&sh), ah);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    mma_bf16(d[t], al[0], ah[0], al[1], ah[1], o.x[t][g].x, o.x[t][g].y);
+                    mma_bf16(d[t], al[2], ah[2], al[3], ah[3], o.x[t][g].z, o.x[t][g].w);
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[r][t][i] += d[t][i];
+        }
+        return;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t wl[4] = {o.lo[r].x, o.lo[r].y, o.lo[r].z, o.lo[r].w}, wh[4] = {o.hi[r].x, o.hi[r].y, o.hi[r].z, o.hi[r].w};
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            uint32_t al[4], ah[4];
+            decode_word(wl[g], 0x7E807E80u, al);                // 2^126
+            decode_word(wh[g], 0x7E807E80u, ah);
+            const float f_lo = scale_value(o.s_lo[r] >> (8 * g) & 255u), f_hi = scale_value(o.s_hi[r] >> (8 * g) & 255u);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float d[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_bf16(d, al[0], ah[0], al[1], ah[1], o.x[t][g].x, o.x[t][g].y);
+                mma_bf16(d, al[2], ah[2], al[3], ah[3], o.x[t][g].z, o.x[t][g].w);
+                acc[r][t][0] = fmaf(f_lo, d[0], acc[r][t][0]);
+                acc[r][t][1] = fmaf(f_lo, d[1], acc[r][t][1]);
+                acc[r][t][2] = fmaf(f_hi, d[2], acc[r][t][2]);
+                acc[r][t][3] = fmaf(f_hi, d[3], acc[r][t][3]);
+            }
+        }
+    }
+}
 
 template <typename T> __device__ __forceinline__ T to_out(float v);
 template <> __device__ __forceinline__ float to_out<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 to_out<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// CTA (i, u): 16 rows of a matrix times the slots that chose it, eight at a time; the eight warps split the columns and
-// add their sums in a fixed order.  u counts slots (the first slot with a matrix works for all of them, the others
-// leave) or, where there are fewer matrices than slots, matrices.
-template <typename OUT>
-__global__ void __launch_bounds__(MV_THREADS) matvec_kernel(const MatvecArgs a, int by_matrix)
+template <int R, int NT> constexpr int WARP_SUMS = R * TILE_ROWS * (8 * NT + 1);      // floats of a warp's sums, padded
+
+// CTA (i, u): groups of R row tiles times the slots that chose a matrix, 8 NT at a time.  `split` warps share a group and
+// take its column tiles in turn; their sums meet in shared memory and are added in a fixed order.  Weights and activations go
+// from global memory to the registers that the tensor instructions read them from; other warps cover the latency, or,
+// where registers leave few of them (AHEAD), the next tile's loads run under this tile's products.
+// u counts slots (the first slot with a matrix works for all of them, the others leave) or, where there are fewer
+// matrices than slots, matrices.
+template <typename OUT, int R, int NT, int PER_SM, bool AHEAD>
+__global__ void __launch_bounds__(MV_THREADS, PER_SM) matvec_kernel(const MatvecArgs a)
 {
+    extern __shared__ float sums[];
     __shared__ int list[MV_MAX_SLOTS];
-    __shared__ float sums[MV_WARPS][TILE_ROWS][9];      // 8 tokens per row, padded
     __shared__ int listed;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, u = blockIdx.y;
-    int matrix = 0;
-    if (a.ids == nullptr) {
-        for (int i = tid; i < a.slots; i += MV_THREADS) list[i] = i;
-        if (tid == 0) listed = a.slots;
-    } else {
-        matrix = by_matrix ? u : a.ids[u];
+    const int groups = MV_WARPS / a.split;                                 // row groups of this CTA
+    const int64_t row0 = (int64_t)blockIdx.x * groups * R * TILE_ROWS;     // its first row
+    const int cta_rows = groups * R * TILE_ROWS;
+    OUT* y = static_cast<OUT*>(a.y);
+    int matrix = 0, count = a.slots;
+    if (a.ids != nullptr) {
+        matrix = a.by_matrix ? u : a.ids[u];
         if ((unsigned)matrix >= (unsigned)a.matrices) {
             // no such matrix: this slot's rows are zero
-            const int64_t n = (int64_t)blockIdx.x * TILE_ROWS + tid;
-            if (tid < TILE_ROWS && n < a.rows) static_cast<OUT*>(a.y)[(int64_t)u * a.rows + n] = to_out<OUT>(0.f);
+            for (int n = tid; n < cta_rows; n += MV_THREADS)
+                if (row0 + n < a.rows) y[(int64_t)u * a.rows + row0 + n] = to_out<OUT>(0.f);
             return;
         }
         if (warp == 0) {
-            int count = 0, first = -1;
+            int found = 0, first = -1;
             for (int base = 0; base < a.slots; base += 32) {
                 const int s = base + lane;
                 const unsigned hit = __ballot_sync(0xFFFFFFFFu, s < a.slots && a.ids[min(s, a.slots - 1)] == matrix);
                 if (hit && first < 0) first = base + __ffs(hit) - 1;
-                if (hit >> lane & 1u) list[count + __popc(hit & ((1u << lane) - 1u))] = s;
-                count += __popc(hit);
+                if (hit >> lane & 1u) list[found + __popc(hit & ((1u << lane) - 1u))] = s;
+                found += __popc(hit);
             }
-            if (lane == 0) listed = (by_matrix || first == u) ? count : 0;
+            if (lane == 0) listed = (a.by_matrix || first == u) ? found : 0;
         }
-        if (by_matrix && blockIdx.y == 0) {             // slots without a matrix: theirs are zero
-            const int64_t n = (int64_t)blockIdx.x * TILE_ROWS + (tid & 15);
-            for (int s = tid >> 4; s < a.slots; s += MV_THREADS / 16)
-                if ((unsigned)a.ids[s] >= (unsigned)a.matrices && n < a.rows) static_cast<OUT*>(a.y)[(int64_t)s * a.rows + n] = to_out<OUT>(0.f);
-        }
-    }
-    __syncthreads();
-    const int count = listed;
-    const int row = lane >> 2, quarter = lane & 3;      // of the tensor instructions' operands
-    const uint8_t* tiles = a.packed + ((int64_t)matrix * a.row_tiles + blockIdx.x) * a.col_tiles * TILE_BYTES;
-    for (int s0 = 0; s0 < count; s0 += 8) {
-        const bool has = s0 + row < count;
-        const __nv_bfloat16* x = a.x + (has ? (int64_t)(list[s0 + row] / a.per_token) * a.cols : 0) + quarter * 8;
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int kt = warp; kt < a.col_tiles; kt += MV_WARPS) {
-            const uint8_t* tile = tiles + (int64_t)kt * TILE_BYTES;
-            const uint4 lo = *reinterpret_cast<const uint4*>(tile + lane * 16), hi = *reinterpret_cast<const uint4*>(tile + 512 + lane * 16);
-            const uint32_t s_lo = *reinterpret_cast<const uint32_t*>(tile + TILE_CODES + row * 4), s_hi = *reinterpret_cast<const uint32_t*>(tile + TILE_CODES + 32 + row * 4);
-            const uint32_t w_lo[4] = {lo.x, lo.y, lo.z, lo.w}, w_hi[4] = {hi.x, hi.y, hi.z, hi.w};
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int64_t k = (int64_t)kt * TILE_COLS + g * 32;
-                uint4 b = make_uint4(0u, 0u, 0u, 0u);
-                if (has && k < a.cols) b = *reinterpret_cast<const uint4*>(x + k);
-                uint32_t al[4], ah[4];
-                decode_word(w_lo[g], al);
-                decode_word(w_hi[g], ah);
-                float d[4] = {0.f, 0.f, 0.f, 0.f};
-                mma_bf16(d, al[0], ah[0], al[1], ah[1], b.x, b.y);
-                mma_bf16(d, al[2], ah[2], al[3], ah[3], b.z, b.w);
-                const float f_lo = scale_value(s_lo >> (8 * g) & 255u), f_hi = scale_value(s_hi >> (8 * g) & 255u);
-                acc[0] = fmaf(f_lo, d[0], acc[0]);
-                acc[1] = fmaf(f_lo, d[1], acc[1]);
-                acc[2] = fmaf(f_hi, d[2], acc[2]);
-                acc[3] = fmaf(f_hi, d[3], acc[3]);
-            }
-        }
-        sums[warp][row][2 * quarter] = acc[0];
-        sums[warp][row][2 * quarter + 1] = acc[1];
-        sums[warp][row + 8][2 * quarter] = acc[2];
-        sums[warp][row + 8][2 * quarter + 1] = acc[3];
+        if (a.by_matrix && u == 0)                      // slots without a matrix: theirs are zero
+            for (int s = warp; s < a.slots; s += MV_WARPS)
+                if ((unsigned)a.ids[s] >= (unsigned)a.matrices)
+                    for (int n = lane; n < cta_rows; n += 32)
+                        if (row0 + n < a.rows) y[(int64_t)s * a.rows + row0 + n] = to_out<OUT>(0.f);
         __syncthreads();
-        if (tid < 8 * TILE_ROWS) {
-            const int r = tid & 15, j = tid >> 4;
-            const int64_t n = (int64_t)blockIdx.x * TILE_ROWS + r;
+        count = listed;
+    }
+    auto slot = [&](int i) { return a.ids ? list[i] : i; };
+    const int token = lane >> 2, quarter = lane & 3;    // as columns of the tensor instructions' second operand
+    const int group = warp / a.split, part = warp % a.split;
+    const int rt0 = (blockIdx.x * groups + group) * R;  // this warp's first row tile
+    const uint8_t* tile[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)                         // rows behind the matrix repeat its last tile and are not stored
+        tile[r] = a.packed + ((int64_t)matrix * a.row_tiles + min(rt0 + r, a.row_tiles - 1)) * a.col_tiles * TILE_BYTES + lane * 16;
+    const int whole = (int)(a.cols / TILE_COLS);        // column tiles without padding
+    for (int s0 = 0; s0 < count; s0 += 8 * NT) {
+        const int tokens = min(8 * NT, count - s0);
+        const __nv_bfloat16* x[NT];
+        bool has[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            has[t] = 8 * t + token < tokens;
+            x[t] = a.x + (has[t] ? (int64_t)(slot(s0 + 8 * t + token) / a.per_token) * a.cols : 0) + quarter * 8;
+        }
+        float acc[R][NT][4];
+        Operands<R, NT> now;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) now.x[t][g] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[r][t][i] = 0.f;
+        int kt = part;
+        if constexpr (!AHEAD) {
+            for (; kt < whole; kt += a.split) {
+                now.load(tile, (int64_t)kt * TILE_BYTES, x, has, (int64_t)kt * TILE_COLS, lane);
+                product<R, NT>(now, acc);
+            }
+        } else {
+            Operands<R, NT> next = now;
+            if (kt < whole) now.load(tile, (int64_t)kt * TILE_BYTES, x, has, (int64_t)kt * TILE_COLS, lane);
+            while (kt < whole) {
+                kt += a.split;
+                if (kt < whole) next.load(tile, (int64_t)kt * TILE_BYTES, x, has, (int64_t)kt * TILE_COLS, lane);
+                product<R, NT>(now, acc);
+                if (kt >= whole) break;
+                kt += a.split;
+                if (kt < whole) now.load(tile, (int64_t)kt * TILE_BYTES, x, has, (int64_t)kt * TILE_COLS, lane);
+                product<R, NT>(next, acc);
+            }
+        }
+        if (whole < a.col_tiles && whole % a.split == part) {      // the columns end inside the last tile
+            bool none[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) none[t] = false;
+            now.load(tile, (int64_t)whole * TILE_BYTES, x, none, 0, lane);
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int64_t k = (int64_t)whole * TILE_COLS + g * 32;
+                    now.x[t][g] = make_uint4(0u, 0u, 0u, 0u);
+                    if (has[t] && k < a.cols) now.x[t][g] = *reinterpret_cast<const uint4*>(x[t] + k);
+                }
+            product<R, NT>(now, acc);
+        }
+        constexpr int P = 8 * NT + 1;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float* to = sums + warp * WARP_SUMS<R, NT> + (r * TILE_ROWS + token) * P + 8 * t + 2 * quarter;
+                to[0] = acc[r][t][0];
+                to[1] = acc[r][t][1];
+                to[8 * P] = acc[r][t][2];
+                to[8 * P + 1] = acc[r][t][3];
+            }
+        __syncthreads();
+        for (int i = tid; i < cta_rows * tokens; i += MV_THREADS) {
+            const int n = i % cta_rows, j = i / cta_rows;
+            const int g = n / (R * TILE_ROWS), m = n % (R * TILE_ROWS);
             float v = 0.f;
-#pragma unroll
-            for (int w = 0; w < MV_WARPS; ++w) v += sums[w][r][j];
-            if (s0 + j < count && n < a.rows) static_cast<OUT*>(a.y)[(int64_t)list[s0 + j] * a.rows + n] = to_out<OUT>(v);
+            for (int w = 0; w < a.split; ++w) v += sums[(g * a.split + w) * WARP_SUMS<R, NT> + m * P + j];
+            if (row0 + n < a.rows) y[(int64_t)slot(s0 + j) * a.rows + row0 + n] = to_out<OUT>(v);
         }
         __syncthreads();
     }
+}
+
+template <typename OUT, int R, int NT, int PER_SM, bool AHEAD>
+cudaError_t launch_matvec(MatvecArgs a, unsigned grid_y, cudaStream_t st)
+{
+    auto kernel = matvec_kernel<OUT, R, NT, PER_SM, AHEAD>;
+    constexpr int SUMS = MV_WARPS * WARP_SUMS<R, NT> * (int)sizeof(float);
+    static unsigned long long set = 0;
+    cudaError_t err = ensure_dynamic_smem(kernel, SUMS, set);
+    if (err != cudaSuccess) return err;
+    a.split = 1;
+    while (a.split < MV_WARPS && a.split < a.col_tiles) a.split <<= 1;
+    auto ctas = [&](int split) { return (int64_t)((a.row_tiles + MV_WARPS / split * R - 1) / (MV_WARPS / split * R)); };
+    // Longer runs per warp wherever at least two full waves of CTAs remain: 2816 x 2048 matrices of six experts for eight
+    // tokens take 34 us with two warps to a row group and 43 us with eight; one 28672 x 4096 matrix, whose waves would
+    // run out, 25 us with two and 22 us with eight.
+    while (a.split > 1 && ctas(a.split >> 1) * grid_y >= 2 * PER_SM * 148) a.split >>= 1;
+    kernel<<<dim3((unsigned)ctas(a.split), grid_y), MV_THREADS, SUMS, st>>>(a);
+    count_launch(1);
+    return cudaGetLastError();
+}
+
+// Tokens worked on together: 8, 16 or 32 (a matrix's slots are seldom more than a few when they choose).  Two row tiles to a
+// group halve the reads of the activations; one keeps more multiprocessors busy while there are few row tiles (6144 x
+// 4096 for one token: 6.2 us with one, 6.9 us with two; 28672 x 4096 for 16 tokens: 33 us with one, 31 us with two).
+template <typename OUT>
+cudaError_t launch_matvec(const MatvecArgs& a, unsigned grid_y, cudaStream_t st)
+{
+    const bool few = (int64_t)(a.row_tiles + 1) / 2 * grid_y < 4 * 148;
+    if (a.slots <= 8 || a.ids) return few ? launch_matvec<OUT, 1, 1, 4, false>(a, grid_y, st) : launch_matvec<OUT, 2, 1, 3, false>(a, grid_y, st);
+    if (a.slots <= 16) return few ? launch_matvec<OUT, 1, 2, 3, false>(a, grid_y, st) : launch_matvec<OUT, 2, 2, 2, false>(a, grid_y, st);
+    return few ? launch_matvec<OUT, 1, 4, 2, false>(a, grid_y, st) : launch_matvec<OUT, 2, 4, 1, true>(a, grid_y, st);
 }
 
 // One thread per word of eight codes of the packed layout, from the library's own slots (16 codes to 16 bytes, code i
@@ -220,17 +399,15 @@ extern "C" int mxfp8_e2m1_matvec(const void* x, int64_t tokens, int64_t cols, co
     if (tokens > MV_MAX_SLOTS || tokens * slots_per_token > MV_MAX_SLOTS || num_matrices > 65535) return MXFP8_ERR_UNSUPPORTED;
     MatvecArgs a{};
     const int64_t rt = (rows + TILE_ROWS - 1) / TILE_ROWS, kt = (cols + TILE_COLS - 1) / TILE_COLS;
-    if (rt > 0x7FFFFFFFLL || kt > 0x7FFFFFFFLL / MV_THREADS) return MXFP8_ERR_UNSUPPORTED;
+    if (rt > 0x7FFFFFFLL || kt > 0x7FFFFFFLL) return MXFP8_ERR_UNSUPPORTED;
     a.x = static_cast<const __nv_bfloat16*>(x);
     a.packed = static_cast<const uint8_t*>(packed);
     a.ids = matrix_ids; a.y = y;
     a.slots = (int)(tokens * slots_per_token); a.per_token = slots_per_token; a.matrices = (int)num_matrices;
     a.rows = rows; a.cols = cols; a.row_tiles = (int)rt; a.col_tiles = (int)kt;
-    const int by_matrix = matrix_ids && num_matrices < a.slots;
-    const dim3 grid((unsigned)rt, (unsigned)(!matrix_ids ? 1 : (by_matrix ? num_matrices : a.slots)));
+    a.by_matrix = matrix_ids && num_matrices < a.slots;
+    const unsigned grid_y = (unsigned)(!matrix_ids ? 1 : (a.by_matrix ? num_matrices : a.slots));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (y_dtype == MXFP8_BF16) matvec_kernel<__nv_bfloat16><<<grid, MV_THREADS, 0, st>>>(a, by_matrix);
-    else matvec_kernel<float><<<grid, MV_THREADS, 0, st>>>(a, by_matrix);
-    count_launch(1);
-    return cudaGetLastError() == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
+    const cudaError_t err = y_dtype == MXFP8_BF16 ? launch_matvec<__nv_bfloat16>(a, grid_y, st) : launch_matvec<float>(a, grid_y, st);
+    return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
 }
