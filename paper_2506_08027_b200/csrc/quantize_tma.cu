@@ -18,8 +18,8 @@ int quantize_read_and_clear_status()
 // defined in quantize_tma_fp6_fp4.cu (opaque pointers: the batch types live in an unnamed namespace)
 cudaError_t quantize_tma_launch_fp6_fp4(int elem, bool bf16_src, int orientation, bool emulate, const void* maps,
                                         const void* batch, cudaStream_t st);
-// defined in quantize_tma_gather.cu
-cudaError_t quantize_tma_launch_gather(int elem, bool bf16_src, int orientation, const void* maps, const void* batch, cudaStream_t st);
+// defined in quantize_gather.cu
+cudaError_t quantize_launch_gather(int elem, bool bf16_src, int orientation, const void* batch, cudaStream_t st);
 
 namespace {
 
@@ -89,6 +89,7 @@ int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int 
     if (gather) {
         if (count != 1 || gated || second_src) return MXFP8_ERR_UNSUPPORTED;
         p.slot_of = gather->slot_of;
+        p.gather_src = items[0].src;
         p.used_rows = gather->used;
         p.slot_weights = gather->weights;
         p.top_k = (uint32_t)gather->top_k;
@@ -110,9 +111,9 @@ int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int 
                 return MXFP8_ERR_CUDA;
             continue;
         }
-        if (!make_map_2d(&ms.m[i], bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, bf ? 2 : 4,
-                         const_cast<void*>(it.src), (uint64_t)(gated ? 2 * it.cols : it.cols), (uint64_t)(gather ? gather->tokens : it.rows), t_cols,
-                         gather ? 1 : T_ROWS))
+        if (!gather &&
+            !make_map_2d(&ms.m[i], bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, bf ? 2 : 4,
+                         const_cast<void*>(it.src), (uint64_t)(gated ? 2 * it.cols : it.cols), (uint64_t)it.rows, t_cols, T_ROWS))
             return MXFP8_ERR_CUDA;
         if (i >= count) continue;
         QParams& q = p.t[i];
@@ -160,7 +161,7 @@ int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int 
 #endif
     cudaError_t err;
     if (gather) {
-        err = quantize_tma_launch_gather(elem, bf, orientation, &ms, &p, stream);
+        err = quantize_launch_gather(elem, bf, orientation, &p, stream);
         return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
     }
     switch (elem) {

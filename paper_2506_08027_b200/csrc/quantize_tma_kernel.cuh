@@ -178,34 +178,6 @@ __device__ __forceinline__ void glu_slab(uint8_t* gate, const uint8_t* up)
     }
 }
 
-// Gathered rows in place, same ownership as act_slab: row j of this warp's slab times its weight (one FP32 product,
-// rounded once to the source dtype), zero where the row has no slot.  A row without a slot holds some row of the source
-// (its load has to name one), which may be anything: it is overwritten, not multiplied.
-template <bool BF>
-__device__ __forceinline__ void gather_slab(uint8_t* mine, const float* __restrict__ row_weight, const uint8_t* __restrict__ row_live, bool weighted)
-{
-#pragma unroll 8
-    for (int j = 0; j < 32; ++j) {
-        const bool live = row_live[j] != 0;
-        if (live && !weighted) continue;
-        uint2 w = make_uint2(0u, 0u);
-        if (live) {
-            w = *reinterpret_cast<const uint2*>(mine + j * T_BYTES);
-            const float f = row_weight[j];
-            if constexpr (BF) {
-                const __nv_bfloat162 lo = __floats2bfloat162_rn(__uint_as_float(w.x << 16) * f, __uint_as_float(w.x & 0xFFFF0000u) * f);
-                const __nv_bfloat162 hi = __floats2bfloat162_rn(__uint_as_float(w.y << 16) * f, __uint_as_float(w.y & 0xFFFF0000u) * f);
-                w.x = *reinterpret_cast<const uint32_t*>(&lo);
-                w.y = *reinterpret_cast<const uint32_t*>(&hi);
-            } else {
-                w.x = __float_as_uint(__uint_as_float(w.x) * f);
-                w.y = __float_as_uint(__uint_as_float(w.y) * f);
-            }
-        }
-        *reinterpret_cast<uint2*>(mine + j * T_BYTES) = w;
-    }
-}
-
 // One launch converts up to QT_MAX_TENSORS tensors: their tiles are numbered one tensor after the
 // other and dealt out to the CTAs as one pool, so small tensors share one ramp-up and one tail and
 // the per-CTA tile counts even out.
@@ -222,9 +194,10 @@ struct QBatch {
     const void* beta;                     //   source dtype (added last); both null for RMS normalisation
     int glu_cols;                         // gated activation: the source is [rows, 2 * glu_cols] = (gate | up); 0 when unused
     int up_map;                           // two-source launches: tensor map of the second factor (1), or 0 when it is the up half of the first
-    const int* slot_of;                   // gather ahead of the conversion (one tensor): slot of every row (-1: none), rows in use
-    const int* used_rows;                 //   (device), a weight per slot or null, slots per source row, number of slots, and
-    const float* slot_weights;            //   the word that reports a bad array
+    const int* slot_of;                   // gathered conversion (quantize_gather.cu, one tensor): slot of every row (-1: none), rows in
+    const int* used_rows;                 //   use (device), a weight per slot or null, the source, slots per source row, number
+    const float* slot_weights;            //   of slots, and the word that reports a bad array
+    const void* gather_src;
     int* args_status;
     uint32_t top_k, top_k_magic, slots;
     int count;
@@ -538,10 +511,68 @@ __device__ __noinline__ void slab_careful(const uint8_t* __restrict__ my_in, uin
     }
 }
 
+// The scale bytes of one tile (1/32 of the output) leave from the staging arrays; the whole CTA calls.
+template <bool BF, bool DO_ROW, bool DO_COL, bool EMU>
+__device__ __forceinline__ void store_scales(const QParams& p, int tile_x, int tile_y, const uint8_t* sm_row, const uint8_t* sm_col,
+                                             int tid, int lane, int warp)
+{
+    constexpr int T_COLS = T_BYTES / (BF ? 2 : 4), NKB = T_COLS / 32;
+    const int64_t gcol0 = (int64_t)tile_x * T_COLS, grow0 = (int64_t)tile_y * T_ROWS;
+    // A BF16 tile wholly inside the tensor fills exactly one 512-byte atom of the swizzled layout per orientation,
+    // and the staging arrays are in the atom's order: one warp stores each atom, 16 bytes per lane.
+    if (BF && !EMU && p.sf_layout == MXFP8_SF_SWIZZLED && grow0 + T_ROWS <= p.rows && gcol0 + T_COLS <= p.cols &&
+        ((reinterpret_cast<uintptr_t>(p.s_row) | reinterpret_cast<uintptr_t>(p.s_col)) & 15) == 0) {
+        if (DO_ROW && warp == 0) {
+            const int64_t atoms_k = ((p.cols >> 5) + 3) >> 2;
+            *reinterpret_cast<uint4*>(p.s_row + ((int64_t)tile_y * atoms_k + tile_x) * 512 + lane * 16) =
+                *reinterpret_cast<const uint4*>(sm_row + lane * 16);
+        }
+        if (DO_COL && warp == (DO_ROW ? 1 : 0)) {
+            const int64_t atoms_r = ((p.rows >> 5) + 3) >> 2;
+            *reinterpret_cast<uint4*>(p.s_col + ((int64_t)tile_x * atoms_r + tile_y) * 512 + lane * 16) =
+                *reinterpret_cast<const uint4*>(sm_col + lane * 16);
+        }
+        return;
+    }
+    // every other tile (ragged, FP32 source, linear layout): one thread per row / per column
+    auto first_bytes = [](uint32_t word, int n) { return n >= 4 ? word : (word & ((1u << (8 * max(n, 0))) - 1u)); };
+    if (DO_ROW && !EMU && tid < T_ROWS) {
+        const int64_t r = grow0 + tid, ncb = p.cols >> 5, kb0 = (int64_t)tile_x * NKB;
+        const int nkb = (int)min((int64_t)NKB, ncb - kb0);
+        const uint32_t v = r < p.rows ? first_bytes(*reinterpret_cast<const uint32_t*>(sm_row + stage_offset(tid)), nkb) : 0u;
+        if (p.sf_layout == MXFP8_SF_SWIZZLED) {
+            // every row of a started 128-row atom is written (pad rows / pad K-blocks get 0)
+            uint8_t* d = p.s_row + ((int64_t)tile_y * ((ncb + 3) >> 2) + (kb0 >> 2)) * 512 + stage_offset(tid) + (kb0 & 3);
+            // a 64-column FP32 tile owns half of the atom's 4 K-blocks; the left half also zeroes
+            // the right half when no tile exists there (pad K-blocks)
+            if (NKB == 4 || ((kb0 & 3) == 0 && kb0 + NKB >= ncb)) *reinterpret_cast<uint32_t*>(d) = v;
+            else *reinterpret_cast<uint16_t*>(d) = (uint16_t)v;
+        } else if (r < p.rows) {
+            uint8_t* d = p.s_row + r * ncb + kb0;
+            for (int kb = 0; kb < nkb; ++kb) d[kb] = (uint8_t)(v >> (8 * kb));
+        }
+    }
+    if (DO_COL && !EMU && tid < T_COLS) {
+        const int64_t c = gcol0 + tid, nrb = p.rows >> 5, rb0 = (int64_t)tile_y * 4;
+        const int nrb_here = (int)min((int64_t)4, nrb - rb0);
+        const uint32_t v = c < p.cols ? first_bytes(*reinterpret_cast<const uint32_t*>(sm_col + stage_offset(tid)), nrb_here) : 0u;
+        if (p.sf_layout == MXFP8_SF_SWIZZLED) {
+            const int64_t padded_cols = ((p.cols + 127) >> 7) << 7;
+            if (c < padded_cols) {
+                *reinterpret_cast<uint32_t*>(p.s_col + ((c >> 7) * ((nrb + 3) >> 2) + tile_y) * 512 + (c & 31) * 16 + ((c >> 5) & 3) * 4) = v;
+                // pad columns no tile covers (FP32 tiles are 64 wide, atoms 128 wide)
+                if (T_COLS == 64 && tile_x == p.tiles_x - 1 && c + 64 >= (int64_t)p.tiles_x * 64 && c + 64 < padded_cols)
+                    *reinterpret_cast<uint32_t*>(p.s_col + (((c + 64) >> 7) * ((nrb + 3) >> 2) + tile_y) * 512 + ((c + 64) & 31) * 16 + (((c + 64) >> 5) & 3) * 4) = 0u;
+            }
+        } else if (c < p.cols) {
+            for (int w = 0; w < nrb_here; ++w) p.s_col[(rb0 + w) * p.cols + c] = (uint8_t)(v >> (8 * w));
+        }
+    }
+}
+
 // PRO: what runs on a tile before the conversion.  Separate instantiations, so that the plain conversion carries
 // none of the prologue code (folding the prologues in at run time cost the plain kernels 2-5 %).
-enum { PRO_NONE = 0, PRO_ELEMENTWISE = 1 /* activation or RMS normalisation */, PRO_GLU = 2 /* gated activation */,
-       PRO_GATHER = 3 /* rows gathered by an index, optionally weighted */ };
+enum { PRO_NONE = 0, PRO_ELEMENTWISE = 1 /* activation or RMS normalisation */, PRO_GLU = 2 /* gated activation */ };
 
 template <int DTYPE, int ELEM, bool DO_ROW, bool DO_COL, bool EMU, int PRO>
 __global__ void __launch_bounds__(QT_THREADS, QT_CTAS_PER_SM)
@@ -550,7 +581,6 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
     constexpr bool BF = (DTYPE == MXFP8_BF16);
     constexpr int VEC = BF ? 4 : 2;                 // elements per lane per row
     constexpr int T_COLS = T_BYTES / (BF ? 2 : 4);  // 128 or 64
-    constexpr int NKB = T_COLS / 32;                // row blocks per tile row: 4 or 2
     constexpr int LPB = 32 / VEC;                   // lanes per row block: 8 or 16
     constexpr bool GLU = (PRO == PRO_GLU);
 
@@ -560,9 +590,6 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
     uint64_t* bars = reinterpret_cast<uint64_t*>(sm_scales + 2048);   // [0 .. RING): ring slots; [RING]: the up tile (gated mode)
     uint8_t* up_buf = sm_scales + 2048 + 128;                         // gated mode only: [128][256], allocated by such launches
     const int glu_cols = GLU ? batch.glu_cols : 0;
-    constexpr bool GATHER = (PRO == PRO_GATHER);
-    float* row_weight = reinterpret_cast<float*>(sm_scales + 2048 + 128);               // gather mode only: RING x 128 weights,
-    uint8_t* row_live = sm_scales + 2048 + 128 + RING * T_ROWS * sizeof(float);         //   RING x 128 flags
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;   // warp = 32-row slab of the tile
     const uint32_t rule_offset = (batch.t[0].rule == MXFP8_RULE_PAPER) ? paper_offset<ELEM>() : 0u;
@@ -574,15 +601,7 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
     }
     __syncthreads();
 
-    int num_tiles = batch.tile_start[batch.count];
-    if constexpr (GATHER) {
-        // rows in use: whole 128-row tiles by construction of the sort; anything else is reported and nothing is stored
-        const int used = *batch.used_rows;
-        if (used < 0 || used > batch.t[0].rows || used % T_ROWS) {
-            if (tid == 0 && blockIdx.x == 0) atomicExch(batch.args_status, (int)MXFP8_ERR_DEVICE_ARGS);
-            num_tiles = 0;
-        } else num_tiles = (used / T_ROWS) * batch.t[0].tiles_x;
-    }
+    const int num_tiles = batch.tile_start[batch.count];
     int load_ti = 0;                          // tensor of the tile being loaded (tiles only move forward)
     auto issue_load = [&](int t, int buf) {   // one thread: tile t -> ring slot buf
 #ifdef MXFP8_TEST_HOOKS
@@ -595,35 +614,6 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
         asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"((uint32_t)IN_BYTES) : "memory");
         asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                      ::"r"(smem_addr(in_ring + buf * IN_BYTES)), "l"(&maps.m[load_ti]), "r"(b), "r"(lx * T_COLS), "r"(ly * T_ROWS)
-                     : "memory");
-    };
-    // gather mode, all lanes of warp 0: tile t -> ring slot buf.  Lane l fetches rows 4l .. 4l + 3 of the tile by one
-    // gathering copy (the box is one row high) and leaves their weights beside the slot; a row without a slot names source row 0.
-    auto issue_gather = [&](int t, int buf) {
-        int lx, ly;
-        divmod((uint32_t)t, (uint32_t)batch.t[0].tiles_x, batch.t[0].tiles_x_magic, ly, lx);
-        const int4 s4 = *reinterpret_cast<const int4*>(batch.slot_of + (int64_t)ly * T_ROWS + lane * 4);
-        const int slot[4] = {s4.x, s4.y, s4.z, s4.w};
-        int row[4];
-        float wt[4];
-        uint32_t live = 0u;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool ok = (uint32_t)slot[i] < batch.slots;
-            if (!ok && slot[i] != -1) atomicExch(batch.args_status, (int)MXFP8_ERR_DEVICE_ARGS);
-            int q, r;
-            divmod(ok ? (uint32_t)slot[i] : 0u, batch.top_k, batch.top_k_magic, q, r);
-            row[i] = q;
-            wt[i] = (ok && batch.slot_weights != nullptr) ? batch.slot_weights[slot[i]] : 1.f;
-            live |= ok ? (1u << (8 * i)) : 0u;
-        }
-        *reinterpret_cast<float4*>(row_weight + buf * T_ROWS + lane * 4) = make_float4(wt[0], wt[1], wt[2], wt[3]);
-        *reinterpret_cast<uint32_t*>(row_live + buf * T_ROWS + lane * 4) = live;
-        const uint32_t b = smem_addr(&bars[buf]);
-        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"((uint32_t)IN_BYTES) : "memory");
-        __syncwarp();
-        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
-                     ::"r"(smem_addr(in_ring + buf * IN_BYTES + lane * 4 * T_BYTES)), "l"(&maps.m[0]), "r"(b), "r"(lx * T_COLS), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3])
                      : "memory");
     };
     auto issue_up = [&](int t) {              // gated mode (one tensor per launch): the up half of tile t
@@ -675,14 +665,9 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
         for (int k = 0; k < RING; ++k) {
             t = next_tile(t);
             slot_tile[k] = t;
-            if (!GATHER && t < num_tiles) issue_load(t, k);
+            if (t < num_tiles) issue_load(t, k);
         }
         if (GLU && slot_tile[0] < num_tiles) issue_up(slot_tile[0]);
-    }
-    if (GATHER && warp == 0) {
-        __syncwarp();
-        for (int k = 0; k < RING; ++k)
-            if (slot_tile[k] < num_tiles) issue_gather(slot_tile[k], k);
     }
     __syncthreads();
     for (int it = 0;; ++it) {
@@ -741,11 +726,6 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
             __syncthreads();                     // every warp has consumed the up tile: fetch the next one under the conversion
             if (tid == 0 && slot_tile[(it + 1) % RING] < num_tiles) issue_up(slot_tile[(it + 1) % RING]);
         }
-        if constexpr (GATHER) {
-            gather_slab<BF>(in_tile + warp * 32 * T_BYTES + lane * 8, row_weight + buf * T_ROWS + warp * 32, row_live + buf * T_ROWS + warp * 32,
-                            batch.slot_weights != nullptr);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        }
         if (PRO == PRO_ELEMENTWISE && batch.rstd != nullptr) {
             // RMS normalisation in place (single-tensor launches only), then the unchanged conversion
             const int64_t row_first = grow0 + warp * 32;
@@ -796,64 +776,10 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
         if (__syncthreads_or((int)!ok)) { give_up(); return; }
         if (tid == 0) {
             slot_tile[buf] = refill;
-            if (!GATHER && refill < num_tiles) issue_load(refill, buf);
-        }
-        if (GATHER && warp == 0) {
-            const int t = __shfl_sync(0xFFFFFFFFu, refill, 0);
-            if (t < num_tiles) issue_gather(t, buf);
+            if (refill < num_tiles) issue_load(refill, buf);
         }
 
-        // ---- scale bytes (1/32 of the output) leave from the staging arrays ----------
-        // A BF16 tile wholly inside the tensor fills exactly one 512-byte atom of the swizzled layout per orientation,
-        // and the staging arrays are in the atom's order: one warp stores each atom, 16 bytes per lane.
-        if (BF && !EMU && p.sf_layout == MXFP8_SF_SWIZZLED && grow0 + T_ROWS <= p.rows && gcol0 + T_COLS <= p.cols &&
-            ((reinterpret_cast<uintptr_t>(p.s_row) | reinterpret_cast<uintptr_t>(p.s_col)) & 15) == 0) {
-            if (DO_ROW && warp == 0) {
-                const int64_t atoms_k = ((p.cols >> 5) + 3) >> 2;
-                *reinterpret_cast<uint4*>(p.s_row + ((int64_t)tile_y * atoms_k + tile_x) * 512 + lane * 16) =
-                    *reinterpret_cast<const uint4*>(sm_row + lane * 16);
-            }
-            if (DO_COL && warp == (DO_ROW ? 1 : 0)) {
-                const int64_t atoms_r = ((p.rows >> 5) + 3) >> 2;
-                *reinterpret_cast<uint4*>(p.s_col + ((int64_t)tile_x * atoms_r + tile_y) * 512 + lane * 16) =
-                    *reinterpret_cast<const uint4*>(sm_col + lane * 16);
-            }
-            continue;
-        }
-        // every other tile (ragged, FP32 source, linear layout): one thread per row / per column
-        auto first_bytes = [](uint32_t word, int n) { return n >= 4 ? word : (word & ((1u << (8 * max(n, 0))) - 1u)); };
-        if (DO_ROW && !EMU && tid < T_ROWS) {
-            const int64_t r = grow0 + tid, ncb = p.cols >> 5, kb0 = (int64_t)tile_x * NKB;
-            const int nkb = (int)min((int64_t)NKB, ncb - kb0);
-            const uint32_t v = r < p.rows ? first_bytes(*reinterpret_cast<const uint32_t*>(sm_row + stage_offset(tid)), nkb) : 0u;
-            if (p.sf_layout == MXFP8_SF_SWIZZLED) {
-                // every row of a started 128-row atom is written (pad rows / pad K-blocks get 0)
-                uint8_t* d = p.s_row + ((int64_t)tile_y * ((ncb + 3) >> 2) + (kb0 >> 2)) * 512 + stage_offset(tid) + (kb0 & 3);
-                // a 64-column FP32 tile owns half of the atom's 4 K-blocks; the left half also zeroes
-                // the right half when no tile exists there (pad K-blocks)
-                if (NKB == 4 || ((kb0 & 3) == 0 && kb0 + NKB >= ncb)) *reinterpret_cast<uint32_t*>(d) = v;
-                else *reinterpret_cast<uint16_t*>(d) = (uint16_t)v;
-            } else if (r < p.rows) {
-                uint8_t* d = p.s_row + r * ncb + kb0;
-                for (int kb = 0; kb < nkb; ++kb) d[kb] = (uint8_t)(v >> (8 * kb));
-            }
-        }
-        if (DO_COL && !EMU && tid < T_COLS) {
-            const int64_t c = gcol0 + tid, nrb = p.rows >> 5, rb0 = (int64_t)tile_y * 4;
-            const int nrb_here = (int)min((int64_t)4, nrb - rb0);
-            const uint32_t v = c < p.cols ? first_bytes(*reinterpret_cast<const uint32_t*>(sm_col + stage_offset(tid)), nrb_here) : 0u;
-            if (p.sf_layout == MXFP8_SF_SWIZZLED) {
-                const int64_t padded_cols = ((p.cols + 127) >> 7) << 7;
-                if (c < padded_cols) {
-                    *reinterpret_cast<uint32_t*>(p.s_col + ((c >> 7) * ((nrb + 3) >> 2) + tile_y) * 512 + (c & 31) * 16 + ((c >> 5) & 3) * 4) = v;
-                    // pad columns no tile covers (FP32 tiles are 64 wide, atoms 128 wide)
-                    if (T_COLS == 64 && tile_x == p.tiles_x - 1 && c + 64 >= (int64_t)p.tiles_x * 64 && c + 64 < padded_cols)
-                        *reinterpret_cast<uint32_t*>(p.s_col + (((c + 64) >> 7) * ((nrb + 3) >> 2) + tile_y) * 512 + ((c + 64) & 31) * 16 + (((c + 64) >> 5) & 3) * 4) = 0u;
-                }
-            } else if (c < p.cols) {
-                for (int w = 0; w < nrb_here; ++w) p.s_col[(rb0 + w) * p.cols + c] = (uint8_t)(v >> (8 * w));
-            }
-        }
+        store_scales<BF, DO_ROW, DO_COL, EMU>(p, tile_x, tile_y, sm_row, sm_col, tid, lane, warp);
     }
     if (tid == 0) leave();
 }
@@ -873,8 +799,7 @@ cudaError_t launch(const QMaps& ms, const QBatch& p, cudaStream_t stream)
 {
     constexpr bool GLU = (PRO == PRO_GLU);
     constexpr int SMEM = RING * IN_BYTES + 2048 + 128;          // ring, scale staging, barriers
-    // + the up tile of the gated mode, or the row weights and flags of the gather mode
-    constexpr int SMEM_USED = GLU ? SMEM + IN_BYTES : (PRO == PRO_GATHER ? SMEM + RING * T_ROWS * 5 : SMEM);
+    constexpr int SMEM_USED = GLU ? SMEM + IN_BYTES : SMEM;  // + the up tile of the gated mode
     auto kernel = quantize_tma_kernel<DTYPE, ELEM, R, C, EMU, PRO>;
     static unsigned long long smem_set = 0;
     cudaError_t err = ensure_dynamic_smem(kernel, SMEM_USED, smem_set);
@@ -903,7 +828,6 @@ cudaError_t launch_o(int orientation, const QMaps& ms, const QBatch& p, cudaStre
 template <int ELEM>
 cudaError_t quantize_tma_launch(bool bf16_src, int orientation, bool emulate, const QMaps& ms, const QBatch& p, cudaStream_t st)
 {
-    if (p.slot_of) return cudaErrorInvalidValue;      // gathered launches have a translation unit of their own
     if (p.glu_cols || p.up_map)
         return bf16_src ? launch_o<MXFP8_BF16, ELEM, false, PRO_GLU>(orientation, ms, p, st) : launch_o<MXFP8_FP32, ELEM, false, PRO_GLU>(orientation, ms, p, st);
     if (p.rstd != nullptr || p.act != MXFP8_ACT_NONE)
