@@ -210,64 +210,108 @@ struct MoveArgs {
     int top_k, group;         // group: threads that share a token (a power of two, 32 .. 256)
 };
 
-constexpr int MOVE_THREADS = 256;
-constexpr int MOVE_UNROLL = 8;        // rows in flight per thread
+constexpr int MOVE_THREADS = 256, MOVE_WARPS = MOVE_THREADS / 32;
 
 // Row of a slot, or -1.  Anything but -1 and a row of the tensor is an error of the caller's array: reported, not used.
-__device__ __forceinline__ int64_t checked_row(int32_t r, int64_t rows, int* status)
+__device__ __forceinline__ int checked_row(int32_t r, int64_t rows, int* status)
 {
     if (r >= 0 && r < rows) return r;
     if (r != -1) atomicExch(status, (int)MXFP8_ERR_DEVICE_ARGS);
     return -1;
 }
 
+// Vectors per lane and row when there is plenty to do: a lane asks for 256 bytes of the K rows before it uses any, which
+// with 16 warps on a multiprocessor keeps more than 100 KB in flight.
+template <int DTYPE, int V, int K> constexpr int MANY = (256 / K / (V * (DTYPE == MXFP8_BF16 ? 2 : 4))) < 1 ? 1
+                                                      : (256 / K / (V * (DTYPE == MXFP8_BF16 ? 2 : 4))) > 8 ? 8 : (256 / K / (V * (DTYPE == MXFP8_BF16 ? 2 : 4)));
+template <int U> constexpr int COMBINE_CTAS = U == 1 ? 4 : 2;       // per multiprocessor
+
 // dst[t, c] = sum_j w[t, j] * src[row_of[t, j], c]: FP32 sums in the order of j, one rounding at the end.
-template <int SRC, int DST, int V>
-__global__ void __launch_bounds__(MOVE_THREADS) moe_combine_kernel(const MoveArgs a)
+// A warp takes one token's run of 32 * V * U columns at a time; lane j fetches the j-th row number and weight of its next
+// item while the current one is summed, so that the two dependent loads of a gather are paid once per warp, not per item.
+template <int SRC, int DST, int V, int K, int U>
+__global__ void __launch_bounds__(MOVE_THREADS, COMBINE_CTAS<U>) moe_combine_kernel(const MoveArgs a)
 {
-    const int per_block = MOVE_THREADS / a.group;
-    const int64_t t = (int64_t)blockIdx.x * per_block + threadIdx.x / a.group;
-    const int64_t c = ((int64_t)blockIdx.y * a.group + threadIdx.x % a.group) * V;
-    if (t >= a.tokens || c >= a.cols) return;
-    float acc[V];
+    constexpr int RUN = 32 * V * U;
+    const int lane = threadIdx.x & 31;
+    const uint32_t runs = (uint32_t)((a.cols + RUN - 1) / RUN), items = (uint32_t)a.tokens * runs, step = gridDim.x * MOVE_WARPS;
+    const bool one_round = a.top_k <= K;
+    auto lookup = [&](uint32_t t, int j, int& row, float& w) {
+        row = -1;
+        w = 0.f;
+        if (j < a.top_k) {
+            const int64_t slot = (int64_t)t * a.top_k + j;
+            row = checked_row(a.row_of[slot], a.rows, a.status);
+            w = a.weights ? a.weights[slot] : 1.f;
+        }
+    };
+    uint32_t item = blockIdx.x * MOVE_WARPS + (threadIdx.x >> 5);
+    if (item >= items) return;
+    uint32_t t = item / runs, run = item - t * runs;                           // token and run of the item, carried on by additions
+    const uint32_t t_step = step / runs, run_step = step - t_step * runs;
+    int my_row = -1, next_row = -1;
+    float my_w = 0.f, next_w = 0.f;
+    if (lane < K) lookup(t, lane, my_row, my_w);
+    for (; item < items; item += step) {
+        const int64_t c0 = (int64_t)run * RUN + lane * V;
+        uint32_t next_t = t + t_step, next_run = run + run_step;
+        if (next_run >= runs) { next_run -= runs; ++next_t; }
+        if (one_round && item + step < items && lane < K) lookup(next_t, lane, next_row, next_w);
+        float acc[U][V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] = 0.f;
-    for (int j0 = 0; j0 < a.top_k; j0 += MOVE_UNROLL) {
-        Vec<SRC, V> x[MOVE_UNROLL];
-        float w[MOVE_UNROLL];
-        bool live[MOVE_UNROLL];
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int j = 0; j < MOVE_UNROLL; ++j) {
-            live[j] = false;
-            if (j0 + j < a.top_k) {
-                const int64_t slot = t * a.top_k + j0 + j;
-                const int64_t r = checked_row(a.row_of[slot], a.rows, a.status);
+            for (int i = 0; i < V; ++i) acc[u][i] = 0.f;
+        for (int j0 = 0; j0 < a.top_k; j0 += K) {
+            if (!one_round) {
+                my_row = -1;
+                if (lane < K) lookup(t, j0 + lane, my_row, my_w);
+            }
+            Vec<SRC, V> x[K][U];
+            bool live[K];
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const int r = __shfl_sync(0xFFFFFFFFu, my_row, j);
                 live[j] = r >= 0;
-                if (live[j]) {
-                    w[j] = a.weights ? a.weights[slot] : 1.f;
-                    x[j].load(a.src, r * a.cols + c);
-                }
+                if (live[j])
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (c0 + u * 32 * V < a.cols) x[j][u].load(a.src, (int64_t)r * a.cols + c0 + u * 32 * V);
+            }
+#pragma unroll
+            for (int j = 0; j < K; ++j) {
+                const float w = __shfl_sync(0xFFFFFFFFu, my_w, j);
+                if (live[j])
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) acc[u][i] = fmaf(w, x[j][u].get(i), acc[u][i]);
             }
         }
 #pragma unroll
-        for (int j = 0; j < MOVE_UNROLL; ++j)
-            if (live[j])
+        for (int u = 0; u < U; ++u)
+            if (c0 + u * 32 * V < a.cols) {
+                Vec<DST, V> y;
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] = fmaf(w[j], x[j].get(i), acc[i]);
+                for (int i = 0; i < V; ++i) y.set(i, acc[u][i]);
+                y.store(a.dst, (int64_t)t * a.cols + c0 + u * 32 * V);
+            }
+        my_row = next_row;
+        my_w = next_w;
+        t = next_t;
+        run = next_run;
     }
-    Vec<DST, V> y;
-#pragma unroll
-    for (int i = 0; i < V; ++i) y.set(i, acc[i]);
-    y.store(a.dst, t * a.cols + c);
 }
 
 // d_src[row_of[t, j], c] = w[t, j] * dy[t, c] (one FP32 product, rounded to src's type) and
 // d_weights[t, j] = sum_c dy[t, c] * src[row_of[t, j], c] (FP32: lane-strided partial sums, then a fixed tree), so dy is
-// read once per token.  CTAs behind the tokens' clear the padding rows of the segments.
-template <int DY, int SRC, int V>
+// read once per token and K choices.  `group` threads share a token: one warp while tokens fill the machine, which
+// leaves the sums to shuffles; up to a whole CTA for few tokens.  CTAs behind the tokens' clear the padding rows.
+template <int DY, int SRC, int V, int K>
 __global__ void __launch_bounds__(MOVE_THREADS) moe_combine_grad_kernel(const MoveArgs a)
 {
-    __shared__ float sums[MOVE_THREADS / 32][MOVE_UNROLL];
+    constexpr int U = MANY<SRC, V, K> < 2 ? 1 : 2;
+    __shared__ float sums[MOVE_WARPS][K];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if ((int64_t)blockIdx.x >= a.token_blocks) {
         const int used = *a.used;
@@ -286,67 +330,85 @@ __global__ void __launch_bounds__(MOVE_THREADS) moe_combine_grad_kernel(const Mo
     }
     const int per_block = MOVE_THREADS / a.group, member = tid % a.group;
     const int64_t t = (int64_t)blockIdx.x * per_block + tid / a.group;
-    for (int j0 = 0; j0 < a.top_k; j0 += MOVE_UNROLL) {
-        int64_t row[MOVE_UNROLL];
-        float w[MOVE_UNROLL], acc[MOVE_UNROLL];
+    const int64_t stride = (int64_t)a.group * V;
+    for (int j0 = 0; j0 < a.top_k; j0 += K) {
+        int my_row = -1;
+        float my_w = 0.f;
+        if (t < a.tokens && lane < K && j0 + lane < a.top_k) {
+            const int64_t slot = t * a.top_k + j0 + lane;
+            my_row = checked_row(a.row_of[slot], a.rows, a.status);
+            my_w = a.weights ? a.weights[slot] : 1.f;
+        }
+        int row[K];
+        float w[K], acc[K];
 #pragma unroll
-        for (int j = 0; j < MOVE_UNROLL; ++j) {
+        for (int j = 0; j < K; ++j) {
+            row[j] = __shfl_sync(0xFFFFFFFFu, my_row, j);
+            w[j] = __shfl_sync(0xFFFFFFFFu, my_w, j);
             acc[j] = 0.f;
-            row[j] = -1;
-            w[j] = 0.f;
-            if (t < a.tokens && j0 + j < a.top_k) {
-                const int64_t slot = t * a.top_k + j0 + j;
-                row[j] = checked_row(a.row_of[slot], a.rows, a.status);
-                w[j] = a.weights ? a.weights[slot] : 1.f;
-            }
         }
         if (t < a.tokens)
-            for (int64_t c = (int64_t)member * V; c < a.cols; c += (int64_t)a.group * V) {
-                Vec<DY, V> g;
-                g.load(a.dy, t * a.cols + c);
-                Vec<SRC, V> x[MOVE_UNROLL];
+            for (int64_t c0 = (int64_t)member * V; c0 < a.cols; c0 += U * stride) {
+                Vec<DY, V> g[U];
+                Vec<SRC, V> x[K][U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (c0 + u * stride < a.cols) g[u].load(a.dy, t * a.cols + c0 + u * stride);
                 if (a.d_weights != nullptr)
 #pragma unroll
-                    for (int j = 0; j < MOVE_UNROLL; ++j)
-                        if (row[j] >= 0) x[j].load(a.src, row[j] * a.cols + c);
+                    for (int j = 0; j < K; ++j)
+                        if (row[j] >= 0)
 #pragma unroll
-                for (int j = 0; j < MOVE_UNROLL; ++j) {
+                            for (int u = 0; u < U; ++u)
+                                if (c0 + u * stride < a.cols) x[j][u].load(a.src, (int64_t)row[j] * a.cols + c0 + u * stride);
+#pragma unroll
+                for (int j = 0; j < K; ++j) {
                     if (row[j] < 0) continue;
-                    if (a.d_weights != nullptr)
 #pragma unroll
-                        for (int i = 0; i < V; ++i) acc[j] = fmaf(g.get(i), x[j].get(i), acc[j]);
-                    if (a.dst != nullptr) {
-                        Vec<SRC, V> d;
+                    for (int u = 0; u < U; ++u) {
+                        if (c0 + u * stride >= a.cols) continue;
+                        if (a.d_weights != nullptr)
 #pragma unroll
-                        for (int i = 0; i < V; ++i) d.set(i, w[j] * g.get(i));
-                        d.store(a.dst, row[j] * a.cols + c);
+                            for (int i = 0; i < V; ++i) acc[j] = fmaf(g[u].get(i), x[j][u].get(i), acc[j]);
+                        if (a.dst != nullptr) {
+                            Vec<SRC, V> d;
+#pragma unroll
+                            for (int i = 0; i < V; ++i) d.set(i, w[j] * g[u].get(i));
+                            d.store(a.dst, (int64_t)row[j] * a.cols + c0 + u * stride);
+                        }
                     }
                 }
             }
         if (a.d_weights == nullptr) continue;
+        float mine = 0.f;                                  // lane j ends with the sum of choice j
 #pragma unroll
-        for (int j = 0; j < MOVE_UNROLL; ++j)
+        for (int j = 0; j < K; ++j) {
+            float v = acc[j];
 #pragma unroll
-            for (int off = 16; off > 0; off >>= 1) acc[j] += __shfl_xor_sync(0xFFFFFFFFu, acc[j], off);
-        if (lane == 0)
-#pragma unroll
-            for (int j = 0; j < MOVE_UNROLL; ++j) sums[warp][j] = acc[j];
+            for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
+            if (lane == j) mine = v;
+        }
+        if (a.group == 32) {
+            if (t < a.tokens && lane < K && j0 + lane < a.top_k) a.d_weights[t * a.top_k + j0 + lane] = mine;
+            continue;
+        }
+        if (lane < K) sums[warp][lane] = mine;
         __syncthreads();
-        if (member < MOVE_UNROLL && t < a.tokens && j0 + member < a.top_k) {
+        if (member < K && t < a.tokens && j0 + member < a.top_k) {
             const int w0 = (tid / a.group) * (a.group / 32);
-            float s = 0.f;
-            for (int k = 0; k < a.group / 32; ++k) s += sums[w0 + k][member];
-            a.d_weights[t * a.top_k + j0 + member] = s;
+            float v = 0.f;
+            for (int k = 0; k < a.group / 32; ++k) v += sums[w0 + k][member];
+            a.d_weights[t * a.top_k + j0 + member] = v;
         }
         __syncthreads();
     }
 }
 
-// Largest vector (8, 4, 2 or 1 elements) that every row of every tensor starts on: it has to divide cols, and each base
-// has to lie on a boundary of its pieces.
-int vector_width(int64_t cols, const void* const* ptrs, const int* esz, int count)
+// Largest vector (8, 4, 2 or 1 elements, at most `most`) that every row of every tensor starts on: it has to divide cols,
+// and each base has to lie on a boundary of its pieces.
+int vector_width(int64_t cols, const void* const* ptrs, const int* esz, int count, int most)
 {
-    for (int v = 8; v > 1; v >>= 1) {
+    for (int v = most; v > 1; v >>= 1) {
         bool ok = cols % v == 0;
         for (int i = 0; ok && i < count; ++i) {
             const int bytes = v * esz[i] < 16 ? v * esz[i] : 16;
@@ -357,10 +419,19 @@ int vector_width(int64_t cols, const void* const* ptrs, const int* esz, int coun
     return 1;
 }
 
-int group_threads(int64_t vectors)
+int sm_count()
+{
+    static PerDeviceCache<int> cache;
+    int n = 0;
+    return cache.get(n, [](int dev, int& v) { return cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && v > 0; }) ? n : 0;
+}
+
+// Threads that share a token in the gradient: as few as keep 24 warps on every multiprocessor, at most what a row has
+// vectors for.
+int group_threads(int64_t tokens, int64_t vectors, int sms)
 {
     int g = 32;
-    while (g < MOVE_THREADS && g < vectors) g <<= 1;
+    while (g < MOVE_THREADS && g < vectors && tokens * (g / 32) < 24 * sms) g <<= 1;
     return g;
 }
 
@@ -416,25 +487,52 @@ extern "C" int mxfp8_moe_sort(const int32_t* expert_ids, int64_t tokens, int top
 }
 
 namespace {
-template <int A, int B>
-cudaError_t launch_combine(int v, dim3 grid, const MoveArgs& m, cudaStream_t st)
+// Two or eight rows in flight per lane; several vectors of each where the rows are long enough and the items fill the machine
+template <int A, int B, int V, int K>
+cudaError_t launch_combine_k(const MoveArgs& m, int sms, cudaStream_t st)
 {
-    if (v == 8) moe_combine_kernel<A, B, 8><<<grid, MOVE_THREADS, 0, st>>>(m);
-    else if (v == 4) moe_combine_kernel<A, B, 4><<<grid, MOVE_THREADS, 0, st>>>(m);
-    else if (v == 2) moe_combine_kernel<A, B, 2><<<grid, MOVE_THREADS, 0, st>>>(m);
-    else moe_combine_kernel<A, B, 1><<<grid, MOVE_THREADS, 0, st>>>(m);
+    auto go = [&](auto kernel, int run, int ctas) {
+        const int64_t items = m.tokens * ((m.cols + run - 1) / run), blocks = (items + MOVE_WARPS - 1) / MOVE_WARPS;
+        kernel<<<(unsigned)(blocks < (int64_t)ctas * sms ? blocks : (int64_t)ctas * sms), MOVE_THREADS, 0, st>>>(m);
+    };
+    constexpr int U = MANY<A, V, K>, RUN = 32 * V * U;
+    if (U > 1 && m.cols >= RUN && m.tokens * (m.cols / RUN) >= (int64_t)2 * MOVE_WARPS * COMBINE_CTAS<U> * sms)
+        go(moe_combine_kernel<A, B, V, K, U>, RUN, COMBINE_CTAS<U>);
+    else go(moe_combine_kernel<A, B, V, K, 1>, 32 * V, COMBINE_CTAS<1>);
+    count_launch(1);
+    return cudaGetLastError();
+}
+template <int A, int B, int V>
+cudaError_t launch_combine_v(const MoveArgs& m, int sms, cudaStream_t st)
+{
+    return m.top_k <= 2 ? launch_combine_k<A, B, V, 2>(m, sms, st) : launch_combine_k<A, B, V, 8>(m, sms, st);
+}
+template <int A, int B>
+cudaError_t launch_combine(int v, const MoveArgs& m, int sms, cudaStream_t st)
+{
+    if constexpr (A == MXFP8_BF16)
+        if (v == 8) return launch_combine_v<A, B, 8>(m, sms, st);
+    if (v >= 4) return launch_combine_v<A, B, 4>(m, sms, st);
+    if (v == 2) return launch_combine_v<A, B, 2>(m, sms, st);
+    return launch_combine_v<A, B, 1>(m, sms, st);
+}
+template <int A, int B, int V>
+cudaError_t launch_grad_v(unsigned grid, const MoveArgs& m, cudaStream_t st)
+{
+    if (m.top_k <= 2) moe_combine_grad_kernel<A, B, V, 2><<<grid, MOVE_THREADS, 0, st>>>(m);
+    else if (m.top_k <= 4) moe_combine_grad_kernel<A, B, V, 4><<<grid, MOVE_THREADS, 0, st>>>(m);
+    else moe_combine_grad_kernel<A, B, V, 8><<<grid, MOVE_THREADS, 0, st>>>(m);
     count_launch(1);
     return cudaGetLastError();
 }
 template <int A, int B>
 cudaError_t launch_grad(int v, unsigned grid, const MoveArgs& m, cudaStream_t st)
 {
-    if (v == 8) moe_combine_grad_kernel<A, B, 8><<<grid, MOVE_THREADS, 0, st>>>(m);
-    else if (v == 4) moe_combine_grad_kernel<A, B, 4><<<grid, MOVE_THREADS, 0, st>>>(m);
-    else if (v == 2) moe_combine_grad_kernel<A, B, 2><<<grid, MOVE_THREADS, 0, st>>>(m);
-    else moe_combine_grad_kernel<A, B, 1><<<grid, MOVE_THREADS, 0, st>>>(m);
-    count_launch(1);
-    return cudaGetLastError();
+    if constexpr (B == MXFP8_BF16)
+        if (v == 8) return launch_grad_v<A, B, 8>(grid, m, st);
+    if (v >= 4) return launch_grad_v<A, B, 4>(grid, m, st);
+    if (v == 2) return launch_grad_v<A, B, 2>(grid, m, st);
+    return launch_grad_v<A, B, 1>(grid, m, st);
 }
 bool misaligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) % bytes) != 0; }
 bool bad_dtype(int d) { return d != MXFP8_FP32 && d != MXFP8_BF16; }
@@ -447,6 +545,7 @@ extern "C" int mxfp8_moe_combine(const void* src, int src_dtype, int64_t rows, i
     if (bad_dtype(src_dtype) || bad_dtype(dst_dtype)) return MXFP8_ERR_ENUM;
     if (rows < 0 || cols <= 0 || tokens < 0 || top_k < 1) return MXFP8_ERR_SHAPE;
     if (tokens == 0) return MXFP8_OK;
+    if (rows > 0x7FFFFFFFLL || cols > 0x7FFFFFFFLL || tokens > 0x7FFFFFFFLL) return MXFP8_ERR_UNSUPPORTED;
     if ((rows > 0 && !src) || !row_of || !dst) return MXFP8_ERR_NULL;
     if (misaligned(src, esize(src_dtype)) || misaligned(dst, esize(dst_dtype)) || misaligned(row_of, 4) || misaligned(weights, 4)) return MXFP8_ERR_ALIGN;
     MoveArgs m{};
@@ -454,16 +553,14 @@ extern "C" int mxfp8_moe_combine(const void* src, int src_dtype, int64_t rows, i
     m.rows = rows; m.cols = cols; m.tokens = tokens; m.top_k = top_k;
     const void* ptrs[2] = {src, dst};
     const int esz[2] = {esize(src_dtype), esize(dst_dtype)};
-    const int v = vector_width(cols, ptrs, esz, 2);
-    m.group = group_threads(cols / v);
-    const int64_t gx = (tokens + MOVE_THREADS / m.group - 1) / (MOVE_THREADS / m.group), gy = (cols / v + m.group - 1) / m.group;
-    if (gx > 0x7FFFFFFFLL || gy > 65535 || tokens > 0x7FFFFFFFFFFFLL / top_k) return MXFP8_ERR_UNSUPPORTED;
-    if (!(m.status = device_status_word())) return MXFP8_ERR_CUDA;
-    const dim3 grid((unsigned)gx, (unsigned)gy);
+    const int v = vector_width(cols, ptrs, esz, 2, 16 / esize(src_dtype));
+    if (tokens * ((cols + 32 * v - 1) / (32 * v)) >= 0x7FFF0000LL) return MXFP8_ERR_UNSUPPORTED;      // items are counted in 32 bits
+    const int sms = sm_count();
+    if (sms <= 0 || !(m.status = device_status_word())) return MXFP8_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t err;
-    if (src_dtype == MXFP8_BF16) err = dst_dtype == MXFP8_BF16 ? launch_combine<MXFP8_BF16, MXFP8_BF16>(v, grid, m, st) : launch_combine<MXFP8_BF16, MXFP8_FP32>(v, grid, m, st);
-    else err = dst_dtype == MXFP8_BF16 ? launch_combine<MXFP8_FP32, MXFP8_BF16>(v, grid, m, st) : launch_combine<MXFP8_FP32, MXFP8_FP32>(v, grid, m, st);
+    if (src_dtype == MXFP8_BF16) err = dst_dtype == MXFP8_BF16 ? launch_combine<MXFP8_BF16, MXFP8_BF16>(v, m, sms, st) : launch_combine<MXFP8_BF16, MXFP8_FP32>(v, m, sms, st);
+    else err = dst_dtype == MXFP8_BF16 ? launch_combine<MXFP8_FP32, MXFP8_BF16>(v, m, sms, st) : launch_combine<MXFP8_FP32, MXFP8_FP32>(v, m, sms, st);
     return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
 }
 
@@ -474,6 +571,7 @@ extern "C" int mxfp8_moe_combine_grad(const void* dy, int dy_dtype, int64_t toke
     if (bad_dtype(dy_dtype) || bad_dtype(src_dtype)) return MXFP8_ERR_ENUM;
     if (rows < 0 || cols <= 0 || tokens < 0 || top_k < 1 || num_groups < 1) return MXFP8_ERR_SHAPE;
     if (tokens == 0) return MXFP8_OK;
+    if (rows > 0x7FFFFFFFLL || cols > 0x7FFFFFFFLL || tokens > 0x7FFFFFFFLL) return MXFP8_ERR_UNSUPPORTED;
     if (!dy || !row_of || (!d_src && !d_weights)) return MXFP8_ERR_NULL;
     if ((d_weights && rows > 0 && !src) || (d_src && rows > 0 && (!slot_of || !group_offsets))) return MXFP8_ERR_NULL;
     if (misaligned(dy, esize(dy_dtype)) || misaligned(src, esize(src_dtype)) || misaligned(d_src, esize(src_dtype)) || misaligned(row_of, 4) ||
@@ -485,11 +583,13 @@ extern "C" int mxfp8_moe_combine_grad(const void* dy, int dy_dtype, int64_t toke
     m.used = group_offsets ? group_offsets + num_groups : nullptr;
     const void* ptrs[3] = {dy, src, d_src};
     const int esz[3] = {esize(dy_dtype), esize(src_dtype), esize(src_dtype)};
-    const int v = vector_width(cols, ptrs, esz, 3);
-    m.group = group_threads(cols / v);
+    const int v = vector_width(cols, ptrs, esz, 3, 16 / esize(src_dtype));
+    const int sms = sm_count();
+    if (sms <= 0) return MXFP8_ERR_CUDA;
+    m.group = group_threads(tokens, cols / v, sms);
     m.token_blocks = (tokens + MOVE_THREADS / m.group - 1) / (MOVE_THREADS / m.group);
     const int64_t blocks = m.token_blocks + (d_src ? (rows + 31) / 32 : 0);
-    if (blocks > 0x7FFFFFFFLL || tokens > 0x7FFFFFFFFFFFLL / top_k) return MXFP8_ERR_UNSUPPORTED;
+    if (blocks > 0x7FFFFFFFLL) return MXFP8_ERR_UNSUPPORTED;
     if (!(m.status = device_status_word())) return MXFP8_ERR_CUDA;
     const unsigned grid = (unsigned)blocks;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
