@@ -4,7 +4,7 @@
 //   loads  : a warp fetches its own slab with 16-byte asynchronous copies, two rows per instruction, straight from the
 //            tokens' rows (a gathering tensor copy was tried first: its issue runs through the lanes one by one, some 2000
 //            cycles of one warp per tile with the other three waiting: 88 us for the row-blocked copy of 53248 x 2048
-//            rows against %s us).  Rows without a slot and columns behind the tensor are zero-filled by the copies.
+//            rows against 55 us).  Rows without a slot and columns behind the tensor are zero-filled by the copies.
 //   weights: one FP32 product and one rounding per element, in place in the slab, before the conversion
 //   order  : slots of the tile after next are asked for under the current slab, its copies go out as soon as the slab
 //            is done; the CTA meets once per tile, for the scale bytes
