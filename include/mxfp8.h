@@ -401,7 +401,7 @@ int mxfp8_grouped_gemm(const void* Aq, const void* As, const void* Bq, const voi
  * mxfp8_moe_combine_grad -- the gradients of that sum, dy read once:
  *     d_src[row_of[t, j], :] = weights[t, j] * dy[t, :]                one FP32 product, rounded to src's type; 0 in padding rows
  *     d_weights[t, j]        = sum over c of dy[t, c] * src[row_of[t, j], c]    FP32 in a fixed order; 0 without a row
- *   d_src (with slot_of, group_offsets) or d_weights (with src) may be NULL.  weights NULL: all ones.
+ *   d_src (with slot_of, group_offsets) or d_weights (with src) may be NULL; d_src may be src itself.  weights NULL: all ones.
  *
  * Entries of row_of / slot_of that are neither -1 nor a row / slot of the tensors, or a group_offsets[num_groups] that is
  * no possible end, leave MXFP8_ERR_DEVICE_ARGS in the device status word; such an entry counts as -1, and with such an end
@@ -438,7 +438,8 @@ int mxfp8_moe_combine_grad(const void* dy, int dy_dtype, int64_t tokens, int64_t
  *   with the codes and scale bytes of matrix matrix_ids[s] (slot s = token * slots_per_token + choice), or of the only
  *   matrix when matrix_ids is NULL (num_matrices and slots_per_token are 1 then).  A slot whose number is outside
  *   0 .. num_matrices - 1 gets zeros.  x [tokens, cols] BF16, 16-byte aligned; y [tokens * slots_per_token, rows] FP32 or BF16.
- *   Products are exact, each group's sum is FP32, the groups are added in FP32 in a fixed order; scale byte 0xFF gives NaN.
+ *   Products are exact (below FP32's normal range they keep what FP32 keeps); 128 columns at a time are summed in the tensor
+ *   cores' FP32 accumulators, these sums in FP32 in a fixed order; scale byte 0xFF gives NaN.
  *   At most 1024 slots and 65535 matrices (ERR_UNSUPPORTED): beyond that mxfp8_gemm / mxfp8_grouped_gemm are the tools.
  */
 size_t mxfp8_e2m1_packed_bytes(int64_t num_matrices, int64_t rows, int64_t cols);

@@ -177,7 +177,7 @@ def _ptr(t):
         return None
     if not t.is_contiguous():
         raise ValueError("the C entry points take dense row-major buffers: pass a contiguous tensor")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()           # the declared argument types turn it into a pointer (0, an empty tensor's, into NULL)
 
 
 # torch.cuda.current_stream() builds a Stream object (3 us of the 10 to 12 us that a call through this module took); the
@@ -188,9 +188,8 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 def _stream(stream=None):
     if stream is None and _raw_stream is not None:
-        return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
-    s = torch.cuda.current_stream() if stream is None else stream
-    return ctypes.c_void_p(s.cuda_stream)
+        return _raw_stream(torch.cuda.current_device())
+    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -553,6 +552,8 @@ def mxfp8_e2m1_pack(q: torch.Tensor, s: torch.Tensor, num_matrices: int, packed:
     """q: [num_matrices * rows, cols] E2M1 slots and s: their linear ROW scales, as mxfp8_quantize writes them."""
     all_rows, cols = q.shape
     _on_device(stream, q, s, packed)
+    if q.element_size() != 1 or s.element_size() != 1:
+        raise TypeError("codes and scales are bytes")
     if num_matrices < 1 or all_rows % num_matrices:
         raise ValueError("q holds num_matrices matrices of the same number of rows")
     rows = all_rows // num_matrices

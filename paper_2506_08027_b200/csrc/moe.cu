@@ -498,7 +498,7 @@ extern "C" int mxfp8_moe_sort(const int32_t* expert_ids, int64_t tokens, int top
 {
     if (tokens < 0 || top_k < 1 || num_experts < 1 || rows < 0) return MXFP8_ERR_SHAPE;
     if (!group_offsets || (tokens > 0 && (!expert_ids || !row_of)) || (rows > 0 && !slot_of)) return MXFP8_ERR_NULL;
-    if (num_experts > SORT_MAX_EXPERTS || tokens > 0x7F000000LL || tokens * top_k > 0x7F000000LL || rows > 0x7FFFFFFFLL) return MXFP8_ERR_UNSUPPORTED;
+    if (num_experts > SORT_MAX_EXPERTS || tokens > 0x7F000000LL || tokens * top_k > 0x7F000000LL || rows > 0x7FF00000LL) return MXFP8_ERR_UNSUPPORTED;   // 32-bit counters
     if (rows < mxfp8_moe_rows(tokens, top_k, num_experts)) return MXFP8_ERR_SHAPE;
     for (const void* p : {(const void*)expert_ids, (const void*)group_offsets, (const void*)row_of, (const void*)slot_of, (const void*)ws})
         if (reinterpret_cast<uintptr_t>(p) & 3u) return MXFP8_ERR_ALIGN;

@@ -98,6 +98,50 @@ def test_chosen_matrices(tokens, choices, matrices, kind):
     assert not y[(ids.reshape(-1) < 0) | (ids.reshape(-1) >= matrices)].any()
 
 
+@pytest.mark.parametrize("tokens", [1, 8, 13, 33, 70])
+@pytest.mark.parametrize("rows,cols", [(19007, 288), (18944, 1152)])
+@pytest.mark.parametrize("out", ["bf16", "fp32"])
+def test_one_matrix_of_many_rows(tokens, rows, cols, out):
+    """Enough row tiles that two share a warp's activations; the last group of them ragged."""
+    packed, codes, scales = random_weights(1, rows, cols, rows)
+    x, y = run(synth.student_t((tokens, cols), tokens), packed, 1, None, rows, out)
+    want, mag = orc.matvec_f64(x, codes, scales)
+    check(y, want, mag, cols, out)
+
+
+@pytest.mark.parametrize("tokens,choices,matrices,rows,cols", [(8, 6, 64, 413, 288), (100, 4, 48, 413, 96), (8, 6, 12, 2816, 1184)])
+def test_chosen_matrices_of_many_rows(tokens, choices, matrices, rows, cols):
+    rng = np.random.default_rng(tokens)
+    ids = rng.integers(-1, matrices, (tokens, choices)).astype(np.int32)
+    packed, codes, scales = random_weights(matrices, rows, cols, 9)
+    x, y = run(synth.gaussian((tokens, cols), 2), packed, matrices, ids, rows, "fp32")
+    want, mag = orc.matvec_f64(x, codes, scales, ids)
+    check(y, want, mag, cols, "fp32")
+
+
+def test_scales_outside_the_fast_range_in_some_tiles():
+    """Tiles whose scales all lie in 2^-63 .. 1 and tiles with one byte outside take different ways to the same sums."""
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    rows, cols = 19008, 512
+    rng = np.random.default_rng(4)
+    codes = rng.integers(0, 16, (1, rows, cols)).astype(np.uint8)
+    scales = rng.integers(64, 128, (1, rows, cols // 32)).astype(np.uint8)
+    odd = rng.random(scales.shape) < 0.002
+    scales[odd] = rng.choice([0, 1, 63, 128, 129, 200, 254], odd.sum()).astype(np.uint8)
+    flat = codes.reshape(-1, cols // 16, 16)
+    slots = np.zeros_like(flat)
+    slots[:, :, :8] = flat[:, :, 0::2] | flat[:, :, 1::2] << 4
+    packed = torch.empty(B.mxfp8_e2m1_packed_bytes(1, rows, cols), dtype=torch.uint8, device="cuda")
+    B.mxfp8_e2m1_pack(dev(slots.reshape(-1, cols)), dev(scales.reshape(-1)), 1, packed)
+    x, y = run(synth.gaussian((5, cols), 3), packed, 1, None, rows, "fp32")
+    want, mag = orc.matvec_f64(x, codes, scales)
+    small = mag < 2.0 ** 127                        # nothing near the top of FP32's range
+    assert small.any()
+    err = np.abs(y - want)
+    assert (err[small] <= ((2 * 2 * 17 + cols / 32 + 16) * 2.0 ** -24 * mag[small] + 2.0 ** -24 * np.abs(want[small])) * (1 + 2.0 ** -20) + 2.0 ** -133).all()
+
+
 def test_a_large_matrix_and_long_rows():
     """14336 columns and, apart, a packed tensor of more than 2^31 bytes (the last matrix lies behind that offset)."""
     import torch

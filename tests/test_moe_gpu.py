@@ -318,6 +318,43 @@ def test_combine_gradient_against_the_oracle(cols, dy, src, top_k):
     assert torch.equal(a, d_y) and torch.equal(b, d_w)
 
 
+@pytest.mark.parametrize("src,dst", [("bf16", "bf16"), ("fp32", "bf16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("top_k,cols", [(1, 2088), (2, 1027), (6, 520), (3, 2052)])
+def test_combine_and_gradient_of_a_batch_that_fills_the_machine(src, dst, top_k, cols):
+    """Enough tokens that a lane keeps several vectors of a row in flight (sum) and a warp takes a token alone (gradient);
+    the last run of columns ragged.  Bounds as above."""
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    tokens, experts = 5003, 8
+    rng = np.random.default_rng(cols)
+    off, row_of, slot_of = gpu_sort(routing(tokens, top_k, experts, 3, "holes"), experts)
+    rows, used = slot_of.numel(), int(off[-1])
+    dt = lambda n: torch.bfloat16 if n == "bf16" else torch.float32
+    y = torch.randn(rows, cols, device="cuda").to(dt(src))
+    w = torch.randn(tokens, top_k, device="cuda")
+    out = torch.full((tokens, cols), float("nan"), dtype=dt(dst), device="cuda")
+    B.mxfp8_moe_combine(y, row_of, w, out)
+    live = (row_of >= 0).unsqueeze(2)
+    want = torch.zeros(tokens, cols, dtype=torch.float64, device="cuda")
+    mag = torch.zeros_like(want)
+    for j in range(top_k):
+        term = torch.where(live[:, j], y.double()[row_of[:, j].long().clamp(min=0)] * w[:, j:j + 1].double(), torch.zeros_like(want))
+        want += term
+        mag += term.abs()
+    sums = top_k * 2.0 ** -24 * mag * (1 + 2.0 ** -20)
+    assert ((out.double() - want).abs() <= sums + HALF[dst] * (want.abs() + sums)).all()
+    g = torch.randn(tokens, cols, device="cuda").to(dt(dst))
+    d_y, d_w = torch.full_like(y, 3.0), torch.full((tokens, top_k), float("nan"), device="cuda")
+    B.mxfp8_moe_combine_grad(g, y, row_of, slot_of, w, off, d_y, d_w)
+    assert B.mxfp8_device_status() == 0
+    slot = slot_of[:used].long().clamp(min=0)
+    d_want = torch.where((slot_of[:used] >= 0).unsqueeze(1), g.float()[slot // top_k] * w.reshape(-1)[slot].unsqueeze(1), torch.zeros((), device="cuda"))
+    assert torch.equal(d_y[:used], d_want.to(dt(src))) and (d_y[used:] == 3.0).all()
+    for j in range(top_k):
+        terms = torch.where(live[:, j], y.double()[row_of[:, j].long().clamp(min=0)] * g.double(), torch.zeros_like(want))
+        assert ((d_w[:, j].double() - terms.sum(dim=1)).abs() <= (cols + 16) * 2.0 ** -24 * terms.abs().sum(dim=1) * (1 + 2.0 ** -10)).all()
+
+
 @pytest.mark.parametrize("shift", [1, 2, 4])
 def test_combine_of_tensors_that_start_between_16_byte_boundaries(shift):
     import torch
