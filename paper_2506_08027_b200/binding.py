@@ -184,11 +184,12 @@ def _ptr(t):
 # handle alone costs a tenth of a microsecond.  Every torch that this library builds against has it; the public call
 # stands in if one day it does not.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _stream(stream=None):
     if stream is None and _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_current_device())
     return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
 
 
@@ -455,14 +456,16 @@ def mxfp8_glu_quantize(src: torch.Tensor, act: int, orientation: int, scale_rule
                                     _stream(stream)), "mxfp8_glu_quantize")
 
 
-def _on_device(stream, *tensors) -> None:
-    """Every tensor lies on the device that the call's stream belongs to (a launch elsewhere would read foreign addresses)."""
-    device = torch.cuda.current_device()
+def _stream_for(stream, *tensors) -> int:
+    """The call's stream, after a look at its tensors: all of them lie on the device that the stream belongs to and that
+    is current (a launch elsewhere would read foreign addresses)."""
+    device = _current_device()
     if stream is not None and stream.device.index != device:
         raise ValueError("the call runs on the current device, cuda:%d: its stream belongs to %s" % (device, stream.device))
     for t in tensors:
         if t is not None and t.get_device() != device:           # -1 for a host tensor
             raise ValueError("a tensor of shape %s is on %s, the call runs on cuda:%d" % (tuple(t.shape), t.device, device))
+    return _stream(stream)
 
 
 def _int32(*tensors) -> None:
@@ -484,11 +487,11 @@ def mxfp8_moe_sort(expert_ids: torch.Tensor, num_experts: int, group_offsets: to
     """expert_ids, row_of: [tokens, top_k]; group_offsets: [num_experts + 1]; slot_of: [rows], rows >= mxfp8_moe_rows(...)."""
     tokens, top_k = expert_ids.shape
     _int32(expert_ids, group_offsets, row_of, slot_of)
-    _on_device(stream, expert_ids, group_offsets, row_of, slot_of, ws)
+    st = _stream_for(stream, expert_ids, group_offsets, row_of, slot_of, ws)
     if group_offsets.numel() != num_experts + 1 or row_of.shape != expert_ids.shape:
         raise ValueError("group_offsets holds num_experts + 1 numbers, row_of has the shape of expert_ids")
     _check(lib().mxfp8_moe_sort(_ptr(expert_ids), tokens, top_k, num_experts, _ptr(group_offsets), _ptr(row_of), _ptr(slot_of), slot_of.numel(),
-                                _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)), "mxfp8_moe_sort")
+                                _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size(), st), "mxfp8_moe_sort")
 
 
 def mxfp8_moe_dispatch_quantize(src: torch.Tensor, slot_of: torch.Tensor, top_k: int, weights, group_offsets: torch.Tensor,
@@ -497,7 +500,7 @@ def mxfp8_moe_dispatch_quantize(src: torch.Tensor, slot_of: torch.Tensor, top_k:
     tokens, cols = src.shape
     rows = slot_of.numel()
     _int32(slot_of, group_offsets)
-    _on_device(stream, src, slot_of, weights, group_offsets, q_row, s_row, q_col, s_col)
+    st = _stream_for(stream, src, slot_of, weights, group_offsets, q_row, s_row, q_col, s_col)
     _float_weights(weights, tokens, top_k)
     for o, q, s in ((ROW, q_row, s_row), (COL, q_col, s_col)):
         if orientation & o and q is not None and s is not None and rows % 128 == 0:
@@ -505,7 +508,7 @@ def mxfp8_moe_dispatch_quantize(src: torch.Tensor, slot_of: torch.Tensor, top_k:
                 raise ValueError("an output is smaller than [%d, %d] needs" % (rows, cols))
     _check(lib().mxfp8_moe_dispatch_quantize(_ptr(src), _dtype_code(src), tokens, cols, _ptr(slot_of), rows, top_k, _ptr(weights),
                                              _ptr(group_offsets), group_offsets.numel() - 1, orientation, scale_rule, elem,
-                                             _ptr(q_row), _ptr(s_row), _ptr(q_col), _ptr(s_col), sf_layout, _stream(stream)),
+                                             _ptr(q_row), _ptr(s_row), _ptr(q_col), _ptr(s_col), sf_layout, st),
            "mxfp8_moe_dispatch_quantize")
 
 
@@ -519,12 +522,12 @@ def mxfp8_moe_combine(src: torch.Tensor, row_of: torch.Tensor, weights, dst: tor
     rows, cols = src.shape
     tokens, top_k = row_of.shape
     _int32(row_of)
-    _on_device(stream, src, row_of, weights, dst)
+    st = _stream_for(stream, src, row_of, weights, dst)
     _float_weights(weights, tokens, top_k)
     if dst.shape != (tokens, cols):
         raise ValueError("dst must be [tokens, cols]")
     _check(lib().mxfp8_moe_combine(_ptr(src), _dtype_code(src), rows, cols, _ptr(row_of), _ptr(weights), tokens, top_k, _ptr(dst),
-                                   _dtype_code(dst), _stream(stream)), "mxfp8_moe_combine")
+                                   _dtype_code(dst), st), "mxfp8_moe_combine")
 
 
 def mxfp8_moe_combine_grad(dy: torch.Tensor, src: torch.Tensor, row_of: torch.Tensor, slot_of: torch.Tensor, weights, group_offsets: torch.Tensor,
@@ -533,7 +536,7 @@ def mxfp8_moe_combine_grad(dy: torch.Tensor, src: torch.Tensor, row_of: torch.Te
     tokens, cols = dy.shape
     rows = src.shape[0]
     _int32(row_of, slot_of, group_offsets)
-    _on_device(stream, dy, src, row_of, slot_of, weights, group_offsets, d_src, d_weights)
+    st = _stream_for(stream, dy, src, row_of, slot_of, weights, group_offsets, d_src, d_weights)
     top_k = row_of.shape[1]
     _float_weights(weights, tokens, top_k)
     _float_weights(d_weights, tokens, top_k)
@@ -541,7 +544,7 @@ def mxfp8_moe_combine_grad(dy: torch.Tensor, src: torch.Tensor, row_of: torch.Te
         raise ValueError("shapes or types of dy, src, d_src, row_of and slot_of do not agree")
     _check(lib().mxfp8_moe_combine_grad(_ptr(dy), _dtype_code(dy), tokens, cols, _ptr(src), _dtype_code(src), rows, _ptr(row_of), _ptr(slot_of), top_k,
                                         _ptr(weights), _ptr(group_offsets), group_offsets.numel() - 1, _ptr(d_src), _ptr(d_weights),
-                                        _stream(stream)), "mxfp8_moe_combine_grad")
+                                        st), "mxfp8_moe_combine_grad")
 
 
 def mxfp8_e2m1_packed_bytes(num_matrices: int, rows: int, cols: int) -> int:
@@ -551,7 +554,7 @@ def mxfp8_e2m1_packed_bytes(num_matrices: int, rows: int, cols: int) -> int:
 def mxfp8_e2m1_pack(q: torch.Tensor, s: torch.Tensor, num_matrices: int, packed: torch.Tensor, stream=None) -> None:
     """q: [num_matrices * rows, cols] E2M1 slots and s: their linear ROW scales, as mxfp8_quantize writes them."""
     all_rows, cols = q.shape
-    _on_device(stream, q, s, packed)
+    st = _stream_for(stream, q, s, packed)
     if q.element_size() != 1 or s.element_size() != 1:
         raise TypeError("codes and scales are bytes")
     if num_matrices < 1 or all_rows % num_matrices:
@@ -559,7 +562,7 @@ def mxfp8_e2m1_pack(q: torch.Tensor, s: torch.Tensor, num_matrices: int, packed:
     rows = all_rows // num_matrices
     if s.numel() * s.element_size() < all_rows * (cols // 32) or packed.numel() * packed.element_size() < mxfp8_e2m1_packed_bytes(num_matrices, rows, cols):
         raise ValueError("s or packed is too small")
-    _check(lib().mxfp8_e2m1_pack(_ptr(q), _ptr(s), num_matrices, rows, cols, _ptr(packed), _stream(stream)), "mxfp8_e2m1_pack")
+    _check(lib().mxfp8_e2m1_pack(_ptr(q), _ptr(s), num_matrices, rows, cols, _ptr(packed), st), "mxfp8_e2m1_pack")
 
 
 def mxfp8_e2m1_matvec(x: torch.Tensor, packed: torch.Tensor, num_matrices: int, matrix_ids, y: torch.Tensor, stream=None) -> None:
@@ -568,7 +571,7 @@ def mxfp8_e2m1_matvec(x: torch.Tensor, packed: torch.Tensor, num_matrices: int, 
     if x.dtype != torch.bfloat16:
         raise TypeError("x must be bfloat16")
     _int32(matrix_ids)
-    _on_device(stream, x, packed, matrix_ids, y)
+    st = _stream_for(stream, x, packed, matrix_ids, y)
     per_token = 1 if matrix_ids is None else matrix_ids.shape[1]
     if (matrix_ids is not None and matrix_ids.shape[0] != tokens) or y.shape[0] != tokens * per_token:
         raise ValueError("y holds one row per token and choice")
@@ -576,4 +579,4 @@ def mxfp8_e2m1_matvec(x: torch.Tensor, packed: torch.Tensor, num_matrices: int, 
     if packed.numel() * packed.element_size() < mxfp8_e2m1_packed_bytes(num_matrices, rows, cols):
         raise ValueError("packed is smaller than num_matrices matrices of [%d, %d]" % (rows, cols))
     _check(lib().mxfp8_e2m1_matvec(_ptr(x), tokens, cols, _ptr(packed), num_matrices, rows, _ptr(matrix_ids), per_token, _ptr(y),
-                                   _dtype_code(y), _stream(stream)), "mxfp8_e2m1_matvec")
+                                   _dtype_code(y), st), "mxfp8_e2m1_matvec")
