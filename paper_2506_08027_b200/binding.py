@@ -502,14 +502,21 @@ def mxfp8_moe_dispatch_quantize(src: torch.Tensor, slot_of: torch.Tensor, top_k:
     _int32(slot_of, group_offsets)
     st = _stream_for(stream, src, slot_of, weights, group_offsets, q_row, s_row, q_col, s_col)
     _float_weights(weights, tokens, top_k)
-    for o, q, s in ((ROW, q_row, s_row), (COL, q_col, s_col)):
-        if orientation & o and q is not None and s is not None and rows % 128 == 0:
-            if q.numel() * q.element_size() < rows * cols or s.numel() * s.element_size() < mxfp8_scale_bytes(rows, cols, o, sf_layout):
-                raise ValueError("an output is smaller than [%d, %d] needs" % (rows, cols))
+    if orientation & ROW and q_row is not None and s_row is not None:
+        _holds(q_row, s_row, rows, cols, rows, cols // 32, sf_layout)
+    if orientation & COL and q_col is not None and s_col is not None:
+        _holds(q_col, s_col, rows, cols, cols, rows // 32, sf_layout)
     _check(lib().mxfp8_moe_dispatch_quantize(_ptr(src), _dtype_code(src), tokens, cols, _ptr(slot_of), rows, top_k, _ptr(weights),
                                              _ptr(group_offsets), group_offsets.numel() - 1, orientation, scale_rule, elem,
                                              _ptr(q_row), _ptr(s_row), _ptr(q_col), _ptr(s_col), sf_layout, st),
            "mxfp8_moe_dispatch_quantize")
+
+
+def _holds(q, s, rows: int, cols: int, mn: int, blocks: int, sf_layout: int) -> None:
+    """Codes and scales of a [rows, cols] conversion with `mn` x `blocks` scales fit their buffers."""
+    need = mn * blocks if sf_layout == SF_LINEAR else (mn + 127) // 128 * ((blocks + 3) // 4) * 512
+    if q.nbytes < rows * cols or s.nbytes < need:
+        raise ValueError("an output is smaller than [%d, %d] needs" % (rows, cols))
 
 
 def _float_weights(weights, tokens: int, top_k: int) -> None:
