@@ -25,7 +25,6 @@ namespace mxfp8 {
 namespace {
 
 constexpr int TILE_ROWS = 16, TILE_COLS = 128, TILE_CODES = 1024, TILE_BYTES = 1088;
-constexpr int MV_WARPS = 8, MV_THREADS = 32 * MV_WARPS;
 constexpr int MV_MAX_SLOTS = 1024;              // (token, choice) pairs of one call
 
 struct MatvecArgs {
@@ -36,7 +35,8 @@ struct MatvecArgs {
     int slots, per_token, matrices, by_matrix;
     int64_t rows, cols;
     int row_tiles, col_tiles;
-    int split;                   // warps that share a row group and split its columns (1, 2, 4 or 8)
+    int split_log;               // 2^split_log warps share a row group and split its columns (1, 2, 4 or 8)
+    uint32_t per_token_magic;
 };
 
 // Code pairs p = 0 .. 3 of a word as BF16 pairs (column 2p in the low half), times `scale` (both halves: 2^126 X).
@@ -178,23 +178,25 @@ template <int R, int NT> constexpr int WARP_SUMS = R * TILE_ROWS * (8 * NT + 1);
 // where registers leave few of them (AHEAD), the next tile's loads run under this tile's products.
 // u counts slots (the first slot with a matrix works for all of them, the others leave) or, where there are fewer
 // matrices than slots, matrices.
-template <typename OUT, int R, int NT, int PER_SM, bool AHEAD>
-__global__ void __launch_bounds__(MV_THREADS, PER_SM) matvec_kernel(const MatvecArgs a)
+template <typename OUT, int R, int NT, int WARPS, int PER_SM, bool AHEAD>
+__global__ void __launch_bounds__(32 * WARPS, PER_SM) matvec_kernel(const MatvecArgs a)
 {
+    constexpr int THREADS = 32 * WARPS;
     extern __shared__ float sums[];
     __shared__ int list[MV_MAX_SLOTS];
     __shared__ int listed;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, u = blockIdx.y;
-    const int groups = MV_WARPS / a.split;                                 // row groups of this CTA
-    const int64_t row0 = (int64_t)blockIdx.x * groups * R * TILE_ROWS;     // its first row
-    const int cta_rows = groups * R * TILE_ROWS;
+    const int split = 1 << a.split_log, groups = WARPS >> a.split_log;  // row groups of this CTA
+    static_assert((R & (R - 1)) == 0 && (WARPS & (WARPS - 1)) == 0, "rows of a CTA are a power of two");
+    const int cta_rows = groups * R * TILE_ROWS, cta_rows_log = 31 - __clz(cta_rows);
+    const int64_t row0 = (int64_t)blockIdx.x * cta_rows;                   // its first row
     OUT* y = static_cast<OUT*>(a.y);
     int matrix = 0, count = a.slots;
     if (a.ids != nullptr) {
         matrix = a.by_matrix ? u : a.ids[u];
         if ((unsigned)matrix >= (unsigned)a.matrices) {
             // no such matrix: this slot's rows are zero
-            for (int n = tid; n < cta_rows; n += MV_THREADS)
+            for (int n = tid; n < cta_rows; n += THREADS)
                 if (row0 + n < a.rows) y[(int64_t)u * a.rows + row0 + n] = to_out<OUT>(0.f);
             return;
         }
@@ -210,7 +212,7 @@ __global__ void __launch_bounds__(MV_THREADS, PER_SM) matvec_kernel(const Matvec
             if (lane == 0) listed = (a.by_matrix || first == u) ? found : 0;
         }
         if (a.by_matrix && u == 0)                      // slots without a matrix: theirs are zero
-            for (int s = warp; s < a.slots; s += MV_WARPS)
+            for (int s = warp; s < a.slots; s += WARPS)
                 if ((unsigned)a.ids[s] >= (unsigned)a.matrices)
                     for (int n = lane; n < cta_rows; n += 32)
                         if (row0 + n < a.rows) y[(int64_t)s * a.rows + row0 + n] = to_out<OUT>(0.f);
@@ -219,7 +221,7 @@ __global__ void __launch_bounds__(MV_THREADS, PER_SM) matvec_kernel(const Matvec
     }
     auto slot = [&](int i) { return a.ids ? list[i] : i; };
     const int token = lane >> 2, quarter = lane & 3;    // as columns of the tensor instructions' second operand
-    const int group = warp / a.split, part = warp % a.split;
+    const int group = warp >> a.split_log, part = warp & (split - 1);
     const int rt0 = (blockIdx.x * groups + group) * R;  // this warp's first row tile
     const uint8_t* tile[R];
 #pragma unroll
@@ -233,7 +235,9 @@ __global__ void __launch_bounds__(MV_THREADS, PER_SM) matvec_kernel(const Matvec
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             has[t] = 8 * t + token < tokens;
-            x[t] = a.x + (has[t] ? (int64_t)(slot(s0 + 8 * t + token) / a.per_token) * a.cols : 0) + quarter * 8;
+            int row = 0, choice = 0;
+            if (has[t]) divmod((uint32_t)slot(s0 + 8 * t + token), (uint32_t)a.per_token, a.per_token_magic, row, choice);
+            x[t] = a.x + (int64_t)row * a.cols + quarter * 8;
         }
         float acc[R][NT][4];
         Operands<R, NT> now;
@@ -249,7 +253,7 @@ __global__ void __launch_bounds__(MV_THREADS, PER_SM) matvec_kernel(const Matvec
                 for (int i = 0; i < 4; ++i) acc[r][t][i] = 0.f;
         int kt = part;
         if constexpr (!AHEAD) {
-            for (; kt < whole; kt += a.split) {
+            for (; kt < whole; kt += split) {
                 now.load(tile, (int64_t)kt * TILE_BYTES, x, has, (int64_t)kt * TILE_COLS, lane);
                 product<R, NT>(now, acc);
             }
@@ -257,16 +261,16 @@ __global__ void __launch_bounds__(MV_THREADS, PER_SM) matvec_kernel(const Matvec
             Operands<R, NT> next = now;
             if (kt < whole) now.load(tile, (int64_t)kt * TILE_BYTES, x, has, (int64_t)kt * TILE_COLS, lane);
             while (kt < whole) {
-                kt += a.split;
+                kt += split;
                 if (kt < whole) next.load(tile, (int64_t)kt * TILE_BYTES, x, has, (int64_t)kt * TILE_COLS, lane);
                 product<R, NT>(now, acc);
                 if (kt >= whole) break;
-                kt += a.split;
+                kt += split;
                 if (kt < whole) now.load(tile, (int64_t)kt * TILE_BYTES, x, has, (int64_t)kt * TILE_COLS, lane);
                 product<R, NT>(next, acc);
             }
         }
-        if (whole < a.col_tiles && whole % a.split == part) {      // the columns end inside the last tile
+        if (whole < a.col_tiles && (whole & (split - 1)) == part) {      // the columns end inside the last tile
             bool none[NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) none[t] = false;
@@ -293,47 +297,52 @@ __global__ void __launch_bounds__(MV_THREADS, PER_SM) matvec_kernel(const Matvec
                 to[8 * P + 1] = acc[r][t][3];
             }
         __syncthreads();
-        for (int i = tid; i < cta_rows * tokens; i += MV_THREADS) {
-            const int n = i % cta_rows, j = i / cta_rows;
+        for (int i = tid; i < cta_rows * tokens; i += THREADS) {
+            const int n = i & (cta_rows - 1), j = i >> cta_rows_log;
             const int g = n / (R * TILE_ROWS), m = n % (R * TILE_ROWS);
+            const float* from = sums + (g << a.split_log) * WARP_SUMS<R, NT> + m * P + j;
             float v = 0.f;
-            for (int w = 0; w < a.split; ++w) v += sums[(g * a.split + w) * WARP_SUMS<R, NT> + m * P + j];
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w)
+                if (w < split) v += from[w * WARP_SUMS<R, NT>];
             if (row0 + n < a.rows) y[(int64_t)slot(s0 + j) * a.rows + row0 + n] = to_out<OUT>(v);
         }
         __syncthreads();
     }
 }
 
-template <typename OUT, int R, int NT, int PER_SM, bool AHEAD>
+template <typename OUT, int R, int NT, int WARPS, int PER_SM, bool AHEAD>
 cudaError_t launch_matvec(MatvecArgs a, unsigned grid_y, cudaStream_t st)
 {
-    auto kernel = matvec_kernel<OUT, R, NT, PER_SM, AHEAD>;
-    constexpr int SUMS = MV_WARPS * WARP_SUMS<R, NT> * (int)sizeof(float);
+    auto kernel = matvec_kernel<OUT, R, NT, WARPS, PER_SM, AHEAD>;
+    constexpr int SUMS = WARPS * WARP_SUMS<R, NT> * (int)sizeof(float);
     static unsigned long long set = 0;
     cudaError_t err = ensure_dynamic_smem(kernel, SUMS, set);
     if (err != cudaSuccess) return err;
-    a.split = 1;
-    while (a.split < MV_WARPS && a.split < a.col_tiles) a.split <<= 1;
-    auto ctas = [&](int split) { return (int64_t)((a.row_tiles + MV_WARPS / split * R - 1) / (MV_WARPS / split * R)); };
+    a.split_log = 0;
+    while ((1 << a.split_log) < WARPS && (1 << a.split_log) < a.col_tiles) ++a.split_log;
+    a.per_token_magic = div_magic((uint32_t)a.per_token);
+    auto ctas = [&](int log) { return (int64_t)((a.row_tiles + (WARPS >> log) * R - 1) / ((WARPS >> log) * R)); };
     // Longer runs per warp wherever at least two full waves of CTAs remain: 2816 x 2048 matrices of six experts for eight
-    // tokens take 34 us with two warps to a row group and 43 us with eight; one 28672 x 4096 matrix, whose waves would
+    // tokens took 34 us with two warps to a row group and 43 us with eight; one 28672 x 4096 matrix, whose waves would
     // run out, 25 us with two and 22 us with eight.
-    while (a.split > 1 && ctas(a.split >> 1) * grid_y >= 2 * PER_SM * 148) a.split >>= 1;
-    kernel<<<dim3((unsigned)ctas(a.split), grid_y), MV_THREADS, SUMS, st>>>(a);
+    while (a.split_log > 0 && ctas(a.split_log - 1) * grid_y >= 2 * PER_SM * 148) --a.split_log;
+    kernel<<<dim3((unsigned)ctas(a.split_log), grid_y), 32 * WARPS, SUMS, st>>>(a);
     count_launch(1);
     return cudaGetLastError();
 }
 
-// Tokens worked on together: 8, 16 or 32 (a matrix's slots are seldom more than a few when they choose).  Two row tiles to a
-// group halve the reads of the activations; one keeps more multiprocessors busy while there are few row tiles (6144 x
-// 4096 for one token: 6.2 us with one, 6.9 us with two; 28672 x 4096 for 16 tokens: 33 us with one, 31 us with two).
+// Tokens worked on together: 8, 16 or 32 (a matrix's slots are seldom more than a few when they choose).  Many row tiles: two
+// to a warp, which halves the reads of the activations, in small CTAs that end one by one; few: one to a warp and eight
+// warps to its columns, which keeps more multiprocessors busy.  28672 x 4096: 8 tokens 19.3 us (eight-warp CTAs 21.6),
+// 16 tokens 26.6 us (29.7), 32 tokens 45 us (49); 6144 x 4096 for one token: 5.7 us with few, 6.5 us with many.
 template <typename OUT>
 cudaError_t launch_matvec(const MatvecArgs& a, unsigned grid_y, cudaStream_t st)
 {
     const bool few = (int64_t)(a.row_tiles + 1) / 2 * grid_y < 4 * 148;
-    if (a.slots <= 8 || a.ids) return few ? launch_matvec<OUT, 1, 1, 4, false>(a, grid_y, st) : launch_matvec<OUT, 2, 1, 3, false>(a, grid_y, st);
-    if (a.slots <= 16) return few ? launch_matvec<OUT, 1, 2, 3, false>(a, grid_y, st) : launch_matvec<OUT, 2, 2, 2, false>(a, grid_y, st);
-    return few ? launch_matvec<OUT, 1, 4, 2, false>(a, grid_y, st) : launch_matvec<OUT, 2, 4, 1, true>(a, grid_y, st);
+    if (a.slots <= 8 || a.ids) return few ? launch_matvec<OUT, 1, 1, 8, 4, false>(a, grid_y, st) : launch_matvec<OUT, 2, 1, 4, 4, true>(a, grid_y, st);
+    if (a.slots <= 16) return few ? launch_matvec<OUT, 1, 2, 8, 3, false>(a, grid_y, st) : launch_matvec<OUT, 2, 2, 4, 4, false>(a, grid_y, st);
+    return few ? launch_matvec<OUT, 1, 4, 8, 2, false>(a, grid_y, st) : launch_matvec<OUT, 2, 4, 4, 2, true>(a, grid_y, st);
 }
 
 // One thread per word of eight codes of the packed layout, from the library's own slots (16 codes to 16 bytes, code i
