@@ -1,13 +1,18 @@
 // mxfp8_moe_dispatch_quantize: the conversion of rows gathered by an index (tokens in the order of their experts, App. A.4),
-// optionally weighted.  The arithmetic of a 32-row slab is that of the fast path (quantize_tma_kernel.cuh); what differs is
-// how a slab arrives and who waits for whom:
-//   loads  : a warp fetches its own slab with 16-byte asynchronous copies, two rows per instruction, straight from the
-//            tokens' rows (a gathering tensor copy was tried first: its issue runs through the lanes one by one, some 2000
-//            cycles of one warp per tile with the other three waiting: 88 us for the row-blocked copy of 53248 x 2048
+// optionally weighted.  Tile, slab and staging of the scale bytes are those of the fast path (quantize_tma_kernel.cuh), and so
+// is the careful path for slabs with Inf or NaN or columns behind the tensor; the rest is made for rows that mostly come from L2,
+// where the conversion's instructions, not its bytes, set the pace:
+//   loads  : a warp fetches its own 32-row slab with 16-byte asynchronous copies, two rows per instruction, straight from
+//            the tokens' rows (a gathering tensor copy was tried first: its issue runs through the lanes one by one, some
+//            2000 cycles of one warp per tile with the other three waiting: 88 us for the row-blocked copy of 53248 x 2048
 //            rows against 55 us).  Rows without a slot and columns behind the tensor are zero-filled by the copies.
-//   weights: one FP32 product and one rounding per element, in place in the slab, before the conversion
 //   order  : slots of the tile after next are asked for under the current slab, its copies go out as soon as the slab
 //            is done; the CTA meets once per tile, for the scale bytes
+//   rows   : lane r takes the whole of row r, 16 bytes at a time: weights it (one FP32 product and one rounding per element,
+//            back in place) and finds the row's block maxima without a shuffle; 16-byte piece c of row r lies at c ^ (r mod
+//            16), so that this walk and the walk by columns both read shared memory without conflicts
+//   columns: lane l owns 8 bytes of every row, as in the fast path; the 32 rows stay in registers for the conversion
+//   cast   : products of two elements per instruction
 #include "quantize_tma_kernel.cuh"
 
 namespace mxfp8 {
@@ -15,24 +20,182 @@ namespace {
 
 constexpr int SLAB_BYTES = 32 * T_BYTES;
 
-// Gathered rows in place, same ownership as act_slab: row j times the weight that lane j holds.
-template <bool BF>
-__device__ __forceinline__ void weigh_slab(uint8_t* mine, float weight)
+// The larger magnitude of each half; the sign bits are of no meaning.  A NaN gives way to the other operand.
+__device__ __forceinline__ uint32_t max_magnitude2(uint32_t a, uint32_t b)
 {
-#pragma unroll 8
-    for (int j = 0; j < 32; ++j) {
-        const float f = __shfl_sync(0xFFFFFFFFu, weight, j);
-        uint2 w = *reinterpret_cast<const uint2*>(mine + j * T_BYTES);
-        if constexpr (BF) {
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(__uint_as_float(w.x << 16) * f, __uint_as_float(w.x & 0xFFFF0000u) * f);
-            const __nv_bfloat162 hi = __floats2bfloat162_rn(__uint_as_float(w.y << 16) * f, __uint_as_float(w.y & 0xFFFF0000u) * f);
-            w.x = *reinterpret_cast<const uint32_t*>(&lo);
-            w.y = *reinterpret_cast<const uint32_t*>(&hi);
-        } else {
-            w.x = __float_as_uint(__uint_as_float(w.x) * f);
-            w.y = __float_as_uint(__uint_as_float(w.y) * f);
+    uint32_t m;
+    asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
+}
+// Two FP32 products, each rounded to nearest even
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 bf16_pair(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ uint32_t weigh_pair(uint32_t w, float f)
+{
+    const float2 p = mul2(bf16_pair(w), make_float2(f, f));
+    const __nv_bfloat162 r = __floats2bfloat162_rn(p.x, p.y);
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// 8 bytes of row j of a slab that belong to this lane / 16-byte piece c of row r
+__device__ __forceinline__ uint32_t lane_place(int j, int lane) { return j * T_BYTES + ((((lane >> 1) ^ (j & 15)) << 4) | ((lane & 1) << 3)); }
+__device__ __forceinline__ uint32_t piece_place(int r, int c) { return r * T_BYTES + ((c ^ (r & 15)) << 4); }
+
+// First walk: row `lane` of the slab is weighted in place and its block maxima become scale bytes (staged) and factors 1/X
+// (in `inv`, four per row).  Returns whether a maximum is Inf (NaN elements do not enter it).
+template <int DTYPE, int ELEM, bool DO_ROW>
+__device__ __forceinline__ bool walk_row(uint8_t* slab, float* inv, float weight, bool weighted, uint8_t* my_scales, int lane, uint32_t rule_offset)
+{
+    constexpr bool BF = (DTYPE == MXFP8_BF16);
+    constexpr int NKB = BF ? 4 : 2, PIECES = 16 / NKB;       // blocks of the row, pieces of a block
+    uint32_t top[NKB];
+#pragma unroll
+    for (int b = 0; b < NKB; ++b) {
+        uint32_t m = 0u;
+        float f = 0.f;
+#pragma unroll
+        for (int c = 0; c < PIECES; ++c) {
+            uint4* at = reinterpret_cast<uint4*>(slab + piece_place(lane, b * PIECES + c));
+            uint4 v = *at;
+            if (weighted) {
+                if constexpr (BF) {
+                    v.x = weigh_pair(v.x, weight); v.y = weigh_pair(v.y, weight);
+                    v.z = weigh_pair(v.z, weight); v.w = weigh_pair(v.w, weight);
+                } else {
+                    const float2 w2 = make_float2(weight, weight);
+                    const float2 lo = mul2(make_float2(__uint_as_float(v.x), __uint_as_float(v.y)), w2);
+                    const float2 hi = mul2(make_float2(__uint_as_float(v.z), __uint_as_float(v.w)), w2);
+                    v = make_uint4(__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x), __float_as_uint(hi.y));
+                }
+                *at = v;
+            }
+            if constexpr (!DO_ROW) continue;
+            if constexpr (BF) m = max_magnitude2(max_magnitude2(max_magnitude2(max_magnitude2(m, v.x), v.y), v.z), v.w);
+            else f = fmaxf(fmaxf(f, fmaxf(fabsf(__uint_as_float(v.x)), fabsf(__uint_as_float(v.y)))),
+                           fmaxf(fabsf(__uint_as_float(v.z)), fabsf(__uint_as_float(v.w))));
         }
-        *reinterpret_cast<uint2*>(mine + j * T_BYTES) = w;
+        if constexpr (BF) top[b] = max(m & 0x7FFFu, (m >> 16) & 0x7FFFu);
+        else top[b] = __float_as_uint(f);
+    }
+    if constexpr (!DO_ROW) return false;
+    if constexpr (BF) {
+        const uint32_t z01 = top[0] | (top[1] << 16), z23 = top[NKB - 2] | (top[NKB - 1] << 16), off2 = (rule_offset >> 16) * 0x00010001u;
+        const uint32_t e01 = inv_exp_field2<ELEM>(z01, off2), e23 = inv_exp_field2<ELEM>(z23, off2);
+        *reinterpret_cast<uint32_t*>(my_scales) = __byte_perm(0x00FE00FEu - e01, 0x00FE00FEu - e23, 0x6420);
+        *reinterpret_cast<float4*>(inv + lane * 4) = make_float4(__uint_as_float(e01 << 23), __uint_as_float((e01 & 0xFFFF0000u) << 7),
+                                                                  __uint_as_float(e23 << 23), __uint_as_float((e23 & 0xFFFF0000u) << 7));
+        return (nonfinite2(z01) | nonfinite2(z23)) != 0u;
+    } else {
+        const uint32_t e0 = inv_exp_field<ELEM>(top[0], rule_offset), e1 = inv_exp_field<ELEM>(top[1], rule_offset);
+        *reinterpret_cast<uint16_t*>(my_scales) = (uint16_t)((254u - e0) | (254u - e1) << 8);
+        *reinterpret_cast<float2*>(inv + lane * 4) = make_float2(__uint_as_float(e0 << 23), __uint_as_float(e1 << 23));
+        return top[0] == 0x7F800000u || top[1] == 0x7F800000u;
+    }
+}
+
+// This lane's VEC elements of a row times the factors, as codes
+template <int ELEM, int VEC>
+__device__ __forceinline__ void store_codes(uint8_t* to, const float2 (&x)[VEC / 2], const float2 (&f)[VEC / 2], int lane)
+{
+    constexpr bool SUB = (ELEM != MXFP8_E4M3 && ELEM != MXFP8_E5M2);
+    if constexpr (VEC == 4) {
+        const float2 a = mul2(x[0], f[0]), b = mul2(x[1], f[1]);
+        uint32_t c = cvt_fp8x4<ELEM>(a.x, a.y, b.x, b.y);
+        if constexpr (SUB) c = pack_slot<ELEM, VEC>(c, lane);
+        *reinterpret_cast<uint32_t*>(to) = c;
+    } else {
+        const float2 a = mul2(x[0], f[0]);
+        uint32_t c = cvt_fp8x2<ELEM>(a.x, a.y);
+        if constexpr (SUB) c = pack_slot<ELEM, VEC>(c, lane);
+        *reinterpret_cast<uint16_t*>(to) = (uint16_t)c;
+    }
+}
+
+// One slab whose columns all lie inside the tensor.  Returns true, with nothing stored but staged scale bytes, when an Inf
+// takes part (or a whole column of NaN); the slab then holds the weighted rows.
+template <int DTYPE, int ELEM, bool DO_ROW, bool DO_COL>
+__device__ __forceinline__ bool convert_slab(uint8_t* slab, float* inv, uint8_t* my_qrow, uint8_t* my_qcol, uint32_t pitch, uint8_t* my_row_scales,
+                                             uint8_t* my_sm_col, float weight, bool weighted, int lane, uint32_t rule_offset)
+{
+    constexpr bool BF = (DTYPE == MXFP8_BF16);
+    constexpr int VEC = BF ? 4 : 2;
+    bool special = false;
+    if (DO_ROW || weighted) {
+        special = walk_row<DTYPE, ELEM, DO_ROW>(slab, inv, weight, weighted, my_row_scales, lane, rule_offset);
+        __syncwarp();
+    }
+    uint2 raw[DO_COL ? 32 : 1];
+    float2 col[VEC / 2];
+    if constexpr (DO_COL) {
+        uint32_t bits[VEC];
+        if constexpr (BF) {
+            uint32_t m0 = 0u, m1 = 0u;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                raw[j] = *reinterpret_cast<const uint2*>(slab + lane_place(j, lane));
+                m0 = max_magnitude2(m0, raw[j].x);
+                m1 = max_magnitude2(m1, raw[j].y);
+            }
+            bits[0] = (m0 & 0x7FFFu) << 16; bits[1] = m0 & 0x7FFF0000u;
+            bits[2] = (m1 & 0x7FFFu) << 16; bits[3] = m1 & 0x7FFF0000u;
+        } else {
+            float m0 = 0.f, m1 = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                raw[j] = *reinterpret_cast<const uint2*>(slab + lane_place(j, lane));
+                m0 = fmaxf(m0, fabsf(__uint_as_float(raw[j].x)));
+                m1 = fmaxf(m1, fabsf(__uint_as_float(raw[j].y)));
+            }
+            bits[0] = __float_as_uint(m0); bits[1] = __float_as_uint(m1);
+        }
+        float f[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            special = special || bits[i] >= 0x7F800000u;
+            const uint32_t e = inv_exp_field<ELEM>(bits[i], rule_offset);
+            f[i] = __uint_as_float(e << 23);
+            my_sm_col[i * STAGE_PITCH] = (uint8_t)(254u - e);
+        }
+#pragma unroll
+        for (int i = 0; i < VEC / 2; ++i) col[i] = make_float2(f[2 * i], f[2 * i + 1]);
+    }
+    if (__any_sync(0xFFFFFFFFu, special)) return true;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        uint2 w;
+        if constexpr (DO_COL) w = raw[j];
+        else w = *reinterpret_cast<const uint2*>(slab + lane_place(j, lane));
+        float2 x[VEC / 2];
+        if constexpr (BF) {
+            x[0] = bf16_pair(w.x);
+            x[VEC / 2 - 1] = bf16_pair(w.y);
+        } else x[0] = make_float2(__uint_as_float(w.x), __uint_as_float(w.y));
+        if constexpr (DO_ROW) {
+            const float r = inv[j * 4 + lane / (32 / VEC)];
+            float2 f[VEC / 2];
+#pragma unroll
+            for (int i = 0; i < VEC / 2; ++i) f[i] = make_float2(r, r);
+            store_codes<ELEM, VEC>(my_qrow + (uint64_t)j * pitch, x, f, lane);
+        }
+        if constexpr (DO_COL) store_codes<ELEM, VEC>(my_qcol + (uint64_t)j * pitch, x, col, lane);
+    }
+    return false;
+}
+
+// The slab back in plain order, for the careful path
+__device__ __noinline__ void plain_order(uint8_t* slab, int lane)
+{
+    for (int j = 0; j < 32; ++j) {
+        const uint2 v = *reinterpret_cast<const uint2*>(slab + lane_place(j, lane));
+        __syncwarp();
+        *reinterpret_cast<uint2*>(slab + j * T_BYTES + lane * 8) = v;
+        __syncwarp();
     }
 }
 
@@ -48,6 +211,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
 
     extern __shared__ __align__(128) uint8_t smem[];
     uint8_t* sm_scales = smem + RING * IN_BYTES;    // 2 x (row scales + column scales of one tile, 512 bytes each)
+    float* row_inv = reinterpret_cast<float*>(sm_scales + 2048) + (threadIdx.x >> 5) * 128;      // this warp's row factors, four per row
     __shared__ int queue[4];                        // tiles of the next iterations
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;   // warp = 32-row slab of the tile
@@ -81,14 +245,14 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
         const int64_t col = (int64_t)lx * T_COLS + (lane & 15) * (16 / ESZ);
         const bool col_ok = col < p.cols;
         const uint8_t* src = static_cast<const uint8_t*>(batch.gather_src) + (col_ok ? col : 0) * ESZ;
-        const uint32_t to = smem_addr(my_slabs + buf * IN_BYTES + (lane >> 4) * T_BYTES + (lane & 15) * 16);
+        const uint32_t to = smem_addr(my_slabs + buf * IN_BYTES);
         if (slot < 0) token = -1;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const int tk = __shfl_sync(0xFFFFFFFFu, token, 2 * i + (lane >> 4));
             const uint32_t bytes = (tk >= 0 && col_ok) ? 16u : 0u;               // 0: the 16 bytes are filled with zeros
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                         ::"r"(to + i * 2 * T_BYTES), "l"(src + (int64_t)max(tk, 0) * p.cols * ESZ), "r"(bytes) : "memory");
+                         ::"r"(to + piece_place(2 * i + (lane >> 4), lane & 15)), "l"(src + (int64_t)max(tk, 0) * p.cols * ESZ), "r"(bytes) : "memory");
         }
     };
     auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
@@ -129,23 +293,29 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
 
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         __syncwarp();
-        uint8_t* my_in = my_slabs + buf * IN_BYTES + lane * 8;
-        if (batch.slot_weights != nullptr) {
-            weigh_slab<BF>(my_in, buf ? weight[1] : weight[0]);
-            // a row without a slot holds zeros, which a weight of its own (0) leaves alone
-        }
+        uint8_t* slab = my_slabs + buf * IN_BYTES;
+        const bool weighted = batch.slot_weights != nullptr;          // a row without a slot holds zeros and has the weight 0
+        const float my_weight = buf ? weight[1] : weight[0];
         const int64_t my_col = gcol0 + lane * VEC;
         const bool col_ok = my_col < p.cols;                                         // cols % 16 == 0: a lane's bytes are all in or all out
         uint8_t* my_qrow = p.q_row + ((grow0 + warp * 32) * p.cols + my_col);
         uint8_t* my_qcol = p.q_col + ((grow0 + warp * 32) * p.cols + my_col);
         const uint32_t pitch = (uint32_t)p.cols;
-        uint8_t* my_sm_row = sm_row + warp * 4 + lane / LPB;                   // row 32 warp + j: + j * STAGE_PITCH
         uint8_t* my_sm_col = sm_col + stage_offset(lane * VEC) + warp;         // column lane * VEC + i: + i * STAGE_PITCH
-        bool special = !__all_sync(0xFFFFFFFFu, col_ok);
-        if (!special)
-            special = slab_fast<DTYPE, ELEM, DO_ROW, DO_COL, false>(my_in, my_qrow, my_qcol, pitch, my_sm_row, my_sm_col, lane, rule_offset);
-        if (special)
-            slab_careful<DTYPE, ELEM, DO_ROW, DO_COL, false>(my_in, my_qrow, my_qcol, pitch, my_sm_row, my_sm_col, lane, rule_offset, 32, col_ok);
+        const bool whole = __all_sync(0xFFFFFFFFu, col_ok);
+        bool special = !whole;
+        if (whole)
+            special = convert_slab<DTYPE, ELEM, DO_ROW, DO_COL>(slab, row_inv, my_qrow, my_qcol, pitch, sm_row + stage_offset(warp * 32 + lane), my_sm_col,
+                                                                my_weight, weighted, lane, rule_offset);
+        else if (weighted) {
+            walk_row<DTYPE, ELEM, false>(slab, row_inv, my_weight, true, nullptr, lane, rule_offset);
+            __syncwarp();
+        }
+        if (special) {
+            plain_order(slab, lane);
+            slab_careful<DTYPE, ELEM, DO_ROW, DO_COL, false>(slab + lane * 8, my_qrow, my_qcol, pitch, sm_row + warp * 4 + lane / LPB, my_sm_col, lane,
+                                                             rule_offset, 32, col_ok);
+        }
         __syncwarp();
         if (after < num_tiles) {
             raw = checked(raw);
@@ -172,7 +342,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
 template <int DTYPE, int ELEM, bool R, bool C>
 cudaError_t launch_gather(const QBatch& p, cudaStream_t stream)
 {
-    constexpr int SMEM = RING * IN_BYTES + 2048;
+    constexpr int SMEM = RING * IN_BYTES + 2048 + QT_THREADS * 16;      // ring, scale staging, row factors
     auto kernel = quantize_gather_kernel<DTYPE, ELEM, R, C>;
     static unsigned long long smem_set = 0;
     cudaError_t err = ensure_dynamic_smem(kernel, SMEM, smem_set);
