@@ -7,7 +7,7 @@
 //            2000 cycles of one warp per tile with the other three waiting: 88 us for the row-blocked copy of 53248 x 2048
 //            rows against 55 us).  Rows without a slot and columns behind the tensor are zero-filled by the copies.
 //   order  : slots of the tile after next are asked for under the current slab, its copies go out as soon as the slab
-//            is done; the CTA meets once per tile, for the scale bytes
+//            is done; no warp waits for another but the one that stores a tile's scale bytes, a different one each tile
 //   rows   : lane r takes the whole of row r, 16 bytes at a time: weights it (one FP32 product and one rounding per element,
 //            back in place) and finds the row's block maxima without a shuffle; 16-byte piece c of row r lies at c ^ (r mod
 //            16), so that this walk and the walk by columns both read shared memory without conflicts
@@ -19,6 +19,10 @@ namespace mxfp8 {
 namespace {
 
 constexpr int SLAB_BYTES = 32 * T_BYTES;
+// Scale bytes of the last four tiles.  Warp i mod 4 stores those of the CTA's i-th tile, waiting for the other three, which only
+// announce themselves.  A warp therefore waits for all others once in four tiles, so when it writes the bytes of tile
+// i + 4 everyone has announced a tile after i, and who stored tile i had done so before that: four buffers, four barriers.
+constexpr int STAGES = 4;
 
 // The larger magnitude of each half; the sign bits are of no meaning.  A NaN gives way to the other operand.
 __device__ __forceinline__ uint32_t max_magnitude2(uint32_t a, uint32_t b)
@@ -210,9 +214,8 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
     constexpr int LPB = 32 / VEC;                   // lanes per row block: 8 or 16
 
     extern __shared__ __align__(128) uint8_t smem[];
-    uint8_t* sm_scales = smem + RING * IN_BYTES;    // 2 x (row scales + column scales of one tile, 512 bytes each)
-    float* row_inv = reinterpret_cast<float*>(sm_scales + 2048) + (threadIdx.x >> 5) * 128;      // this warp's row factors, four per row
-    __shared__ int queue[4];                        // tiles of the next iterations
+    uint8_t* sm_scales = smem + RING * IN_BYTES;    // STAGES x (row scales + column scales of one tile, 512 bytes each)
+    float* row_inv = reinterpret_cast<float*>(sm_scales + STAGES * 1024) + (threadIdx.x >> 5) * 128;      // this warp's row factors, four per row
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;   // warp = 32-row slab of the tile
     const QParams& p = batch.t[0];
@@ -245,6 +248,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
         const int64_t col = (int64_t)lx * T_COLS + (lane & 15) * (16 / ESZ);
         const bool col_ok = col < p.cols;
         const uint8_t* src = static_cast<const uint8_t*>(batch.gather_src) + (col_ok ? col : 0) * ESZ;
+        const uint32_t src_pitch = (uint32_t)p.cols * ESZ;
         const uint32_t to = smem_addr(my_slabs + buf * IN_BYTES);
         if (slot < 0) token = -1;
 #pragma unroll
@@ -252,40 +256,33 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
             const int tk = __shfl_sync(0xFFFFFFFFu, token, 2 * i + (lane >> 4));
             const uint32_t bytes = (tk >= 0 && col_ok) ? 16u : 0u;               // 0: the 16 bytes are filled with zeros
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                         ::"r"(to + piece_place(2 * i + (lane >> 4), lane & 15)), "l"(src + (int64_t)max(tk, 0) * p.cols * ESZ), "r"(bytes) : "memory");
+                         ::"r"(to + piece_place(2 * i + (lane >> 4), lane & 15)), "l"(src + (uint64_t)(uint32_t)max(tk, 0) * src_pitch), "r"(bytes) : "memory");
         }
     };
     auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
-    auto next_tile = [&](int it) {                  // one thread: the tile of iteration `it` (handed out in order, or by CTA index)
-        return batch.sched ? (int)atomicAdd(batch.sched, 1u) : (int)blockIdx.x + it * (int)gridDim.x;
-    };
-
-    if (tid == 0)
-        for (int k = 0; k < 3; ++k) queue[k] = next_tile(k);
-    __syncthreads();
-    int slot[RING];                                 // of this lane's row in the slabs of iterations it, it + 1
-    float weight[RING];
+    auto weight_of = [&](int slot) { return (batch.slot_weights != nullptr && slot >= 0) ? batch.slot_weights[slot] : 0.f; };
+    int next_slot = -1;                             // of this lane's row in the next tile
+    float my_weight = 0.f;                          // of this lane's row in this tile (a row without a slot holds zeros and has the weight 0)
 #pragma unroll
     for (int k = 0; k < RING; ++k) {
-        slot[k] = -1;
-        weight[k] = 0.f;
-        if (queue[k] < num_tiles) {
-            slot[k] = checked(slot_in(queue[k]));
-            issue(queue[k], slot[k], k);
-            if (batch.slot_weights != nullptr && slot[k] >= 0) weight[k] = batch.slot_weights[slot[k]];
+        const int t = blockIdx.x + k * gridDim.x;
+        int slot = -1;
+        if (t < num_tiles) {
+            slot = checked(slot_in(t));
+            issue(t, slot, k);
         }
         commit();
+        if (k == 0) my_weight = weight_of(slot);
+        else next_slot = slot;
     }
-    for (int it = 0;; ++it) {
-        const int tile = queue[it & 3];
-        if (tile >= num_tiles) break;
+    int it = 0;
+    for (int tile = blockIdx.x; tile < num_tiles; tile += gridDim.x, ++it) {
         const int buf = it & 1;
-        const int after = queue[(it + 2) & 3];      // the tile that will refill this slab
-        int handed = 0;
-        if (tid == 0) handed = next_tile(it + 3);   // asked for now, needed at the barrier (the counter's round trip hides under the slab)
+        const int after = tile + RING * (int)gridDim.x;         // the tile that will refill this slab
         int raw = -1;
-        if (after < num_tiles) raw = slot_in(after);
-        uint8_t* sm_row = sm_scales + (it & 1) * 1024;          // 128 rows x 4 blocks, at stage_offset(row)
+        if (after < num_tiles) raw = slot_in(after);            // asked for here, needed behind the slab; so is the next tile's weight
+        const float next_weight = weight_of(next_slot);
+        uint8_t* sm_row = sm_scales + (it % STAGES) * 1024;     // 128 rows x 4 blocks, at stage_offset(row)
         uint8_t* sm_col = sm_row + 512;                         // T_COLS columns x 4 blocks, at stage_offset(column)
         int tile_x, tile_y;
         divmod((uint32_t)tile, (uint32_t)p.tiles_x, p.tiles_x_magic, tile_y, tile_x);
@@ -294,8 +291,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         __syncwarp();
         uint8_t* slab = my_slabs + buf * IN_BYTES;
-        const bool weighted = batch.slot_weights != nullptr;          // a row without a slot holds zeros and has the weight 0
-        const float my_weight = buf ? weight[1] : weight[0];
+        const bool weighted = batch.slot_weights != nullptr;
         const int64_t my_col = gcol0 + lane * VEC;
         const bool col_ok = my_col < p.cols;                                         // cols % 16 == 0: a lane's bytes are all in or all out
         uint8_t* my_qrow = p.q_row + ((grow0 + warp * 32) * p.cols + my_col);
@@ -320,30 +316,26 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
         if (after < num_tiles) {
             raw = checked(raw);
             issue(after, raw, buf);
-            const float w = (batch.slot_weights != nullptr && raw >= 0) ? batch.slot_weights[raw] : 0.f;
-            if (buf) weight[1] = w;
-            else weight[0] = w;
         }
+        my_weight = next_weight;
+        next_slot = raw;
         commit();
-        if (tid == 0) queue[(it + 3) & 3] = handed;
-        __syncthreads();                            // the tile's scale bytes are complete
-        store_scales<BF, DO_ROW, DO_COL, false>(p, tile_x, tile_y, sm_row, sm_col, tid, lane, warp);
+        if (it % STAGES == warp) {
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + it % STAGES), "n"(QT_THREADS) : "memory");
+#pragma unroll 1
+            for (int k = 0; k < QT_THREADS / 32; ++k)           // one warp does the whole CTA's part
+                store_scales<BF, DO_ROW, DO_COL, false>(p, tile_x, tile_y, sm_row, sm_col, k * 32 + lane, lane, k);
+        } else asm volatile("bar.arrive %0, %1;" ::"r"(1 + it % STAGES), "n"(QT_THREADS) : "memory");
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
-    if (tid == 0 && batch.sched != nullptr) {       // the last CTA out zeroes the words for the next launch
-        __threadfence();
-        if (atomicAdd(batch.sched + 1, 1u) == gridDim.x - 1) {
-            batch.sched[0] = 0u;
-            batch.sched[1] = 0u;
-        }
-    }
 }
 
 template <int DTYPE, int ELEM, bool R, bool C>
 cudaError_t launch_gather(const QBatch& p, cudaStream_t stream)
 {
-    constexpr int SMEM = RING * IN_BYTES + 2048 + QT_THREADS * 16;      // ring, scale staging, row factors
+    constexpr int SMEM = RING * IN_BYTES + STAGES * 1024 + QT_THREADS * 16;      // ring, scale staging, row factors
     auto kernel = quantize_gather_kernel<DTYPE, ELEM, R, C>;
+    static_assert(QT_THREADS / 32 == STAGES, "every warp stores one tile of STAGES");
     static unsigned long long smem_set = 0;
     cudaError_t err = ensure_dynamic_smem(kernel, SMEM, smem_set);
     if (err != cudaSuccess) return err;
@@ -405,7 +397,7 @@ extern "C" int mxfp8_moe_dispatch_quantize(const void* src, int src_dtype, int64
     if ((reinterpret_cast<uintptr_t>(weights) & 3u) || (reinterpret_cast<uintptr_t>(group_offsets) & 3u)) return MXFP8_ERR_ALIGN;
     if ((orientation & MXFP8_ROW) && (!aligned16(q_row) || !aligned16(s_row))) return MXFP8_ERR_ALIGN;
     if ((orientation & MXFP8_COL) && (!aligned16(q_col) || !aligned16(s_col))) return MXFP8_ERR_ALIGN;
-    if (tokens > 0x7F000000LL || tokens * top_k > 0x7F000000LL) return MXFP8_ERR_UNSUPPORTED;
+    if (tokens > 0x7F000000LL || tokens * top_k > 0x7F000000LL || cols > 0x3FFFFFFFLL) return MXFP8_ERR_UNSUPPORTED;      // 32-bit counters and pitches
     if (!quantize_tma_eligible(src_dtype, rows, cols)) return MXFP8_ERR_UNSUPPORTED;   // needs cols % 16 == 0
     const QuantizeItem item{src, rows, cols, q_row, s_row, q_col, s_col};
     const GatherArgs gather{tokens, slot_of, weights, group_offsets + num_groups, top_k};
