@@ -1,6 +1,6 @@
 // Mixture-of-experts token movement around mxfp8_grouped_gemm (App. A.4): sorting the routed tokens by expert into
 // segments that start at multiples of 128 rows, gathering the experts' outputs back with the router's weights, and the
-// gradient of that sum.  (The gather into the sorted order is fused with the conversion: quantize_tma_kernel.cuh.)
+// gradient of that sum.  (The gather into the sorted order is fused with the conversion: quantize_gather.cu.)
 //
 // A slot is one (token, choice) pair, numbered token * top_k + choice.
 #include "mxfp8_device.cuh"
