@@ -405,7 +405,8 @@ int mxfp8_grouped_gemm(const void* Aq, const void* As, const void* Bq, const voi
  *
  * Entries of row_of / slot_of that are neither -1 nor a row / slot of the tensors, or a group_offsets[num_groups] that is
  * no possible end, leave MXFP8_ERR_DEVICE_ARGS in the device status word; such an entry counts as -1, and with such an end
- * nothing is stored into rows.  Two slots must not share a row.
+ * no row is in use.  In mxfp8_moe_combine_grad an entry of row_of has to lie below that end where group_offsets is given.
+ * Two slots must not share a row.
  */
 int64_t mxfp8_moe_rows(int64_t tokens, int top_k, int num_experts);
 size_t mxfp8_moe_sort_ws_bytes(int64_t tokens, int top_k, int num_experts);

@@ -255,6 +255,15 @@ __device__ __forceinline__ int checked_row(int32_t r, int64_t rows, int* status)
     if (r != -1) atomicExch(status, (int)MXFP8_ERR_DEVICE_ARGS);
     return -1;
 }
+// Rows that the gradient may touch: those in use where the caller names their end, none where that end cannot be one.
+__device__ __forceinline__ int64_t rows_in_use(const MoveArgs& a)
+{
+    if (a.used == nullptr) return a.rows;
+    const int used = *a.used;
+    if (used >= 0 && used <= a.rows) return used;
+    atomicExch(a.status, (int)MXFP8_ERR_DEVICE_ARGS);
+    return 0;
+}
 
 // Vectors per lane and row when there is plenty to do: a lane asks for 256 bytes of the K rows before it uses any, which
 // with 16 warps on a multiprocessor keeps more than 100 KB in flight.
@@ -341,7 +350,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, COMBINE_CTAS<U>) moe_combine_ker
 
 // d_src[row_of[t, j], c] = w[t, j] * dy[t, c] (one FP32 product, rounded to src's type) and
 // d_weights[t, j] = sum_c dy[t, c] * src[row_of[t, j], c] (FP32: lane-strided partial sums, then a fixed tree), so dy is
-// read once per token and K choices.  `group` threads share a token: one warp while tokens fill the machine, which
+// read once per token and K choices.  Rows have to lie among those in use.  `group` threads share a token: one warp while tokens fill the machine, which
 // leaves the sums to shuffles; up to a whole CTA for few tokens.  CTAs behind the tokens' clear the padding rows.
 template <int DY, int SRC, int V, int K>
 __global__ void __launch_bounds__(MOVE_THREADS) moe_combine_grad_kernel(const MoveArgs a)
@@ -350,14 +359,12 @@ __global__ void __launch_bounds__(MOVE_THREADS) moe_combine_grad_kernel(const Mo
     __shared__ float sums[MOVE_WARPS][K];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if ((int64_t)blockIdx.x >= a.token_blocks) {
-        const int used = *a.used;
-        if (used < 0 || used > a.rows) {
-            if (tid == 0) atomicExch(a.status, (int)MXFP8_ERR_DEVICE_ARGS);
-            return;
-        }
+        const int64_t used = rows_in_use(a);
         const int64_t row0 = ((int64_t)blockIdx.x - a.token_blocks) * 32 + warp * 4;
         for (int64_t r = row0; r < row0 + 4 && r < used; ++r) {
-            if (a.slot_of[r] >= 0) continue;
+            const int slot = a.slot_of[r];
+            if (slot >= 0 && slot < a.tokens * a.top_k) continue;
+            if (slot != -1) atomicExch(a.status, (int)MXFP8_ERR_DEVICE_ARGS);
             Vec<SRC, V> z;
             z.zero();
             for (int64_t c = (int64_t)lane * V; c < a.cols; c += 32 * V) z.store(a.dst, r * a.cols + c);
@@ -367,12 +374,13 @@ __global__ void __launch_bounds__(MOVE_THREADS) moe_combine_grad_kernel(const Mo
     const int per_block = MOVE_THREADS / a.group, member = tid % a.group;
     const int64_t t = (int64_t)blockIdx.x * per_block + tid / a.group;
     const int64_t stride = (int64_t)a.group * V;
+    const int64_t rows = rows_in_use(a);
     for (int j0 = 0; j0 < a.top_k; j0 += K) {
         int my_row = -1;
         float my_w = 0.f;
         if (t < a.tokens && lane < K && j0 + lane < a.top_k) {
             const int64_t slot = t * a.top_k + j0 + lane;
-            my_row = checked_row(a.row_of[slot], a.rows, a.status);
+            my_row = checked_row(a.row_of[slot], rows, a.status);
             my_w = a.weights ? a.weights[slot] : 1.f;
         }
         int row[K];

@@ -252,6 +252,38 @@ def test_bad_device_arrays_are_reported():
     assert B.mxfp8_device_status() == B.ERR_DEVICE_ARGS
 
 
+def test_gradient_stores_no_row_that_the_offsets_do_not_own():
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    x = torch.ones(8, 64, device="cuda")
+    off, row_of, slot_of = gpu_sort(routing(8, 2, 4, 1), 4)
+    rows, used = slot_of.numel(), int(off[-1])
+    y = torch.ones(rows, 64, device="cuda")
+    for end in (-1, rows + 1, -2 ** 31, 2 ** 31 - 1):           # no possible end: no row is in use
+        bad = off.clone()
+        bad[-1] = end
+        d_y, d_w = torch.full_like(y, 7.0), torch.full((8, 2), 7.0, device="cuda")
+        B.mxfp8_moe_combine_grad(x, y, row_of, slot_of, None, bad, d_y, d_w)
+        assert B.mxfp8_device_status() == B.ERR_DEVICE_ARGS
+        assert (d_y == 7).all() and (d_w == 0).all()
+    more = torch.cat((slot_of, torch.full((128,), -1, dtype=torch.int32, device="cuda")))
+    y = torch.ones(rows + 128, 64, device="cuda")
+    bad = row_of.clone()
+    bad[5, 0] = used + 3                                        # a row of the tensor, behind the last segment
+    d_y, d_w = torch.full_like(y, 7.0), torch.full((8, 2), 7.0, device="cuda")
+    B.mxfp8_moe_combine_grad(x, y, bad, more, None, off, d_y, d_w)
+    assert B.mxfp8_device_status() == B.ERR_DEVICE_ARGS
+    assert (d_y[used:] == 7).all() and d_w[5, 0] == 0 and d_w[5, 1] == 64
+    for slot in (16, 2 ** 31 - 1, -5):                          # such an entry counts as -1: the row is cleared
+        bad = slot_of.clone()
+        bad[127] = slot
+        assert slot_of[127] == -1
+        d_y = torch.full((rows, 64), 7.0, device="cuda")
+        B.mxfp8_moe_combine_grad(x, y[:rows], row_of, bad, None, off, d_y, None)
+        assert B.mxfp8_device_status() == B.ERR_DEVICE_ARGS
+        assert not d_y[127].any()
+
+
 HALF = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}          # half a step of the type, relative to the value
 COLS = [1, 2, 3, 8, 37, 64, 100, 257, 1408, 2050, 4096]
 
