@@ -14,19 +14,22 @@
 //   columns: lane l owns 8 bytes of every row, as in the fast path; the 32 rows stay in registers for the conversion
 //   cast   : products of two elements per instruction
 // Measured at 53248 x 2048 BF16 rows of 8192 tokens, top-6, with the HBM time of the tokens read once and the outputs written:
-// 39 us for the row-blocked copy (22), 39 us by columns (22), 57 us for both (39), 66 us for both with weights; mxfp8_quantize
-// of the same rows already sorted takes 88 us for both.  62 % of the cycles issue to the integer pipe, the busiest.  One slab per warp instead of two, with 16 warps on a multiprocessor instead of
-// 12: 56 us for both, but 43 us by columns; 20 warps spill (66 us).
+// 38 us for the row-blocked copy (22), 39 us by columns (22), 57 us for both (39), 66 us for both with weights; mxfp8_quantize
+// of the same rows already sorted takes 88 us for both.  6272 x 4096 FP32 rows of 2999 tokens, weighted, both: 27 us (15).
+// From BF16 62 % of the cycles issue to the integer pipe, the busiest.  One slab per warp instead of two, with 16 warps on a
+// multiprocessor instead of 12: 56 us for both, but 43 us by columns; 20 warps spill (66 us).
 #include "quantize_tma_kernel.cuh"
 
 namespace mxfp8 {
 namespace {
 
 constexpr int SLAB_BYTES = 32 * T_BYTES;
-// Scale bytes of the last four tiles.  Warp i mod 4 stores those of the CTA's i-th tile, waiting for the other three, which only
-// announce themselves.  A warp therefore waits for all others once in four tiles, so when it writes the bytes of tile
-// i + 4 everyone has announced a tile after i, and who stored tile i had done so before that: four buffers, four barriers.
-constexpr int STAGES = 4;
+// Scale bytes of the last eight tiles.  Warp i mod 4 stores those of the CTA's i-th tile once it has converted its slab of
+// tile i + 1, by when the other three have mostly announced their slabs of tile i and need not be waited for (waiting right
+// behind tile i cost 9 % of the warps' time, 15 % from FP32).  Why eight buffers and barriers are enough: when a warp writes
+// the bytes of tile i + 8, the last tile m that it stored is at least i + 3, so all others had announced tile m, and who
+// stored tile i had done so before it announced tile i + 1 or any later one.
+constexpr int STORERS = QT_THREADS / 32, STAGES = 8;
 
 // The larger magnitude of each half; the sign bits are of no meaning.  A NaN gives way to the other operand.
 __device__ __forceinline__ uint32_t max_magnitude2(uint32_t a, uint32_t b)
@@ -286,7 +289,15 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
         if (k == 0) my_weight = weight_of(slot);
         else next_slot = slot;
     }
-    int it = 0;
+    auto store_tile = [&](int i, int x, int y) {    // one warp does the whole CTA's part
+        if (i % STORERS != warp) return;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + i % STAGES), "n"(QT_THREADS) : "memory");
+        const uint8_t* at = sm_scales + (i % STAGES) * 1024;
+#pragma unroll 1
+        for (int k = 0; k < QT_THREADS / 32; ++k)
+            store_scales<BF, DO_ROW, DO_COL, false>(p, x, y, at, at + 512, k * 32 + lane, lane, k);
+    };
+    int it = 0, before_x = 0, before_y = 0;         // the tile before this one
     for (int tile = blockIdx.x; tile < num_tiles; tile += gridDim.x, ++it) {
         const int buf = it & 1;
         const int after = tile + RING * (int)gridDim.x;         // the tile that will refill this slab
@@ -331,13 +342,12 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
         my_weight = next_weight;
         next_slot = raw;
         commit();
-        if (it % STAGES == warp) {
-            asm volatile("bar.sync %0, %1;" ::"r"(1 + it % STAGES), "n"(QT_THREADS) : "memory");
-#pragma unroll 1
-            for (int k = 0; k < QT_THREADS / 32; ++k)           // one warp does the whole CTA's part
-                store_scales<BF, DO_ROW, DO_COL, false>(p, tile_x, tile_y, sm_row, sm_col, k * 32 + lane, lane, k);
-        } else asm volatile("bar.arrive %0, %1;" ::"r"(1 + it % STAGES), "n"(QT_THREADS) : "memory");
+        if (it > 0) store_tile(it - 1, before_x, before_y);
+        if (it % STORERS != warp) asm volatile("bar.arrive %0, %1;" ::"r"(1 + it % STAGES), "n"(QT_THREADS) : "memory");
+        before_x = tile_x;
+        before_y = tile_y;
     }
+    if (it > 0) store_tile(it - 1, before_x, before_y);
     asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
@@ -346,7 +356,7 @@ cudaError_t launch_gather(const QBatch& p, cudaStream_t stream)
 {
     constexpr int SMEM = RING * IN_BYTES + STAGES * 1024 + QT_THREADS * 16;      // ring, scale staging, row factors
     auto kernel = quantize_gather_kernel<DTYPE, ELEM, R, C>;
-    static_assert(QT_THREADS / 32 == STAGES, "every warp stores one tile of STAGES");
+    static_assert(STAGES == 2 * STORERS, "see STAGES");
     static unsigned long long smem_set = 0;
     cudaError_t err = ensure_dynamic_smem(kernel, SMEM, smem_set);
     if (err != cudaSuccess) return err;
