@@ -60,10 +60,11 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 2^(b - 127): b = 0 is the subnormal 2^-127, b = 255 is NaN
-__device__ __forceinline__ float scale_value(uint32_t b)
+// 2^(b - c), what a scale byte b leaves to the sums when its weights took c = b clamped to 64 .. 127 (weights are BF16 then,
+// and a sum of 32 products only passes FP32's range where the scaled one does); b = 255 is NaN
+__device__ __forceinline__ float scale_rest(uint32_t b, uint32_t c)
 {
-    return __uint_as_float(b == 0u ? 0x00400000u : (b == 255u ? 0x7FC00000u : b << 23));
+    return __uint_as_float(b == 255u ? 0x7FC00000u : (b + 127u - c) << 23);
 }
 // 2^126 * 2^(b - 127) as BF16, for b <= 127: exponent field b + 126.  Two words hold a row's four factors, one per half, and
 // the product names the half that it takes.
@@ -149,9 +150,11 @@ __device__ __forceinline__ void product(const Operands<R, NT>& o, float (&acc)[R
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             uint32_t al[4], ah[4];
-            decode_word(wl[g], 0x7E807E80u, al);                // 2^126
-            decode_word(wh[g], 0x7E807E80u, ah);
-            const float f_lo = scale_value(o.s_lo[r] >> (8 * g) & 255u), f_hi = scale_value(o.s_hi[r] >> (8 * g) & 255u);
+            const uint32_t b_lo = o.s_lo[r] >> (8 * g) & 255u, b_hi = o.s_hi[r] >> (8 * g) & 255u;
+            const uint32_t c_lo = min(max(b_lo, 64u), 127u), c_hi = min(max(b_hi, 64u), 127u);
+            decode_word(wl[g], (c_lo + 126u) * 0x00800080u, al);       // 2^126 * 2^(c - 127), both halves
+            decode_word(wh[g], (c_hi + 126u) * 0x00800080u, ah);
+            const float f_lo = scale_rest(b_lo, c_lo), f_hi = scale_rest(b_hi, c_hi);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 float d[4] = {0.f, 0.f, 0.f, 0.f};

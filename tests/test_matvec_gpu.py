@@ -199,6 +199,28 @@ def test_every_code_and_every_scale_byte():
             assert np.isnan(y[:, 255]).all()
 
 
+@pytest.mark.parametrize("other", [127, 0, 200])
+def test_large_activations_under_small_scales_do_not_overflow(other):
+    """Sums that pass FP32's range before their scale and not after it; one row's byte decides which way the tile takes."""
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    rows, cols = 16, 64
+    bytes_of_rows = np.array([0, 1, 10, 40, 62, 63, 64, 65, 80, 90, 100, 110, 115, 115, 64, other], np.uint8)
+    codes = np.full((1, rows, cols), 7, np.uint8)               # 6.0
+    codes[:, :, 1::3] = 15                                      # -6.0
+    if other == 127:
+        bytes_of_rows = np.maximum(bytes_of_rows, 64)           # all inside 64 .. 127
+    scales = np.repeat(bytes_of_rows.reshape(1, rows, 1), cols // 32, axis=2)
+    flat = codes.reshape(-1, cols // 16, 16)
+    slots = np.zeros_like(flat)
+    slots[:, :, :8] = flat[:, :, 0::2] | flat[:, :, 1::2] << 4
+    packed = torch.empty(B.mxfp8_e2m1_packed_bytes(1, rows, cols), dtype=torch.uint8, device="cuda")
+    B.mxfp8_e2m1_pack(dev(slots.reshape(-1, cols)), dev(scales.reshape(-1)), 1, packed)
+    x, y = run(np.full((3, cols), 1.5 * 2.0 ** 126), packed, 1, None, rows, "fp32")
+    want, mag = orc.matvec_f64(x, codes, scales)
+    check(y[:, :15], want[:, :15], mag[:, :15], cols, "fp32")
+
+
 def test_special_values_reach_their_token_only():
     packed, codes, scales = random_weights(1, 32, 256, 8)
     codes_used = codes[0]
