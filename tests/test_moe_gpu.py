@@ -450,6 +450,71 @@ def test_two_captured_sorts_with_workspaces_of_their_own_on_two_streams():
             assert np.array_equal(got.cpu().numpy(), want.reshape(-1))
 
 
+@pytest.mark.parametrize("tokens", [300, 2100])            # sorted by one launch and by two
+def test_a_captured_chain_replayed_on_other_routings(tokens):
+    """Sort, gathered conversions, weighted sum and its gradient in one graph, captured on a side stream; every replay reads
+    what its inputs hold then, and two graphs with buffers of their own run side by side."""
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    top_k, experts, cols = 3, 10, 224
+    rows = B.mxfp8_moe_rows(tokens, top_k, experts)
+
+    def buffers():
+        i32 = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")
+        f = lambda *n, t=torch.float32: torch.zeros(n, dtype=t, device="cuda")
+        return dict(ids=i32(tokens, top_k), x=f(tokens, cols, t=torch.bfloat16), w=f(tokens, top_k), dy=f(tokens, cols), h=f(rows, cols, t=torch.bfloat16),
+                    off=i32(experts + 1), row_of=i32(tokens, top_k), slot_of=i32(rows), y=f(tokens, cols),
+                    d_h=f(rows, cols, t=torch.bfloat16), d_w=f(tokens, top_k),
+                    ws=torch.zeros(max(B.mxfp8_moe_sort_ws_bytes(tokens, top_k, experts), 16), dtype=torch.uint8, device="cuda"),
+                    fwd=[t.zero_() if t is not None else None for t in B.alloc_quantize_outputs(rows, cols, B.BOTH, B.SF_SWIZZLED)],
+                    bwd=[t.zero_() if t is not None else None for t in B.alloc_quantize_outputs(rows, cols, B.ROW, B.SF_SWIZZLED)])
+
+    def chain(b):
+        B.mxfp8_moe_sort(b["ids"], experts, b["off"], b["row_of"], b["slot_of"], b["ws"])
+        B.mxfp8_moe_dispatch_quantize(b["x"], b["slot_of"], top_k, None, b["off"], B.BOTH, B.RULE_PAPER, B.E4M3, *b["fwd"], B.SF_SWIZZLED)
+        B.mxfp8_moe_combine(b["h"], b["row_of"], b["w"], b["y"])
+        B.mxfp8_moe_combine_grad(b["dy"], b["h"], b["row_of"], b["slot_of"], b["w"], b["off"], b["d_h"], b["d_w"])
+        B.mxfp8_moe_dispatch_quantize(b["dy"], b["slot_of"], top_k, b["w"], b["off"], B.ROW, B.RULE_OCP, B.E5M2, *b["bwd"], B.SF_SWIZZLED)
+
+    def fill(b, seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        b["ids"].copy_(dev(routing(tokens, top_k, experts, seed, "holes")))
+        for name in ("x", "w", "dy", "h"):
+            b[name].copy_(torch.randn(b[name].shape, generator=g, device="cuda"))
+
+    def outputs(b):
+        used = int(b["off"][-1])
+        tensors = [b["off"], b["row_of"], b["slot_of"], b["y"], b["d_h"][:used], b["d_w"], b["fwd"][0][:used], b["fwd"][2][:used], b["bwd"][0][:used]]
+        scales = [b[n][1].view(-1, cols // 32 + (-(cols // 32)) % 4, 128)[:used // 128] for n in ("fwd", "bwd")]
+        return [t.clone() for t in tensors + scales]
+
+    plain, graphs, streams = buffers(), [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        b = buffers()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            chain(b)                                       # outside the capture first
+            s.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=s):
+                chain(b)
+        graphs.append((g, b))
+    for seed in range(4):
+        for i, (_, b) in enumerate(graphs):
+            fill(b, 10 * seed + i)
+        torch.cuda.synchronize()
+        for s, (g, _) in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for i, (_, b) in enumerate(graphs):
+            fill(plain, 10 * seed + i)
+            chain(plain)
+            for got, want in zip(outputs(b), outputs(plain)):
+                assert torch.equal(got, want)
+    assert B.mxfp8_device_status() == 0
+
+
 @pytest.mark.parametrize("backward", [False, True])
 def test_a_layer_of_experts_end_to_end(backward):
     """Sort, dispatch, the grouped products and the way back, as a layer uses them, against the same layer in 64 bits on the
