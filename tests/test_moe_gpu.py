@@ -178,6 +178,27 @@ def test_dispatch_of_special_values(dtype):
     run_dispatch(x, dtype, routing(200, 2, 6, 5, "holes"), 6, None, 3, 0, orc.E4M3, 1)
 
 
+@pytest.mark.parametrize("elem", [orc.E4M3, orc.E5M2, orc.E2M3, orc.E3M2, orc.E2M1])
+@pytest.mark.parametrize("orientation", [1, 2, 3])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_dispatch_of_the_whole_range(elem, orientation, dtype):
+    """Blocks of subnormals, of the largest values, of zeros of both signs, single Inf and NaN; products that round, underflow
+    and overflow."""
+    rng = np.random.default_rng(7)
+    tokens, cols = 150, 320
+    x = rng.standard_normal((tokens, cols)) * np.exp2(rng.integers(-149, 127, (tokens, 1)).astype(np.float64))
+    x[rng.random((tokens, cols)) < 0.05] *= -0.0
+    x[10:14], x[20, ::2], x[21] = 0.0, -0.0, np.finfo(np.float32).max
+    x[22, 64:96], x[23] = -3.3e38, np.float32(1e-45)
+    x[30, 17], x[31, 40], x[31, 300], x[32, 0] = np.nan, np.inf, -np.inf, np.inf
+    x = x.astype(np.float32)
+    w = (rng.standard_normal((tokens, 2)) * np.exp2(rng.integers(-30, 30, (tokens, 2)))).astype(np.float32)
+    w[40], w[41], w[42] = 0.0, -0.0, 2.0 ** -126
+    for weights in (None, w):
+        with np.errstate(over="ignore", invalid="ignore", under="ignore"):
+            run_dispatch(x, dtype, routing(tokens, 2, 5, 6, "holes"), 5, weights, orientation, orientation & 1, elem, 1)
+
+
 def test_dispatch_equals_two_steps_on_a_batch_that_uses_the_tile_counter():
     """Large enough for several tiles per CTA: the same bytes as gathering first and mxfp8_quantize after it."""
     import torch
