@@ -14,10 +14,11 @@
 //   columns: lane l owns 8 bytes of every row, as in the fast path; the 32 rows stay in registers for the conversion
 //   cast   : products of two elements per instruction
 // Measured at 53248 x 2048 BF16 rows of 8192 tokens, top-6, with the HBM time of the tokens read once and the outputs written:
-// 38 us for the row-blocked copy (22), 39 us by columns (22), 57 us for both (39), 66 us for both with weights; mxfp8_quantize
+// 38 us for the row-blocked copy (22), 37 us by columns (22), 53 us for both (39), 63 us for both with weights; mxfp8_quantize
 // of the same rows already sorted takes 88 us for both.  6272 x 4096 FP32 rows of 2999 tokens, weighted, both: 27 us (15).
-// From BF16 62 % of the cycles issue to the integer pipe, the busiest.  One slab per warp instead of two, with 16 warps on a
-// multiprocessor instead of 12: 56 us for both, but 43 us by columns; 20 warps spill (66 us).
+// From BF16 62 % of the cycles issue to the integer pipe, the busiest, and L2 moves 8.3 TB/s (the six reads of every token and
+// the outputs).  One slab per warp instead of two, with 16 warps on a multiprocessor instead of 12, took 10 % more by columns and
+// 2 % less for both; 20 warps spill.
 #include "quantize_tma_kernel.cuh"
 
 namespace mxfp8 {
@@ -54,17 +55,24 @@ __device__ __forceinline__ uint32_t weigh_pair(uint32_t w, float f)
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// 8 bytes of row j of a slab that belong to this lane / 16-byte piece c of row r
-__device__ __forceinline__ uint32_t lane_place(int j, int lane) { return j * T_BYTES + ((((lane >> 1) ^ (j & 15)) << 4) | ((lane & 1) << 3)); }
-__device__ __forceinline__ uint32_t piece_place(int r, int c) { return r * T_BYTES + ((c ^ (r & 15)) << 4); }
+// A slab lies at a multiple of 256 bytes of shared memory, so that the place of a piece is an exclusive-or of an address that
+// the lane computes once with a constant.
+template <typename T> __device__ __forceinline__ T& shared_at(uint32_t address) { return *static_cast<T*>(__cvta_shared_to_generic(address)); }
+// The 8 bytes of row j that belong to this lane, from own = own_bytes(slab, lane)
+__device__ __forceinline__ uint32_t own_bytes(uint32_t slab, int lane) { return slab | (lane >> 1) << 4 | (lane & 1) << 3; }
+__device__ __forceinline__ uint32_t in_row(uint32_t own, int j) { return (own ^ (j & 15) << 4) + j * T_BYTES; }
+// Piece c of this lane's row, from row = own_row(slab, lane)
+__device__ __forceinline__ uint32_t own_row(uint32_t slab, int lane) { return slab + lane * T_BYTES + (lane & 15) * 16; }
+__device__ __forceinline__ uint32_t piece(uint32_t row, int c) { return row ^ c << 4; }
 
 // First walk: row `lane` of the slab is weighted in place and its block maxima become scale bytes (staged) and factors 1/X
 // (in `inv`, four per row).  Returns whether a maximum is Inf (NaN elements do not enter it).
 template <int DTYPE, int ELEM, bool DO_ROW>
-__device__ __forceinline__ bool walk_row(uint8_t* slab, float* inv, float weight, bool weighted, uint8_t* my_scales, int lane, uint32_t rule_offset)
+__device__ __forceinline__ bool walk_row(uint32_t slab, float* inv, float weight, bool weighted, uint8_t* my_scales, int lane, uint32_t rule_offset)
 {
     constexpr bool BF = (DTYPE == MXFP8_BF16);
     constexpr int NKB = BF ? 4 : 2, PIECES = 16 / NKB;       // blocks of the row, pieces of a block
+    const uint32_t row = own_row(slab, lane);
     uint32_t top[NKB];
 #pragma unroll
     for (int b = 0; b < NKB; ++b) {
@@ -72,8 +80,8 @@ __device__ __forceinline__ bool walk_row(uint8_t* slab, float* inv, float weight
         float f = 0.f;
 #pragma unroll
         for (int c = 0; c < PIECES; ++c) {
-            uint4* at = reinterpret_cast<uint4*>(slab + piece_place(lane, b * PIECES + c));
-            uint4 v = *at;
+            uint4& at = shared_at<uint4>(piece(row, b * PIECES + c));
+            uint4 v = at;
             if (weighted) {
                 if constexpr (BF) {
                     v.x = weigh_pair(v.x, weight); v.y = weigh_pair(v.y, weight);
@@ -84,7 +92,7 @@ __device__ __forceinline__ bool walk_row(uint8_t* slab, float* inv, float weight
                     const float2 hi = mul2(make_float2(__uint_as_float(v.z), __uint_as_float(v.w)), w2);
                     v = make_uint4(__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x), __float_as_uint(hi.y));
                 }
-                *at = v;
+                at = v;
             }
             if constexpr (!DO_ROW) continue;
             if constexpr (BF) m = max_magnitude2(max_magnitude2(max_magnitude2(max_magnitude2(m, v.x), v.y), v.z), v.w);
@@ -110,8 +118,10 @@ __device__ __forceinline__ bool walk_row(uint8_t* slab, float* inv, float weight
     }
 }
 
-// This lane's VEC elements of a row times the factors, as codes
-template <int ELEM, int VEC>
+// This lane's VEC elements of a row times the factors, as codes.  Both copies together push the tokens out of L2 before their
+// last expert has read them, unless the codes leave first: 8192 tokens' 53 us in place of 57, 16384 tokens' 126 in place of 137
+// (FP32 187, 201), 1024 tokens' 13.2, 14.9; one copy alone is 2 % faster without (38.1 us, 38.9).
+template <int ELEM, int VEC, bool FIRST_OUT>
 __device__ __forceinline__ void store_codes(uint8_t* to, const float2 (&x)[VEC / 2], const float2 (&f)[VEC / 2], int lane)
 {
     constexpr bool SUB = (ELEM != MXFP8_E4M3 && ELEM != MXFP8_E5M2);
@@ -126,19 +136,21 @@ __device__ __forceinline__ void store_codes(uint8_t* to, const float2 (&x)[VEC /
                 : "=r"(c) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
         else c = cvt_fp8x4<ELEM>(a.x, a.y, b.x, b.y);
         if constexpr (SUB) c = pack_slot<ELEM, VEC>(c, lane);
-        *reinterpret_cast<uint32_t*>(to) = c;
+        if constexpr (FIRST_OUT) __stcs(reinterpret_cast<uint32_t*>(to), c);
+        else *reinterpret_cast<uint32_t*>(to) = c;
     } else {
         const float2 a = mul2(x[0], f[0]);
         uint32_t c = cvt_fp8x2<ELEM>(a.x, a.y);
         if constexpr (SUB) c = pack_slot<ELEM, VEC>(c, lane);
-        *reinterpret_cast<uint16_t*>(to) = (uint16_t)c;
+        if constexpr (FIRST_OUT) __stcs(reinterpret_cast<uint16_t*>(to), (uint16_t)c);
+        else *reinterpret_cast<uint16_t*>(to) = (uint16_t)c;
     }
 }
 
 // One slab whose columns all lie inside the tensor.  Returns true, with nothing stored but staged scale bytes, when an Inf
 // takes part (or a whole column of NaN); the slab then holds the weighted rows.
 template <int DTYPE, int ELEM, bool DO_ROW, bool DO_COL>
-__device__ __forceinline__ bool convert_slab(uint8_t* slab, float* inv, uint8_t* my_qrow, uint8_t* my_qcol, uint32_t pitch, uint8_t* my_row_scales,
+__device__ __forceinline__ bool convert_slab(uint32_t slab, float* inv, uint8_t* my_qrow, uint8_t* my_qcol, uint32_t pitch, uint8_t* my_row_scales,
                                              uint8_t* my_sm_col, float weight, bool weighted, int lane, uint32_t rule_offset)
 {
     constexpr bool BF = (DTYPE == MXFP8_BF16);
@@ -148,6 +160,7 @@ __device__ __forceinline__ bool convert_slab(uint8_t* slab, float* inv, uint8_t*
         special = walk_row<DTYPE, ELEM, DO_ROW>(slab, inv, weight, weighted, my_row_scales, lane, rule_offset);
         __syncwarp();
     }
+    const uint32_t own = own_bytes(slab, lane);
     uint2 raw[DO_COL ? 32 : 1];
     float2 col[VEC / 2];
     if constexpr (DO_COL) {
@@ -156,7 +169,7 @@ __device__ __forceinline__ bool convert_slab(uint8_t* slab, float* inv, uint8_t*
             uint32_t m0 = 0u, m1 = 0u;
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                raw[j] = *reinterpret_cast<const uint2*>(slab + lane_place(j, lane));
+                raw[j] = shared_at<const uint2>(in_row(own, j));
                 m0 = max_magnitude2(m0, raw[j].x);
                 m1 = max_magnitude2(m1, raw[j].y);
             }
@@ -166,7 +179,7 @@ __device__ __forceinline__ bool convert_slab(uint8_t* slab, float* inv, uint8_t*
             float m0 = 0.f, m1 = 0.f;
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
-                raw[j] = *reinterpret_cast<const uint2*>(slab + lane_place(j, lane));
+                raw[j] = shared_at<const uint2>(in_row(own, j));
                 m0 = fmaxf(m0, fabsf(__uint_as_float(raw[j].x)));
                 m1 = fmaxf(m1, fabsf(__uint_as_float(raw[j].y)));
             }
@@ -188,7 +201,7 @@ __device__ __forceinline__ bool convert_slab(uint8_t* slab, float* inv, uint8_t*
     for (int j = 0; j < 32; ++j) {
         uint2 w;
         if constexpr (DO_COL) w = raw[j];
-        else w = *reinterpret_cast<const uint2*>(slab + lane_place(j, lane));
+        else w = shared_at<const uint2>(in_row(own, j));
         float2 x[VEC / 2];
         if constexpr (BF) {
             x[0] = bf16_pair(w.x);
@@ -199,20 +212,21 @@ __device__ __forceinline__ bool convert_slab(uint8_t* slab, float* inv, uint8_t*
             float2 f[VEC / 2];
 #pragma unroll
             for (int i = 0; i < VEC / 2; ++i) f[i] = make_float2(r, r);
-            store_codes<ELEM, VEC>(my_qrow + (uint64_t)j * pitch, x, f, lane);
+            store_codes<ELEM, VEC, DO_ROW && DO_COL>(my_qrow + (uint64_t)j * pitch, x, f, lane);
         }
-        if constexpr (DO_COL) store_codes<ELEM, VEC>(my_qcol + (uint64_t)j * pitch, x, col, lane);
+        if constexpr (DO_COL) store_codes<ELEM, VEC, DO_ROW && DO_COL>(my_qcol + (uint64_t)j * pitch, x, col, lane);
     }
     return false;
 }
 
 // The slab back in plain order, for the careful path
-__device__ __noinline__ void plain_order(uint8_t* slab, int lane)
+__device__ __noinline__ void plain_order(uint32_t slab, int lane)
 {
+    const uint32_t own = own_bytes(slab, lane);
     for (int j = 0; j < 32; ++j) {
-        const uint2 v = *reinterpret_cast<const uint2*>(slab + lane_place(j, lane));
+        const uint2 v = shared_at<const uint2>(in_row(own, j));
         __syncwarp();
-        *reinterpret_cast<uint2*>(slab + j * T_BYTES + lane * 8) = v;
+        shared_at<uint2>(slab + j * T_BYTES + lane * 8) = v;
         __syncwarp();
     }
 }
@@ -227,14 +241,14 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
     constexpr int T_COLS = T_BYTES / ESZ;           // 128 or 64
     constexpr int LPB = 32 / VEC;                   // lanes per row block: 8 or 16
 
-    extern __shared__ __align__(128) uint8_t smem[];
-    uint8_t* sm_scales = smem + RING * IN_BYTES;    // STAGES x (row scales + column scales of one tile, 512 bytes each)
+    extern __shared__ __align__(256) uint8_t gather_smem[];
+    uint8_t* sm_scales = gather_smem + RING * IN_BYTES;    // STAGES x (row scales + column scales of one tile, 512 bytes each)
     float* row_inv = reinterpret_cast<float*>(sm_scales + STAGES * 1024) + (threadIdx.x >> 5) * 128;      // this warp's row factors, four per row
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;   // warp = 32-row slab of the tile
     const QParams& p = batch.t[0];
     const uint32_t rule_offset = (p.rule == MXFP8_RULE_PAPER) ? paper_offset<ELEM>() : 0u;
-    uint8_t* my_slabs = smem + warp * SLAB_BYTES;   // + IN_BYTES for the ring's second slot
+    const uint32_t my_slabs = smem_addr(gather_smem) + warp * SLAB_BYTES;   // + IN_BYTES for the ring's second slot
 
     // rows in use: whole 128-row tiles by construction of the sort; anything else is reported and nothing is stored
     const int used = *batch.used_rows;
@@ -263,14 +277,15 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
         const bool col_ok = col < p.cols;
         const uint8_t* src = static_cast<const uint8_t*>(batch.gather_src) + (col_ok ? col : 0) * ESZ;
         const uint32_t src_pitch = (uint32_t)p.cols * ESZ;
-        const uint32_t to = smem_addr(my_slabs + buf * IN_BYTES);
+        const int upper = lane >> 4;
+        const uint32_t to = my_slabs + buf * IN_BYTES + upper * T_BYTES + ((lane & 15) ^ upper) * 16;      // its piece of row `upper`
         if (slot < 0) token = -1;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int tk = __shfl_sync(0xFFFFFFFFu, token, 2 * i + (lane >> 4));
+            const int tk = __shfl_sync(0xFFFFFFFFu, token, 2 * i + upper);
             const uint32_t bytes = (tk >= 0 && col_ok) ? 16u : 0u;               // 0: the 16 bytes are filled with zeros
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
-                         ::"r"(to + piece_place(2 * i + (lane >> 4), lane & 15)), "l"(src + (uint64_t)(uint32_t)max(tk, 0) * src_pitch), "r"(bytes) : "memory");
+                         ::"r"((to ^ (2 * i & 15) << 4) + 2 * i * T_BYTES), "l"(src + (uint64_t)(uint32_t)max(tk, 0) * src_pitch), "r"(bytes) : "memory");
         }
     };
     auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
@@ -312,7 +327,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
 
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         __syncwarp();
-        uint8_t* slab = my_slabs + buf * IN_BYTES;
+        const uint32_t slab = my_slabs + buf * IN_BYTES;
         const bool weighted = batch.slot_weights != nullptr;
         const int64_t my_col = gcol0 + lane * VEC;
         const bool col_ok = my_col < p.cols;                                         // cols % 16 == 0: a lane's bytes are all in or all out
@@ -331,7 +346,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch)
         }
         if (special) {
             plain_order(slab, lane);
-            slab_careful<DTYPE, ELEM, DO_ROW, DO_COL, false>(slab + lane * 8, my_qrow, my_qcol, pitch, sm_row + warp * 4 + lane / LPB, my_sm_col, lane,
+            slab_careful<DTYPE, ELEM, DO_ROW, DO_COL, false>(gather_smem + warp * SLAB_BYTES + buf * IN_BYTES + lane * 8, my_qrow, my_qcol, pitch, sm_row + warp * 4 + lane / LPB, my_sm_col, lane,
                                                              rule_offset, 32, col_ok);
         }
         __syncwarp();
