@@ -231,6 +231,37 @@ def test_dispatch_equals_two_steps_on_a_batch_that_uses_the_tile_counter():
         assert torch.equal(per.reshape(-1), want[3])
 
 
+@pytest.mark.parametrize("dtype,tokens,cols,orientation", [
+    ("bf16", 9001, 4128, 3), ("bf16", 9001, 4128, 1), ("fp32", 4500, 4160, 3), ("fp32", 70001, 256, 2), ("bf16", 100001, 384, 3)])
+def test_dispatch_of_tokens_that_do_not_stay_in_l2(dtype, tokens, cols, orientation):
+    """Sources that are walked in groups of columns (uneven ones, single ones): the same bytes as gathering first."""
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    top_k, experts = 2, 5
+    off, _, slot_of = gpu_sort(routing(tokens, top_k, experts, 2, "holes"), experts)
+    rows, used = slot_of.numel(), int(off[-1])
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(tokens, cols, generator=g, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    w = torch.randn(tokens, top_k, generator=g, device="cuda")
+    slots = slot_of[:used].long()
+    for weights in (None, w):
+        y = x[slots.clamp(min=0) // top_k]
+        if weights is not None:
+            y = (y.float() * weights.reshape(-1)[slots.clamp(min=0)].unsqueeze(1)).to(x.dtype)
+        y = torch.where((slots >= 0).unsqueeze(1), y, torch.zeros((), dtype=y.dtype, device="cuda"))
+        want = B.alloc_quantize_outputs(used, cols, orientation, B.SF_LINEAR)
+        B.mxfp8_quantize(y, orientation, B.RULE_PAPER, B.E4M3, *want, B.SF_LINEAR)
+        got = B.alloc_quantize_outputs(rows, cols, orientation, B.SF_LINEAR)
+        for q in got:
+            if q is not None:
+                q.fill_(0xA5)
+        B.mxfp8_moe_dispatch_quantize(x, slot_of, top_k, weights, off, orientation, B.RULE_PAPER, B.E4M3, *got, B.SF_LINEAR)
+        assert B.mxfp8_device_status() == 0
+        for q, ref in zip(got, want):
+            if q is not None:
+                assert torch.equal(q.reshape(-1)[:ref.numel()], ref.reshape(-1)) and (q.reshape(-1)[ref.numel():] == 0xA5).all()
+
+
 def test_bad_device_arrays_are_reported():
     import torch
     from paper_2506_08027_b200 import binding as B
