@@ -537,21 +537,26 @@ def mxfp8_moe_combine(src: torch.Tensor, row_of: torch.Tensor, weights, dst: tor
                                    _dtype_code(dst), st), "mxfp8_moe_combine")
 
 
-def mxfp8_moe_combine_grad(dy: torch.Tensor, src: torch.Tensor, row_of: torch.Tensor, slot_of: torch.Tensor, weights, group_offsets: torch.Tensor,
-                           d_src, d_weights, stream=None) -> None:
-    """dy: [tokens, cols]; src, d_src: [rows, cols]; row_of, weights, d_weights: [tokens, top_k]; d_src or d_weights may be None."""
+def mxfp8_moe_combine_grad(dy: torch.Tensor, src, row_of: torch.Tensor, slot_of, weights, group_offsets, d_src, d_weights, stream=None) -> None:
+    """dy: [tokens, cols]; src, d_src: [rows, cols]; row_of, weights, d_weights: [tokens, top_k]; d_src or d_weights may be None.  Without d_weights
+    src may be None, without d_src slot_of and group_offsets may."""
     tokens, cols = dy.shape
-    rows = src.shape[0]
+    sorted_rows = src if src is not None else d_src
+    if sorted_rows is None:
+        raise ValueError("src or d_src is needed")
+    rows = sorted_rows.shape[0]
     _int32(row_of, slot_of, group_offsets)
     st = _stream_for(stream, dy, src, row_of, slot_of, weights, group_offsets, d_src, d_weights)
     top_k = row_of.shape[1]
     _float_weights(weights, tokens, top_k)
     _float_weights(d_weights, tokens, top_k)
-    if row_of.shape[0] != tokens or src.shape[1] != cols or slot_of.numel() != rows or (d_src is not None and (d_src.shape != src.shape or d_src.dtype != src.dtype)):
+    if row_of.shape[0] != tokens or sorted_rows.shape[1] != cols or (slot_of is not None and slot_of.numel() != rows) or \
+            (d_src is not None and (d_src.shape != sorted_rows.shape or d_src.dtype != sorted_rows.dtype)):
         raise ValueError("shapes or types of dy, src, d_src, row_of and slot_of do not agree")
-    _check(lib().mxfp8_moe_combine_grad(_ptr(dy), _dtype_code(dy), tokens, cols, _ptr(src), _dtype_code(src), rows, _ptr(row_of), _ptr(slot_of), top_k,
-                                        _ptr(weights), _ptr(group_offsets), group_offsets.numel() - 1, _ptr(d_src), _ptr(d_weights),
-                                        st), "mxfp8_moe_combine_grad")
+    num_groups = 1 if group_offsets is None else group_offsets.numel() - 1
+    _check(lib().mxfp8_moe_combine_grad(_ptr(dy), _dtype_code(dy), tokens, cols, _ptr(src), _dtype_code(sorted_rows), rows, _ptr(row_of), _ptr(slot_of), top_k,
+                                        _ptr(weights), _ptr(group_offsets), num_groups, _ptr(d_src), _ptr(d_weights), st),
+           "mxfp8_moe_combine_grad")
 
 
 def mxfp8_e2m1_packed_bytes(num_matrices: int, rows: int, cols: int) -> int:

@@ -1,0 +1,37 @@
+"""The token-movement calls where tests/test_moe_gpu.py does not go: arrays left out, and batches of more than a million slots."""
+import numpy as np
+import pytest
+
+import oracle as orc
+from test_moe_gpu import dev, gpu_sort, routing
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dy,src", [("bf16", "bf16"), ("fp32", "bf16"), ("bf16", "fp32")])
+def test_either_gradient_alone_through_the_binding(dy, src):
+    """The arrays that only the other gradient reads are None; the same bits as with all of them."""
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    kinds = {"bf16": torch.bfloat16, "fp32": torch.float32}
+    tokens, top_k, experts, cols = 150, 3, 5, 264
+    off, row_of, slot_of = gpu_sort(routing(tokens, top_k, experts, 3, "holes"), experts, spare=128)
+    rows = slot_of.numel()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    y = torch.randn(rows, cols, generator=g, device="cuda").to(kinds[src])
+    d = torch.randn(tokens, cols, generator=g, device="cuda").to(kinds[dy])
+    w = torch.randn(tokens, top_k, generator=g, device="cuda")
+    both = torch.full_like(y, 3.0), torch.full((tokens, top_k), 3.0, device="cuda")
+    B.mxfp8_moe_combine_grad(d, y, row_of, slot_of, w, off, *both)
+    rows_only, weights_only = torch.full_like(y, 3.0), torch.full((tokens, top_k), 3.0, device="cuda")
+    B.mxfp8_moe_combine_grad(d, None, row_of, slot_of, w, off, rows_only, None)
+    B.mxfp8_moe_combine_grad(d, y, row_of, None, w, None, None, weights_only)
+    assert B.mxfp8_device_status() == 0
+    assert torch.equal(rows_only, both[0]) and torch.equal(weights_only, both[1])
+    for missing in ((None, off), (slot_of, None)):
+        with pytest.raises(B.Mxfp8Error) as e:
+            B.mxfp8_moe_combine_grad(d, None, row_of, missing[0], w, missing[1], rows_only, None)
+        assert e.value.status == B.ERR_NULL
+    with pytest.raises(B.Mxfp8Error) as e:
+        B.mxfp8_moe_combine_grad(d, None, row_of, slot_of, w, off, rows_only, weights_only)
+    assert e.value.status == B.ERR_NULL
