@@ -196,20 +196,10 @@ struct QuantizeItem {
     int64_t rows, cols;
     void *q_row, *s_row, *q_col, *s_col;
 };
-// A gather ahead of the conversion (mxfp8_moe_dispatch_quantize): row r of the converted tensor is row slot_of[r] / top_k of
-// the source, times weights[slot_of[r]] (weights may be null), or zero where slot_of[r] is -1; *used rows exist.
-struct GatherArgs {
-    int64_t tokens;
-    const int32_t* slot_of;
-    const float* weights;
-    const int32_t* used;
-    int top_k;
-};
 int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int orientation, int scale_rule, int elem,
                        int sf_layout, cudaStream_t stream, bool emulate = false, int act = MXFP8_ACT_NONE,
                        const float* rstd = nullptr, const void* gamma = nullptr, bool gated = false,
-                       const float* mean = nullptr, const void* beta = nullptr, const void* second_src = nullptr,
-                       const GatherArgs* gather = nullptr);
+                       const float* mean = nullptr, const void* beta = nullptr, const void* second_src = nullptr);
 int quantize_read_and_clear_status();
 
 // Device status word (bounded waits report here); defined in gemm.cu.

@@ -35,6 +35,16 @@ struct Walk {
     uint32_t group, group_magic, last, last_magic;     // tile columns of a group and of the last one
     int groups;
 };
+struct GatherArgs {
+    QParams t;                                // the converted tensor [rows, cols]
+    const void* src;                          // [tokens, cols]
+    const int32_t* slot_of;                   // slot of every row, -1: none
+    const float* weights;                     // per slot, or null
+    const int32_t* used;                      // device: rows in use
+    int* status;                              // reports a bad array
+    uint32_t top_k, top_k_magic, slots;       // slots per token and of all tokens
+    int tiles;                                // of all rows
+};
 constexpr int SLAB_BYTES = 32 * T_BYTES;
 // Scale bytes of the last eight tiles.  Warp i mod 4 stores those of the CTA's i-th tile once it has converted its slab of
 // tile i + 1, by when the other three have mostly announced their slabs of tile i and need not be waited for (waiting right
@@ -242,9 +252,56 @@ __device__ __noinline__ void plain_order(uint32_t slab, int lane)
     }
 }
 
+// A quarter of the scale bytes of one tile, row and column `tid` of it, leaves from the staging arrays (both in the order of a
+// swizzled atom).  A tile's rows are all inside the tensor, its columns may not be.  (The fast path's kernel has such code inside:
+// shared between the two as a function, it cost that kernel up to 10 %, 15.3 against 16.7 us for both copies of 4096 x 4096 BF16.)
+template <bool BF, bool DO_ROW, bool DO_COL>
+__device__ __forceinline__ void store_scales(const QParams& p, int tile_x, int tile_y, const uint8_t* sm_row, const uint8_t* sm_col, int tid, int lane, int quarter)
+{
+    constexpr int T_COLS = T_BYTES / (BF ? 2 : 4), NKB = T_COLS / 32;
+    const int64_t gcol0 = (int64_t)tile_x * T_COLS;
+    if (BF && p.sf_layout == MXFP8_SF_SWIZZLED && gcol0 + T_COLS <= p.cols) {      // exactly one atom per orientation, 16 bytes per lane
+        if (DO_ROW && quarter == 0) {
+            const int64_t atoms_k = ((p.cols >> 5) + 3) >> 2;
+            *reinterpret_cast<uint4*>(p.s_row + ((int64_t)tile_y * atoms_k + tile_x) * 512 + lane * 16) = *reinterpret_cast<const uint4*>(sm_row + lane * 16);
+        }
+        if (DO_COL && quarter == (DO_ROW ? 1 : 0))
+            *reinterpret_cast<uint4*>(p.s_col + ((int64_t)tile_x * (p.rows >> 7) + tile_y) * 512 + lane * 16) = *reinterpret_cast<const uint4*>(sm_col + lane * 16);
+        return;
+    }
+    if constexpr (DO_ROW) {
+        const int64_t r = (int64_t)tile_y * T_ROWS + tid, blocks = p.cols >> 5, kb0 = (int64_t)tile_x * NKB;
+        const int nkb = (int)min((int64_t)NKB, blocks - kb0);
+        uint32_t v = *reinterpret_cast<const uint32_t*>(sm_row + stage_offset(tid));
+        if (nkb < 4) v &= (1u << (8 * nkb)) - 1u;          // bytes behind the last block are zero
+        if (p.sf_layout == MXFP8_SF_SWIZZLED) {
+            // a 64-column FP32 tile owns half of the atom's four blocks; without a right neighbour it clears that half too
+            uint8_t* d = p.s_row + ((int64_t)tile_y * ((blocks + 3) >> 2) + (kb0 >> 2)) * 512 + stage_offset(tid) + (kb0 & 3);
+            if (NKB == 4 || ((kb0 & 3) == 0 && kb0 + NKB >= blocks)) *reinterpret_cast<uint32_t*>(d) = v;
+            else *reinterpret_cast<uint16_t*>(d) = (uint16_t)v;
+        } else {
+            uint8_t* d = p.s_row + r * blocks + kb0;
+            for (int kb = 0; kb < nkb; ++kb) d[kb] = (uint8_t)(v >> (8 * kb));
+        }
+    }
+    if (DO_COL && tid < T_COLS) {
+        const int64_t c = gcol0 + tid, atoms_r = p.rows >> 7;
+        const uint32_t v = c < p.cols ? *reinterpret_cast<const uint32_t*>(sm_col + stage_offset(tid)) : 0u;
+        if (p.sf_layout == MXFP8_SF_SWIZZLED) {
+            const int64_t padded_cols = ((p.cols + 127) >> 7) << 7;
+            *reinterpret_cast<uint32_t*>(p.s_col + ((c >> 7) * atoms_r + tile_y) * 512 + (c & 31) * 16 + ((c >> 5) & 3) * 4) = v;
+            // columns of the atom that no 64-column FP32 tile covers
+            if (T_COLS == 64 && tile_x == p.tiles_x - 1 && c + 64 < padded_cols)
+                *reinterpret_cast<uint32_t*>(p.s_col + (((c + 64) >> 7) * atoms_r + tile_y) * 512 + ((c + 64) & 31) * 16 + (((c + 64) >> 5) & 3) * 4) = 0u;
+        } else if (c < p.cols) {
+            for (int w = 0; w < 4; ++w) p.s_col[((int64_t)tile_y * 4 + w) * p.cols + c] = (uint8_t)(v >> (8 * w));
+        }
+    }
+}
+
 template <int DTYPE, int ELEM, bool DO_ROW, bool DO_COL, bool GROUPED>
 __global__ void __launch_bounds__(QT_THREADS, QT_CTAS_PER_SM)
-quantize_gather_kernel(const __grid_constant__ QBatch batch, const Walk walk)
+quantize_gather_kernel(const __grid_constant__ GatherArgs a, const Walk walk)
 {
     constexpr bool BF = (DTYPE == MXFP8_BF16);
     constexpr int VEC = BF ? 4 : 2;                 // elements per lane per row
@@ -257,15 +314,15 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch, const Walk walk)
     float* row_inv = reinterpret_cast<float*>(sm_scales + STAGES * 1024) + (threadIdx.x >> 5) * 128;      // this warp's row factors, four per row
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;   // warp = 32-row slab of the tile
-    const QParams& p = batch.t[0];
+    const QParams& p = a.t;
     const uint32_t rule_offset = (p.rule == MXFP8_RULE_PAPER) ? paper_offset<ELEM>() : 0u;
     const uint32_t my_slabs = smem_addr(gather_smem) + warp * SLAB_BYTES;   // + IN_BYTES for the ring's second slot
 
     // rows in use: whole 128-row tiles by construction of the sort; anything else is reported and nothing is stored
-    const int used = *batch.used_rows;
+    const int used = *a.used;
     int num_tiles = 0;
     if (used < 0 || used > p.rows || used % T_ROWS) {
-        if (tid == 0 && blockIdx.x == 0) atomicExch(batch.args_status, (int)MXFP8_ERR_DEVICE_ARGS);
+        if (tid == 0 && blockIdx.x == 0) atomicExch(a.status, (int)MXFP8_ERR_DEVICE_ARGS);
     } else num_tiles = (used / T_ROWS) * p.tiles_x;
 
     [[maybe_unused]] const uint32_t group = walk.group * (uint32_t)(num_tiles ? used / T_ROWS : 1);      // tiles of a whole group
@@ -283,21 +340,21 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch, const Walk walk)
     auto slot_in = [&](int t) {
         int lx, ly;
         locate(t, ly, lx);
-        return batch.slot_of[(int64_t)ly * T_ROWS + warp * 32 + lane];
+        return a.slot_of[(int64_t)ly * T_ROWS + warp * 32 + lane];
     };
     auto checked = [&](int slot) {
-        if ((uint32_t)slot < batch.slots) return slot;
-        if (slot != -1) atomicExch(batch.args_status, (int)MXFP8_ERR_DEVICE_ARGS);
+        if ((uint32_t)slot < a.slots) return slot;
+        if (slot != -1) atomicExch(a.status, (int)MXFP8_ERR_DEVICE_ARGS);
         return -1;
     };
     // this warp's slab of tile t -> ring slot buf: 16 copies of two rows; lane l carries 16 bytes of row l / 16 of each pair
     auto issue = [&](int t, int slot, int buf) {
         int lx, ly, token, rest;
         locate(t, ly, lx);
-        divmod(slot < 0 ? 0u : (uint32_t)slot, batch.top_k, batch.top_k_magic, token, rest);
+        divmod(slot < 0 ? 0u : (uint32_t)slot, a.top_k, a.top_k_magic, token, rest);
         const int64_t col = (int64_t)lx * T_COLS + (lane & 15) * (16 / ESZ);
         const bool col_ok = col < p.cols;
-        const uint8_t* src = static_cast<const uint8_t*>(batch.gather_src) + (col_ok ? col : 0) * ESZ;
+        const uint8_t* src = static_cast<const uint8_t*>(a.src) + (col_ok ? col : 0) * ESZ;
         const uint32_t src_pitch = (uint32_t)p.cols * ESZ;
         const int upper = lane >> 4;
         const uint32_t to = my_slabs + buf * IN_BYTES + upper * T_BYTES + ((lane & 15) ^ upper) * 16;      // its piece of row `upper`
@@ -311,7 +368,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch, const Walk walk)
         }
     };
     auto commit = [] { asm volatile("cp.async.commit_group;" ::: "memory"); };
-    auto weight_of = [&](int slot) { return (batch.slot_weights != nullptr && slot >= 0) ? batch.slot_weights[slot] : 0.f; };
+    auto weight_of = [&](int slot) { return (a.weights != nullptr && slot >= 0) ? a.weights[slot] : 0.f; };
     int next_slot = -1;                             // of this lane's row in the next tile
     float my_weight = 0.f;                          // of this lane's row in this tile (a row without a slot holds zeros and has the weight 0)
 #pragma unroll
@@ -331,8 +388,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch, const Walk walk)
         asm volatile("bar.sync %0, %1;" ::"r"(1 + i % STAGES), "n"(QT_THREADS) : "memory");
         const uint8_t* at = sm_scales + (i % STAGES) * 1024;
 #pragma unroll 1
-        for (int k = 0; k < QT_THREADS / 32; ++k)
-            store_scales<BF, DO_ROW, DO_COL, false>(p, x, y, at, at + 512, k * 32 + lane, lane, k);
+        for (int k = 0; k < QT_THREADS / 32; ++k) store_scales<BF, DO_ROW, DO_COL>(p, x, y, at, at + 512, k * 32 + lane, lane, k);
     };
     int it = 0, before_x = 0, before_y = 0;         // the tile before this one
     for (int tile = blockIdx.x; tile < num_tiles; tile += gridDim.x, ++it) {
@@ -350,7 +406,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch, const Walk walk)
         asm volatile("cp.async.wait_group 1;" ::: "memory");
         __syncwarp();
         const uint32_t slab = my_slabs + buf * IN_BYTES;
-        const bool weighted = batch.slot_weights != nullptr;
+        const bool weighted = a.weights != nullptr;
         const int64_t my_col = gcol0 + lane * VEC;
         const bool col_ok = my_col < p.cols;                                         // cols % 16 == 0: a lane's bytes are all in or all out
         uint8_t* my_qrow = p.q_row + ((grow0 + warp * 32) * p.cols + my_col);
@@ -389,7 +445,7 @@ quantize_gather_kernel(const __grid_constant__ QBatch batch, const Walk walk)
 }
 
 template <int DTYPE, int ELEM, bool R, bool C, bool GROUPED>
-cudaError_t launch_gather(const QBatch& p, const Walk& walk, cudaStream_t stream)
+cudaError_t launch_gather(const GatherArgs& a, const Walk& walk, cudaStream_t stream)
 {
     constexpr int SMEM = RING * IN_BYTES + STAGES * 1024 + QT_THREADS * 16;      // ring, scale staging, row factors
     auto kernel = quantize_gather_kernel<DTYPE, ELEM, R, C, GROUPED>;
@@ -399,41 +455,38 @@ cudaError_t launch_gather(const QBatch& p, const Walk& walk, cudaStream_t stream
     if (err != cudaSuccess) return err;
     const int sms = qt_sm_count();
     if (sms <= 0) return cudaErrorInvalidDevice;
-    const int tiles = p.tile_start[1], most = sms * QT_CTAS_PER_SM;
-    kernel<<<tiles < most ? tiles : most, QT_THREADS, SMEM, stream>>>(p, walk);
+    const int tiles = a.tiles, most = sms * QT_CTAS_PER_SM;
+    kernel<<<tiles < most ? tiles : most, QT_THREADS, SMEM, stream>>>(a, walk);
     count_launch(1);
     return cudaGetLastError();
 }
 template <int DTYPE, int ELEM, bool R, bool C>
-cudaError_t launch_gather(const QBatch& p, cudaStream_t stream)
+cudaError_t launch_gather(const GatherArgs& a, cudaStream_t stream)
 {
-    const int64_t strip = (int64_t)(p.slots / p.top_k) * T_BYTES;      // bytes of the tokens under one tile column
-    const uint32_t tiles_x = (uint32_t)p.t[0].tiles_x;
+    const int64_t strip = (int64_t)(a.slots / a.top_k) * T_BYTES;      // bytes of the tokens under one tile column
+    const uint32_t tiles_x = (uint32_t)a.t.tiles_x;
     Walk w{};
-    if (strip * tiles_x <= ONE_GROUP<R && C>) return launch_gather<DTYPE, ELEM, R, C, false>(p, w, stream);
+    if (strip * tiles_x <= ONE_GROUP<R && C>) return launch_gather<DTYPE, ELEM, R, C, false>(a, w, stream);
     const uint32_t fit = (uint32_t)(strip >= GROUP_BYTES ? 1 : GROUP_BYTES / strip), groups = (tiles_x + fit - 1) / fit;
     w.group = (tiles_x + groups - 1) / groups;
     w.groups = (int)((tiles_x + w.group - 1) / w.group);
     w.last = tiles_x - w.group * (uint32_t)(w.groups - 1);
     w.group_magic = div_magic(w.group);
     w.last_magic = div_magic(w.last);
-    return launch_gather<DTYPE, ELEM, R, C, true>(p, w, stream);
+    return launch_gather<DTYPE, ELEM, R, C, true>(a, w, stream);
 }
 template <int DTYPE, int ELEM>
-cudaError_t launch_gather_o(int orientation, const QBatch& p, cudaStream_t st)
+cudaError_t launch_gather_o(int orientation, const GatherArgs& a, cudaStream_t st)
 {
-    if (orientation == MXFP8_ROW) return launch_gather<DTYPE, ELEM, true, false>(p, st);
-    if (orientation == MXFP8_COL) return launch_gather<DTYPE, ELEM, false, true>(p, st);
-    return launch_gather<DTYPE, ELEM, true, true>(p, st);
+    if (orientation == MXFP8_ROW) return launch_gather<DTYPE, ELEM, true, false>(a, st);
+    if (orientation == MXFP8_COL) return launch_gather<DTYPE, ELEM, false, true>(a, st);
+    return launch_gather<DTYPE, ELEM, true, true>(a, st);
 }
 
-}  // namespace
-
-cudaError_t quantize_launch_gather(int elem, bool bf16_src, int orientation, const void* batch, cudaStream_t st)
+cudaError_t launch_gather_e(int elem, bool bf16_src, int orientation, const GatherArgs& a, cudaStream_t st)
 {
-    const QBatch& p = *static_cast<const QBatch*>(batch);
 #define MXFP8_GATHER_CASE(E) \
-    case E: return bf16_src ? launch_gather_o<MXFP8_BF16, E>(orientation, p, st) : launch_gather_o<MXFP8_FP32, E>(orientation, p, st);
+    case E: return bf16_src ? launch_gather_o<MXFP8_BF16, E>(orientation, a, st) : launch_gather_o<MXFP8_FP32, E>(orientation, a, st);
     switch (elem) {
         MXFP8_GATHER_CASE(MXFP8_E4M3)
         MXFP8_GATHER_CASE(MXFP8_E5M2)
@@ -445,6 +498,7 @@ cudaError_t quantize_launch_gather(int elem, bool bf16_src, int orientation, con
 #undef MXFP8_GATHER_CASE
 }
 
+}  // namespace
 }  // namespace mxfp8
 
 extern "C" int mxfp8_moe_dispatch_quantize(const void* src, int src_dtype, int64_t tokens, int64_t cols,
@@ -472,8 +526,22 @@ extern "C" int mxfp8_moe_dispatch_quantize(const void* src, int src_dtype, int64
     if ((orientation & MXFP8_COL) && (!aligned16(q_col) || !aligned16(s_col))) return MXFP8_ERR_ALIGN;
     if (tokens > 0x7F000000LL || tokens * top_k > 0x7F000000LL || cols > 0x3FFFFFFFLL) return MXFP8_ERR_UNSUPPORTED;      // 32-bit counters and pitches
     if (!quantize_tma_eligible(src_dtype, rows, cols)) return MXFP8_ERR_UNSUPPORTED;   // needs cols % 16 == 0
-    const QuantizeItem item{src, rows, cols, q_row, s_row, q_col, s_col};
-    const GatherArgs gather{tokens, slot_of, weights, group_offsets + num_groups, top_k};
-    return quantize_tma_batch(&item, 1, src_dtype, orientation, scale_rule, elem, sf_layout, static_cast<cudaStream_t>(stream), false, MXFP8_ACT_NONE,
-                              nullptr, nullptr, false, nullptr, nullptr, nullptr, &gather);
+    const uint32_t t_cols = src_dtype == MXFP8_BF16 ? 128 : 64;
+    GatherArgs a{};
+    QParams& q = a.t;
+    q.rows = rows; q.cols = cols; q.rule = scale_rule; q.sf_layout = sf_layout;
+    q.tiles_x = (int)((cols + t_cols - 1) / t_cols);
+    q.tiles_x_magic = div_magic((uint32_t)q.tiles_x);
+    q.tiles_y = (int)(rows / T_ROWS);
+    q.q_row = static_cast<uint8_t*>(q_row);
+    q.q_col = static_cast<uint8_t*>(q_col);
+    q.s_row = static_cast<uint8_t*>(s_row);
+    q.s_col = static_cast<uint8_t*>(s_col);
+    a.src = src; a.slot_of = slot_of; a.weights = weights; a.used = group_offsets + num_groups;
+    a.top_k = (uint32_t)top_k;
+    a.top_k_magic = div_magic(a.top_k);
+    a.slots = (uint32_t)(tokens * top_k);
+    a.tiles = q.tiles_x * q.tiles_y;                                     // fits: quantize_tma_eligible
+    if (!(a.status = device_status_word())) return MXFP8_ERR_CUDA;
+    return launch_gather_e(elem, src_dtype == MXFP8_BF16, orientation, a, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
 }

@@ -18,8 +18,6 @@ int quantize_read_and_clear_status()
 // defined in quantize_tma_fp6_fp4.cu (opaque pointers: the batch types live in an unnamed namespace)
 cudaError_t quantize_tma_launch_fp6_fp4(int elem, bool bf16_src, int orientation, bool emulate, const void* maps,
                                         const void* batch, cudaStream_t st);
-// defined in quantize_gather.cu
-cudaError_t quantize_launch_gather(int elem, bool bf16_src, int orientation, const void* batch, cudaStream_t st);
 
 namespace {
 
@@ -71,7 +69,7 @@ bool quantize_tma_eligible(int src_dtype, int64_t rows, int64_t cols)
 
 int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int orientation, int scale_rule, int elem,
                        int sf_layout, cudaStream_t stream, bool emulate, int act, const float* rstd, const void* gamma,
-                       bool gated, const float* mean, const void* beta, const void* second_src, const GatherArgs* gather)
+                       bool gated, const float* mean, const void* beta, const void* second_src)
 {
     if (count < 1 || count > QT_MAX_TENSORS) return MXFP8_ERR_UNSUPPORTED;
     const bool bf = src_dtype == MXFP8_BF16;
@@ -86,17 +84,6 @@ int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int 
     p.beta = beta;
     p.glu_cols = gated ? (int)items[0].cols : 0;     // gated: one tensor, source [rows, 2 * cols]
     p.up_map = second_src ? 1 : 0;                   // two sources of one shape: the second one rides in map 1
-    if (gather) {
-        if (count != 1 || gated || second_src) return MXFP8_ERR_UNSUPPORTED;
-        p.slot_of = gather->slot_of;
-        p.gather_src = items[0].src;
-        p.used_rows = gather->used;
-        p.slot_weights = gather->weights;
-        p.top_k = (uint32_t)gather->top_k;
-        p.top_k_magic = div_magic(p.top_k);
-        p.slots = (uint32_t)(gather->tokens * gather->top_k);
-        if (!(p.args_status = device_status_word())) return MXFP8_ERR_CUDA;
-    }
     int64_t tiles = 0;
     for (int i = 0; i < QT_MAX_TENSORS; ++i) {
         const QuantizeItem& it = items[i < count ? i : 0];
@@ -111,8 +98,7 @@ int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int 
                 return MXFP8_ERR_CUDA;
             continue;
         }
-        if (!gather &&
-            !make_map_2d(&ms.m[i], bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, bf ? 2 : 4,
+        if (!make_map_2d(&ms.m[i], bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, bf ? 2 : 4,
                          const_cast<void*>(it.src), (uint64_t)(gated ? 2 * it.cols : it.cols), (uint64_t)it.rows, t_cols, T_ROWS))
             return MXFP8_ERR_CUDA;
         if (i >= count) continue;
@@ -143,7 +129,7 @@ int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int 
     // never shared); where no stream-owned words can be had (a launch being captured, too many streams) the kernel deals
     // tiles out by CTA index
     // (a launch of a few tiles per CTA has nothing to gain from it and keeps the runtime calls of the lookup off its host path)
-    if (!gather && tiles > 4 * (int64_t)QT_CTAS_PER_SM * qt_sm_count()) {
+    if (tiles > 4 * (int64_t)QT_CTAS_PER_SM * qt_sm_count()) {
         static StreamSlots slots;
         static PerDeviceCache<unsigned int*> sched_words;
         unsigned int* base = nullptr;
@@ -160,10 +146,6 @@ int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int 
     if (const char* skip = getenv("MXFP8_TEST_SKIP_TILE")) p.test_skip_tile = atoi(skip);
 #endif
     cudaError_t err;
-    if (gather) {
-        err = quantize_launch_gather(elem, bf, orientation, &p, stream);
-        return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
-    }
     switch (elem) {
         case MXFP8_E4M3: err = quantize_tma_launch<MXFP8_E4M3>(bf, orientation, emulate, ms, p, stream); break;
         case MXFP8_E5M2: err = quantize_tma_launch<MXFP8_E5M2>(bf, orientation, emulate, ms, p, stream); break;

@@ -194,12 +194,6 @@ struct QBatch {
     const void* beta;                     //   source dtype (added last); both null for RMS normalisation
     int glu_cols;                         // gated activation: the source is [rows, 2 * glu_cols] = (gate | up); 0 when unused
     int up_map;                           // two-source launches: tensor map of the second factor (1), or 0 when it is the up half of the first
-    const int* slot_of;                   // gathered conversion (quantize_gather.cu, one tensor): slot of every row (-1: none), rows in
-    const int* used_rows;                 //   use (device), a weight per slot or null, the source, slots per source row, number
-    const float* slot_weights;            //   of slots, and the word that reports a bad array
-    const void* gather_src;
-    int* args_status;
-    uint32_t top_k, top_k_magic, slots;
     int count;
     int tile_start[QT_MAX_TENSORS + 1];   // first tile of each tensor; [count] = all tiles
     QParams t[QT_MAX_TENSORS];
@@ -511,65 +505,6 @@ __device__ __noinline__ void slab_careful(const uint8_t* __restrict__ my_in, uin
     }
 }
 
-// The scale bytes of one tile (1/32 of the output) leave from the staging arrays; the whole CTA calls.
-template <bool BF, bool DO_ROW, bool DO_COL, bool EMU>
-__device__ __forceinline__ void store_scales(const QParams& p, int tile_x, int tile_y, const uint8_t* sm_row, const uint8_t* sm_col,
-                                             int tid, int lane, int warp)
-{
-    constexpr int T_COLS = T_BYTES / (BF ? 2 : 4), NKB = T_COLS / 32;
-    const int64_t gcol0 = (int64_t)tile_x * T_COLS, grow0 = (int64_t)tile_y * T_ROWS;
-    // A BF16 tile wholly inside the tensor fills exactly one 512-byte atom of the swizzled layout per orientation,
-    // and the staging arrays are in the atom's order: one warp stores each atom, 16 bytes per lane.
-    if (BF && !EMU && p.sf_layout == MXFP8_SF_SWIZZLED && grow0 + T_ROWS <= p.rows && gcol0 + T_COLS <= p.cols &&
-        ((reinterpret_cast<uintptr_t>(p.s_row) | reinterpret_cast<uintptr_t>(p.s_col)) & 15) == 0) {
-        if (DO_ROW && warp == 0) {
-            const int64_t atoms_k = ((p.cols >> 5) + 3) >> 2;
-            *reinterpret_cast<uint4*>(p.s_row + ((int64_t)tile_y * atoms_k + tile_x) * 512 + lane * 16) =
-                *reinterpret_cast<const uint4*>(sm_row + lane * 16);
-        }
-        if (DO_COL && warp == (DO_ROW ? 1 : 0)) {
-            const int64_t atoms_r = ((p.rows >> 5) + 3) >> 2;
-            *reinterpret_cast<uint4*>(p.s_col + ((int64_t)tile_x * atoms_r + tile_y) * 512 + lane * 16) =
-                *reinterpret_cast<const uint4*>(sm_col + lane * 16);
-        }
-        return;
-    }
-    // every other tile (ragged, FP32 source, linear layout): one thread per row / per column
-    auto first_bytes = [](uint32_t word, int n) { return n >= 4 ? word : (word & ((1u << (8 * max(n, 0))) - 1u)); };
-    if (DO_ROW && !EMU && tid < T_ROWS) {
-        const int64_t r = grow0 + tid, ncb = p.cols >> 5, kb0 = (int64_t)tile_x * NKB;
-        const int nkb = (int)min((int64_t)NKB, ncb - kb0);
-        const uint32_t v = r < p.rows ? first_bytes(*reinterpret_cast<const uint32_t*>(sm_row + stage_offset(tid)), nkb) : 0u;
-        if (p.sf_layout == MXFP8_SF_SWIZZLED) {
-            // every row of a started 128-row atom is written (pad rows / pad K-blocks get 0)
-            uint8_t* d = p.s_row + ((int64_t)tile_y * ((ncb + 3) >> 2) + (kb0 >> 2)) * 512 + stage_offset(tid) + (kb0 & 3);
-            // a 64-column FP32 tile owns half of the atom's 4 K-blocks; the left half also zeroes
-            // the right half when no tile exists there (pad K-blocks)
-            if (NKB == 4 || ((kb0 & 3) == 0 && kb0 + NKB >= ncb)) *reinterpret_cast<uint32_t*>(d) = v;
-            else *reinterpret_cast<uint16_t*>(d) = (uint16_t)v;
-        } else if (r < p.rows) {
-            uint8_t* d = p.s_row + r * ncb + kb0;
-            for (int kb = 0; kb < nkb; ++kb) d[kb] = (uint8_t)(v >> (8 * kb));
-        }
-    }
-    if (DO_COL && !EMU && tid < T_COLS) {
-        const int64_t c = gcol0 + tid, nrb = p.rows >> 5, rb0 = (int64_t)tile_y * 4;
-        const int nrb_here = (int)min((int64_t)4, nrb - rb0);
-        const uint32_t v = c < p.cols ? first_bytes(*reinterpret_cast<const uint32_t*>(sm_col + stage_offset(tid)), nrb_here) : 0u;
-        if (p.sf_layout == MXFP8_SF_SWIZZLED) {
-            const int64_t padded_cols = ((p.cols + 127) >> 7) << 7;
-            if (c < padded_cols) {
-                *reinterpret_cast<uint32_t*>(p.s_col + ((c >> 7) * ((nrb + 3) >> 2) + tile_y) * 512 + (c & 31) * 16 + ((c >> 5) & 3) * 4) = v;
-                // pad columns no tile covers (FP32 tiles are 64 wide, atoms 128 wide)
-                if (T_COLS == 64 && tile_x == p.tiles_x - 1 && c + 64 >= (int64_t)p.tiles_x * 64 && c + 64 < padded_cols)
-                    *reinterpret_cast<uint32_t*>(p.s_col + (((c + 64) >> 7) * ((nrb + 3) >> 2) + tile_y) * 512 + ((c + 64) & 31) * 16 + (((c + 64) >> 5) & 3) * 4) = 0u;
-            }
-        } else if (c < p.cols) {
-            for (int w = 0; w < nrb_here; ++w) p.s_col[(rb0 + w) * p.cols + c] = (uint8_t)(v >> (8 * w));
-        }
-    }
-}
-
 // PRO: what runs on a tile before the conversion.  Separate instantiations, so that the plain conversion carries
 // none of the prologue code (folding the prologues in at run time cost the plain kernels 2-5 %).
 enum { PRO_NONE = 0, PRO_ELEMENTWISE = 1 /* activation or RMS normalisation */, PRO_GLU = 2 /* gated activation */ };
@@ -581,6 +516,7 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
     constexpr bool BF = (DTYPE == MXFP8_BF16);
     constexpr int VEC = BF ? 4 : 2;                 // elements per lane per row
     constexpr int T_COLS = T_BYTES / (BF ? 2 : 4);  // 128 or 64
+    constexpr int NKB = T_COLS / 32;                // row blocks per tile row: 4 or 2
     constexpr int LPB = 32 / VEC;                   // lanes per row block: 8 or 16
     constexpr bool GLU = (PRO == PRO_GLU);
 
@@ -779,7 +715,57 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
             if (refill < num_tiles) issue_load(refill, buf);
         }
 
-        store_scales<BF, DO_ROW, DO_COL, EMU>(p, tile_x, tile_y, sm_row, sm_col, tid, lane, warp);
+        // ---- scale bytes (1/32 of the output) leave from the staging arrays ----------
+        // A BF16 tile wholly inside the tensor fills exactly one 512-byte atom of the swizzled layout per orientation,
+        // and the staging arrays are in the atom's order: one warp stores each atom, 16 bytes per lane.
+        if (BF && !EMU && p.sf_layout == MXFP8_SF_SWIZZLED && grow0 + T_ROWS <= p.rows && gcol0 + T_COLS <= p.cols &&
+            ((reinterpret_cast<uintptr_t>(p.s_row) | reinterpret_cast<uintptr_t>(p.s_col)) & 15) == 0) {
+            if (DO_ROW && warp == 0) {
+                const int64_t atoms_k = ((p.cols >> 5) + 3) >> 2;
+                *reinterpret_cast<uint4*>(p.s_row + ((int64_t)tile_y * atoms_k + tile_x) * 512 + lane * 16) =
+                    *reinterpret_cast<const uint4*>(sm_row + lane * 16);
+            }
+            if (DO_COL && warp == (DO_ROW ? 1 : 0)) {
+                const int64_t atoms_r = ((p.rows >> 5) + 3) >> 2;
+                *reinterpret_cast<uint4*>(p.s_col + ((int64_t)tile_x * atoms_r + tile_y) * 512 + lane * 16) =
+                    *reinterpret_cast<const uint4*>(sm_col + lane * 16);
+            }
+            continue;
+        }
+        // every other tile (ragged, FP32 source, linear layout): one thread per row / per column
+        auto first_bytes = [](uint32_t word, int n) { return n >= 4 ? word : (word & ((1u << (8 * max(n, 0))) - 1u)); };
+        if (DO_ROW && !EMU && tid < T_ROWS) {
+            const int64_t r = grow0 + tid, ncb = p.cols >> 5, kb0 = (int64_t)tile_x * NKB;
+            const int nkb = (int)min((int64_t)NKB, ncb - kb0);
+            const uint32_t v = r < p.rows ? first_bytes(*reinterpret_cast<const uint32_t*>(sm_row + stage_offset(tid)), nkb) : 0u;
+            if (p.sf_layout == MXFP8_SF_SWIZZLED) {
+                // every row of a started 128-row atom is written (pad rows / pad K-blocks get 0)
+                uint8_t* d = p.s_row + ((int64_t)tile_y * ((ncb + 3) >> 2) + (kb0 >> 2)) * 512 + stage_offset(tid) + (kb0 & 3);
+                // a 64-column FP32 tile owns half of the atom's 4 K-blocks; the left half also zeroes
+                // the right half when no tile exists there (pad K-blocks)
+                if (NKB == 4 || ((kb0 & 3) == 0 && kb0 + NKB >= ncb)) *reinterpret_cast<uint32_t*>(d) = v;
+                else *reinterpret_cast<uint16_t*>(d) = (uint16_t)v;
+            } else if (r < p.rows) {
+                uint8_t* d = p.s_row + r * ncb + kb0;
+                for (int kb = 0; kb < nkb; ++kb) d[kb] = (uint8_t)(v >> (8 * kb));
+            }
+        }
+        if (DO_COL && !EMU && tid < T_COLS) {
+            const int64_t c = gcol0 + tid, nrb = p.rows >> 5, rb0 = (int64_t)tile_y * 4;
+            const int nrb_here = (int)min((int64_t)4, nrb - rb0);
+            const uint32_t v = c < p.cols ? first_bytes(*reinterpret_cast<const uint32_t*>(sm_col + stage_offset(tid)), nrb_here) : 0u;
+            if (p.sf_layout == MXFP8_SF_SWIZZLED) {
+                const int64_t padded_cols = ((p.cols + 127) >> 7) << 7;
+                if (c < padded_cols) {
+                    *reinterpret_cast<uint32_t*>(p.s_col + ((c >> 7) * ((nrb + 3) >> 2) + tile_y) * 512 + (c & 31) * 16 + ((c >> 5) & 3) * 4) = v;
+                    // pad columns no tile covers (FP32 tiles are 64 wide, atoms 128 wide)
+                    if (T_COLS == 64 && tile_x == p.tiles_x - 1 && c + 64 >= (int64_t)p.tiles_x * 64 && c + 64 < padded_cols)
+                        *reinterpret_cast<uint32_t*>(p.s_col + (((c + 64) >> 7) * ((nrb + 3) >> 2) + tile_y) * 512 + ((c + 64) & 31) * 16 + (((c + 64) >> 5) & 3) * 4) = 0u;
+                }
+            } else if (c < p.cols) {
+                for (int w = 0; w < nrb_here; ++w) p.s_col[(rb0 + w) * p.cols + c] = (uint8_t)(v >> (8 * w));
+            }
+        }
     }
     if (tid == 0) leave();
 }

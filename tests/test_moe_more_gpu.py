@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 import oracle as orc
-from test_moe_gpu import dev, gpu_sort, routing
+from test_moe_gpu import gpu_sort, routing
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +35,30 @@ def test_either_gradient_alone_through_the_binding(dy, src):
     with pytest.raises(B.Mxfp8Error) as e:
         B.mxfp8_moe_combine_grad(d, None, row_of, slot_of, w, off, rows_only, weights_only)
     assert e.value.status == B.ERR_NULL
+
+
+@pytest.mark.parametrize("cols", [32, 96, 128, 160, 320, 352])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("orientation", [1, 2, 3])
+@pytest.mark.parametrize("layout", [0, 1])
+def test_dispatch_writes_whole_scale_buffers_as_the_conversion_does(cols, dtype, orientation, layout):
+    """A sorted tensor of exactly the rows in use, widths that end inside a tile and inside an atom of the swizzled layout: every
+    byte of codes and scales, the layout's padding bytes among them, as mxfp8_quantize of the gathered rows writes it."""
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    tokens, top_k, experts = 170, 2, 3
+    off, _, slot_of = gpu_sort(routing(tokens, top_k, experts, 8, "holes"), experts)
+    used = int(off[-1])
+    slot_of = slot_of[:used].contiguous()
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    x = torch.randn(tokens, cols, generator=g, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    y = torch.where((slot_of >= 0).unsqueeze(1), x[slot_of.clamp(min=0).long() // top_k], torch.zeros((), dtype=x.dtype, device="cuda"))
+    want, got = (B.alloc_quantize_outputs(used, cols, orientation, layout) for _ in range(2))
+    for t in want + got:
+        if t is not None:
+            t.fill_(0xA5)
+    B.mxfp8_quantize(y, orientation, B.RULE_PAPER, B.E4M3, *want, layout)
+    B.mxfp8_moe_dispatch_quantize(x, slot_of, top_k, None, off, orientation, B.RULE_PAPER, B.E4M3, *got, layout)
+    assert B.mxfp8_device_status() == 0
+    for a, b in zip(got, want):
+        assert (a is None and b is None) or torch.equal(a, b)
