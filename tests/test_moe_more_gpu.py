@@ -62,3 +62,18 @@ def test_dispatch_writes_whole_scale_buffers_as_the_conversion_does(cols, dtype,
     assert B.mxfp8_device_status() == 0
     for a, b in zip(got, want):
         assert (a is None and b is None) or torch.equal(a, b)
+
+
+@pytest.mark.parametrize("tokens,top_k,experts", [(162501, 8, 256), (312503, 8, 64)])
+@pytest.mark.parametrize("kind", ["holes", "skewed", "one"])
+def test_sort_of_runs_longer_than_a_warp_keeps(tokens, top_k, experts, kind):
+    """From 1212417 slots on a warp's run has more than the 256 slots that stay in its registers: 288 slots, fetched twice
+    for the counts and again for the ranks, and 544 slots, fetched three times; the last chunk ragged."""
+    from paper_2506_08027_b200 import binding as B
+    ids = routing(tokens, top_k, experts, tokens, kind)
+    off, row_of, slot_of = gpu_sort(ids, experts, spare=5)
+    w_off, w_row, w_slot = orc.moe_sort(ids, experts, slot_of.numel())
+    assert np.array_equal(off.cpu().numpy(), w_off)
+    assert np.array_equal(row_of.cpu().numpy(), w_row)
+    assert np.array_equal(slot_of.cpu().numpy(), w_slot)
+    assert B.mxfp8_device_status() == 0
