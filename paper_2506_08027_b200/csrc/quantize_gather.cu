@@ -31,6 +31,13 @@ namespace {
 // 63.7 | 67.2 (64 MiB: one copy alone stays by rows).  Groups of 32 and 40 MiB take 1 % less to 4 % more.
 template <bool BOTH> constexpr int64_t ONE_GROUP = (int64_t)(BOTH ? 48 : 64) << 20;
 constexpr int64_t GROUP_BYTES = (int64_t)24 << 20;
+// Both copies together push the tokens out of L2 before their last expert has read them, unless the codes leave first: the call alone
+// takes 53 us in place of 57 for 8192 tokens, top-6, 2048 BF16 columns (one copy alone is 2 % faster without: 38.1 us, 38.9).  The
+// products that follow read the codes, though, so the codes of up to FIRST_OUT_BYTES, which L2 can hold in part, stay: weighted
+// conversion, DGRAD and WGRAD together 153.9 us with codes that leave first | 152.2 without, of 512 tokens, 175.0 | 173.2 of 1024,
+// 221.9 | 220.3 of 2048, 312.2 | 310.9 of 4096 (conversion and FPROP 0 to 0.7 % less; from FP32 0.6 to 1.8 % less).  From 8192 tokens on (200 MB of codes) the
+// two are within 0.6 % of each other either way, and 24576 tokens of 4096 columns take 0.2 to 0.7 % less with codes that leave first.
+constexpr int64_t FIRST_OUT_BYTES = (int64_t)128 << 20;
 struct Walk {
     uint32_t group, group_magic, last, last_magic;     // tile columns of a group and of the last one
     int groups;
@@ -139,9 +146,7 @@ __device__ __forceinline__ bool walk_row(uint32_t slab, float* inv, float weight
     }
 }
 
-// This lane's VEC elements of a row times the factors, as codes.  Both copies together push the tokens out of L2 before their
-// last expert has read them, unless the codes leave first: 8192 tokens' 53 us in place of 57, 16384 tokens' 126 in place of 137
-// (FP32 187, 201), 1024 tokens' 13.2, 14.9; one copy alone is 2 % faster without (38.1 us, 38.9).
+// This lane's VEC elements of a row times the factors, as codes (FIRST_OUT: they leave L2 before anything else; see FIRST_OUT_BYTES)
 template <int ELEM, int VEC, bool FIRST_OUT>
 __device__ __forceinline__ void store_codes(uint8_t* to, const float2 (&x)[VEC / 2], const float2 (&f)[VEC / 2], int lane)
 {
@@ -170,7 +175,7 @@ __device__ __forceinline__ void store_codes(uint8_t* to, const float2 (&x)[VEC /
 
 // One slab whose columns all lie inside the tensor.  Returns true, with nothing stored but staged scale bytes, when an Inf
 // takes part (or a whole column of NaN); the slab then holds the weighted rows.
-template <int DTYPE, int ELEM, bool DO_ROW, bool DO_COL>
+template <int DTYPE, int ELEM, bool DO_ROW, bool DO_COL, bool FIRST_OUT>
 __device__ __forceinline__ bool convert_slab(uint32_t slab, float* inv, uint8_t* my_qrow, uint8_t* my_qcol, uint32_t pitch, uint8_t* my_row_scales,
                                              uint8_t* my_sm_col, float weight, bool weighted, int lane, uint32_t rule_offset)
 {
@@ -233,9 +238,9 @@ __device__ __forceinline__ bool convert_slab(uint32_t slab, float* inv, uint8_t*
             float2 f[VEC / 2];
 #pragma unroll
             for (int i = 0; i < VEC / 2; ++i) f[i] = make_float2(r, r);
-            store_codes<ELEM, VEC, DO_ROW && DO_COL>(my_qrow + (uint64_t)j * pitch, x, f, lane);
+            store_codes<ELEM, VEC, FIRST_OUT>(my_qrow + (uint64_t)j * pitch, x, f, lane);
         }
-        if constexpr (DO_COL) store_codes<ELEM, VEC, DO_ROW && DO_COL>(my_qcol + (uint64_t)j * pitch, x, col, lane);
+        if constexpr (DO_COL) store_codes<ELEM, VEC, FIRST_OUT>(my_qcol + (uint64_t)j * pitch, x, col, lane);
     }
     return false;
 }
@@ -299,7 +304,7 @@ __device__ __forceinline__ void store_scales(const QParams& p, int tile_x, int t
     }
 }
 
-template <int DTYPE, int ELEM, bool DO_ROW, bool DO_COL, bool GROUPED>
+template <int DTYPE, int ELEM, bool DO_ROW, bool DO_COL, bool GROUPED, bool FIRST_OUT>
 __global__ void __launch_bounds__(QT_THREADS, QT_CTAS_PER_SM)
 quantize_gather_kernel(const __grid_constant__ GatherArgs a, const Walk walk)
 {
@@ -416,7 +421,7 @@ quantize_gather_kernel(const __grid_constant__ GatherArgs a, const Walk walk)
         const bool whole = __all_sync(0xFFFFFFFFu, col_ok);
         bool special = !whole;
         if (whole)
-            special = convert_slab<DTYPE, ELEM, DO_ROW, DO_COL>(slab, row_inv, my_qrow, my_qcol, pitch, sm_row + stage_offset(warp * 32 + lane), my_sm_col,
+            special = convert_slab<DTYPE, ELEM, DO_ROW, DO_COL, FIRST_OUT>(slab, row_inv, my_qrow, my_qcol, pitch, sm_row + stage_offset(warp * 32 + lane), my_sm_col,
                                                                 my_weight, weighted, lane, rule_offset);
         else if (weighted) {
             walk_row<DTYPE, ELEM, false>(slab, row_inv, my_weight, true, nullptr, lane, rule_offset);
@@ -444,11 +449,11 @@ quantize_gather_kernel(const __grid_constant__ GatherArgs a, const Walk walk)
     asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-template <int DTYPE, int ELEM, bool R, bool C, bool GROUPED>
+template <int DTYPE, int ELEM, bool R, bool C, bool GROUPED, bool FIRST_OUT>
 cudaError_t launch_gather(const GatherArgs& a, const Walk& walk, cudaStream_t stream)
 {
     constexpr int SMEM = RING * IN_BYTES + STAGES * 1024 + QT_THREADS * 16;      // ring, scale staging, row factors
-    auto kernel = quantize_gather_kernel<DTYPE, ELEM, R, C, GROUPED>;
+    auto kernel = quantize_gather_kernel<DTYPE, ELEM, R, C, GROUPED, FIRST_OUT>;
     static_assert(STAGES == 2 * STORERS, "see STAGES");
     static unsigned long long smem_set = 0;
     cudaError_t err = ensure_dynamic_smem(kernel, SMEM, smem_set);
@@ -459,6 +464,13 @@ cudaError_t launch_gather(const GatherArgs& a, const Walk& walk, cudaStream_t st
     kernel<<<tiles < most ? tiles : most, QT_THREADS, SMEM, stream>>>(a, walk);
     count_launch(1);
     return cudaGetLastError();
+}
+template <int DTYPE, int ELEM, bool R, bool C, bool GROUPED>
+cudaError_t launch_gather(const GatherArgs& a, const Walk& walk, cudaStream_t stream)
+{
+    if constexpr (R && C)
+        if ((int64_t)a.slots * a.t.cols * 2 > FIRST_OUT_BYTES) return launch_gather<DTYPE, ELEM, R, C, GROUPED, true>(a, walk, stream);
+    return launch_gather<DTYPE, ELEM, R, C, GROUPED, false>(a, walk, stream);
 }
 template <int DTYPE, int ELEM, bool R, bool C>
 cudaError_t launch_gather(const GatherArgs& a, cudaStream_t stream)

@@ -77,3 +77,31 @@ def test_sort_of_runs_longer_than_a_warp_keeps(tokens, top_k, experts, kind):
     assert np.array_equal(row_of.cpu().numpy(), w_row)
     assert np.array_equal(slot_of.cpu().numpy(), w_slot)
     assert B.mxfp8_device_status() == 0
+
+
+@pytest.mark.parametrize("tokens", [2500, 5600])              # codes of both copies: 57 and 129 MiB
+@pytest.mark.parametrize("elem", [orc.E4M3, orc.E5M2, orc.E2M3, orc.E3M2, orc.E2M1])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_dispatch_on_either_side_of_the_size_at_which_codes_leave_l2_first(tokens, elem, dtype, weighted):
+    """The same bytes as gathering, weighting and mxfp8_quantize one after the other."""
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    top_k, experts, cols = 6, 16, 2016
+    off, _, slot_of = gpu_sort(routing(tokens, top_k, experts, 8, "holes"), experts)
+    used = int(off[-1])
+    slot_of = slot_of[:used].contiguous()
+    g = torch.Generator(device="cuda").manual_seed(elem)
+    x = torch.randn(tokens, cols, generator=g, device="cuda").to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    w = torch.randn(tokens, top_k, generator=g, device="cuda") if weighted else None
+    slot = slot_of.clamp(min=0).long()
+    y = x[slot // top_k]
+    if weighted:
+        y = (y.float() * w.reshape(-1)[slot].unsqueeze(1)).to(x.dtype)
+    y = torch.where((slot_of >= 0).unsqueeze(1), y, torch.zeros((), dtype=x.dtype, device="cuda"))
+    want, got = (B.alloc_quantize_outputs(used, cols, B.BOTH, B.SF_SWIZZLED) for _ in range(2))
+    B.mxfp8_quantize(y, B.BOTH, B.RULE_OCP, elem, *want, B.SF_SWIZZLED)
+    B.mxfp8_moe_dispatch_quantize(x, slot_of, top_k, w, off, B.BOTH, B.RULE_OCP, elem, *got, B.SF_SWIZZLED)
+    assert B.mxfp8_device_status() == 0
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
