@@ -189,10 +189,14 @@ int sort_chunk(int64_t slots)
 }
 
 // -------------------------------------------------------------------------------------------- gather, weight, sum
-// V consecutive elements of a row as they lie in memory, read and written in pieces of up to 16 bytes.  Every byte is used
-// once, so rows that are read leave L2 before anything else: the layer's sum (8192 tokens, top-6, 2048 BF16 columns) takes
-// 39.9 us in place of 41.5 and leaves its result there (followed by an elementwise sum 51.6 us in place of 55.8), the gradient
-// 76.4 in place of 77.4.
+// V consecutive elements of a row as they lie in memory, read and written in pieces of up to 16 bytes.  Results are stored the
+// ordinary way, so that L2 keeps what it can of them for the call that reads them: with evict-first stores too, the layer's sum (8192
+// tokens, top-6, 2048 BF16 columns) alone takes 39.2 us in place of 40.2, but followed by an elementwise sum 56.2 in place of 55.2; its
+// gradient alone 76.9 in place of 79.7, but followed by the conversion of the rows that it wrote 167.4 in place of 159.8.
+// STREAM: rows that are read leave L2 before anything else.  In the sum that pays where a lane has up to eight rows in flight (the
+// layer: 40.2 us | 42.5 with ordinary loads, followed by the sum 55.2 | 57.9; 1024 tokens 13.7 | 13.2, 16.8 | 17.2) and costs where it has
+// two (8192 tokens, top-2, 4096 columns: 61.0 | 53.7, followed by the sum 94.2 | 85.7); in the gradient it pays with two (4096 tokens of
+// these 32.9 | 36.5, followed by the conversion 56.5 | 62.3) and makes no difference with more (the layer 79.7 | 79.1, 159.8 | 159.5).
 template <int BYTES> struct Piece { using type = uint4; };
 template <> struct Piece<8> { using type = uint2; };
 template <> struct Piece<4> { using type = uint32_t; };
@@ -203,17 +207,18 @@ template <int DTYPE, int V> struct Vec {
     using P = typename Piece<(BYTES < 16 ? BYTES : 16)>::type;
     static constexpr int N = BYTES / (int)sizeof(P);
     P piece[N];
+    template <bool STREAM>
     __device__ __forceinline__ void load(const void* base, int64_t element)
     {
         const P* p = reinterpret_cast<const P*>(static_cast<const uint8_t*>(base) + element * ESZ);
 #pragma unroll
-        for (int i = 0; i < N; ++i) piece[i] = __ldcs(p + i);
+        for (int i = 0; i < N; ++i) piece[i] = STREAM ? __ldcs(p + i) : p[i];
     }
     __device__ __forceinline__ void store(void* base, int64_t element) const
     {
         P* p = reinterpret_cast<P*>(static_cast<uint8_t*>(base) + element * ESZ);
 #pragma unroll
-        for (int i = 0; i < N; ++i) __stcs(p + i, piece[i]);
+        for (int i = 0; i < N; ++i) p[i] = piece[i];
     }
     __device__ __forceinline__ void zero()
     {
@@ -281,6 +286,7 @@ template <int SRC, int DST, int V, int K, int U>
 __global__ void __launch_bounds__(MOVE_THREADS, COMBINE_CTAS<U>) moe_combine_kernel(const MoveArgs a)
 {
     constexpr int RUN = 32 * V * U;
+    constexpr bool STREAM_ROWS = K > 2;                // see Vec
     const int lane = threadIdx.x & 31;
     const uint32_t runs = (uint32_t)((a.cols + RUN - 1) / RUN), items = (uint32_t)a.tokens * runs, step = gridDim.x * MOVE_WARPS;
     const bool one_round = a.top_k <= K;
@@ -324,7 +330,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, COMBINE_CTAS<U>) moe_combine_ker
                 if (live[j])
 #pragma unroll
                     for (int u = 0; u < U; ++u)
-                        if (c0 + u * 32 * V < a.cols) x[j][u].load(a.src, (int64_t)r * a.cols + c0 + u * 32 * V);
+                        if (c0 + u * 32 * V < a.cols) x[j][u].template load<STREAM_ROWS>(a.src, (int64_t)r * a.cols + c0 + u * 32 * V);
             }
 #pragma unroll
             for (int j = 0; j < K; ++j) {
@@ -400,14 +406,14 @@ __global__ void __launch_bounds__(MOVE_THREADS) moe_combine_grad_kernel(const Mo
                 Vec<SRC, V> x[K][U];
 #pragma unroll
                 for (int u = 0; u < U; ++u)
-                    if (c0 + u * stride < a.cols) g[u].load(a.dy, t * a.cols + c0 + u * stride);
+                    if (c0 + u * stride < a.cols) g[u].template load<true>(a.dy, t * a.cols + c0 + u * stride);
                 if (a.d_weights != nullptr)
 #pragma unroll
                     for (int j = 0; j < K; ++j)
                         if (row[j] >= 0)
 #pragma unroll
                             for (int u = 0; u < U; ++u)
-                                if (c0 + u * stride < a.cols) x[j][u].load(a.src, (int64_t)row[j] * a.cols + c0 + u * stride);
+                                if (c0 + u * stride < a.cols) x[j][u].template load<true>(a.src, (int64_t)row[j] * a.cols + c0 + u * stride);
 #pragma unroll
                 for (int j = 0; j < K; ++j) {
                     if (row[j] < 0) continue;
