@@ -549,6 +549,12 @@ def run_case(args):
         ptrs = B.make_owner_pointers([dw32[r * (F // 8):] for r in range(8)])
         for _ in range(reps):
             B.mxfp8_gemm_reduce_scatter(qdy[2], qdy[3], qx[2], qx[3], F, H, T, B.MN_MAJOR, B.MN_MAJOR, E, E, ptrs, 3)
+    elif args.case == "operator":
+        # one listed case of perf/operators.py
+        ops = operator_cases()
+        state = ops.prepare(next(c for c in ops.listed() if c["name"] == args.operator), 5)
+        for _ in range(reps):
+            ops.run(state)
     elif args.case == "glu":
         # SwiGLU fused ahead of the conversion: source 8192 x (2 x 8192) BF16, both orientations
         src2 = synth.device_tensor("gaussian", (n, 2 * n), 13, "bf16")
@@ -580,6 +586,16 @@ def run_case(args):
             B.mxfp8_gemm(qa[0], qa[1], qw[0], qw[1], m_, n_, k_, B.K_MAJOR, B.K_MAJOR, E, E, y, epi=epi)
     torch.cuda.synchronize()
     print(json.dumps({"case": args.case, "launches": int(B.mxfp8_launch_count()), "device_status": B.mxfp8_device_status()}))
+
+
+def operator_cases():
+    """perf/operators.py (cases, inputs and plain forms of the mixture-of-experts calls and the 4-bit products), set to call the library."""
+    import importlib.util
+    spec = importlib.util.spec_from_file_location("operators", os.path.join(ROOT, "perf", "operators.py"))
+    ops = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ops)
+    ops.own = True
+    return ops
 
 
 def _time_calls(fn, n_bufs, min_iters=10, min_ms=30.0):
@@ -776,6 +792,9 @@ def run_sweep(args):
                     tf / (2 * peaks["bf16_tflops"]), ms_dense * 1e3), flush=True)
             assert B.mxfp8_device_status() == 0
         return
+    if args.sweep == "operators":
+        run_operator_sweep(peaks)
+        return
     if args.sweep == "dp":
         # the data-parallel exchange kernels on ONE GPU (all owners' buffers on this device: the additions go to local
         # memory instead of NVLink, everything else is what a rank of a multi-GPU job launches)
@@ -918,6 +937,110 @@ def run_sweep(args):
     assert B.mxfp8_device_status() == 0
 
 
+def run_operator_sweep(peaks):
+    """The calls around the grouped products and the 4-bit products: the listed cases of perf/operators.py, the gathered conversion by
+    orientation, the calls with and without what reads their results, and 4-bit products by number of tokens beside
+    mxfp8_gemm.  Device times of captured graphs, inputs taken in turn."""
+    import torch
+    from paper_2506_08027_b200 import binding as B
+    P, S, E = B.RULE_PAPER, B.SF_SWIZZLED, B.E4M3
+    ops = operator_cases()
+
+    def us(fn, n_bufs, calls=12):
+        torch.cuda.synchronize()
+        time.sleep(0.2)                                          # the products draw enough power to lower the clock of what follows
+        return 1e3 * statistics.median(_time_graph(fn, n_bufs, calls, 5) for _ in range(7))
+
+    print("| case | us | floor us | of the floor's rate |")
+    print("|---|---|---|---|")
+    for case in ops.listed():
+        states = [ops.prepare(case, 5 + i) for i in range(3)]
+        nbytes = ops.work(case)["bytes"]
+        if case["op"] == "matvec" and case["chosen"]:            # the matrices that are chosen, not as many as could be
+            used = sum(len(s["ids"].unique()) for s in states) / 3
+            nbytes = used * case["rows"] * case["cols"] * 17 / 32 + 2 * case["tokens"] * case["cols"] + 4 * case["tokens"] * case["top_k"] * case["rows"]
+        t, floor = us(lambda i: ops.run(states[i]), 3), nbytes / peaks["hbm_gbs"] / 1e3
+        print("| %s | %.1f | %.2f | %.0f %% |" % (case["name"], t, floor, 100 * floor / t), flush=True)
+        del states
+    g = torch.Generator(device="cuda").manual_seed(7)
+
+    def routed(tokens, top_k, experts):
+        ids = (torch.randn(tokens, experts, generator=g, device="cuda") + torch.randn(experts, generator=g, device="cuda")).topk(top_k, 1).indices.int().contiguous()
+        off = torch.empty(experts + 1, dtype=torch.int32, device="cuda")
+        row_of, slot_of = torch.empty_like(ids), torch.empty(B.mxfp8_moe_rows(tokens, top_k, experts), dtype=torch.int32, device="cuda")
+        B.mxfp8_moe_sort(ids, experts, off, row_of, slot_of, torch.empty(max(1, B.mxfp8_moe_sort_ws_bytes(tokens, top_k, experts)), dtype=torch.uint8, device="cuda"))
+        used = int(off[-1])
+        return off, row_of, slot_of[:used].contiguous(), used
+
+    print()
+    print("| gathered conversion | unweighted us | weighted us | mxfp8_quantize of the sorted rows us |")
+    print("|---|---|---|---|")
+    for tokens, top_k, experts, cols, dtype in ((8192, 6, 64, 2048, torch.bfloat16), (2999, 2, 8, 4096, torch.float32)):
+        r = [routed(tokens, top_k, experts) for _ in range(3)]
+        x = [torch.randn(tokens, cols, generator=g, device="cuda").to(dtype) for _ in range(3)]
+        w = torch.rand(tokens, top_k, generator=g, device="cuda")
+        for o, name in ((B.ROW, "rows"), (B.COL, "columns"), (B.BOTH, "both")):
+            q = [B.alloc_quantize_outputs(r[i][3], cols, o, S) for i in range(3)]
+            y = [torch.randn(r[i][3], cols, generator=g, device="cuda").to(dtype) for i in range(3)]
+            t = [us(lambda i, w=w_: B.mxfp8_moe_dispatch_quantize(x[i], r[i][2], top_k, w, r[i][0], o, P, E, *q[i], S), 3) for w_ in (None, w)]
+            t.append(us(lambda i: B.mxfp8_quantize(y[i], o, P, E, *q[i], S), 3))
+            print("| %d x %d %s, %s | %.1f | %.1f | %.1f |" % (r[0][3], cols, str(dtype)[6:], name, *t), flush=True)
+            del q, y
+        del x
+    print()
+    print("| call, and what reads its result | alone us | both us |")
+    print("|---|---|---|")
+    for tokens, top_k, experts, cols, ffn in ((1024, 6, 64, 2048, 1408), (8192, 6, 64, 2048, 1408), (8192, 2, 8, 4096, 2048)):
+        n = 3 if tokens < 8192 else 2
+        r = [routed(tokens, top_k, experts) for _ in range(n)]
+        new = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)
+        x, y = [new(tokens, cols) for _ in range(n)], [new(r[i][3], cols) for i in range(n)]
+        w = torch.rand(tokens, top_k, generator=g, device="cuda")
+        q = [B.alloc_quantize_outputs(r[i][3], cols, B.BOTH, S) for i in range(n)]
+        wq = B.alloc_quantize_outputs(experts * ffn, cols, B.ROW, S)
+        B.mxfp8_quantize(new(experts * ffn, cols), B.ROW, P, E, *wq, S)
+        z = [torch.empty(r[i][3], ffn, dtype=torch.bfloat16, device="cuda") for i in range(n)]
+        d_y, d_w, dst, other = [torch.empty_like(v) for v in y], torch.empty(tokens, top_k, device="cuda"), [torch.empty_like(v) for v in x], new(tokens, cols)
+        pairs = (("both copies, unweighted; FPROP", lambda i: B.mxfp8_moe_dispatch_quantize(x[i], r[i][2], top_k, None, r[i][0], B.BOTH, P, E, *q[i], S),
+                  lambda i: B.mxfp8_grouped_gemm(q[i][0], q[i][1], wq[0], wq[1], r[i][0], B.GROUP_M, r[i][3], ffn, cols, B.K_MAJOR, E, E, z[i])),
+                 ("weighted sum; an elementwise sum", lambda i: B.mxfp8_moe_combine(y[i], r[i][1], w, dst[i]), lambda i: torch.add(dst[i], other, out=x[i])),
+                 ("its gradient; conversion of the rows", lambda i: B.mxfp8_moe_combine_grad(x[i], y[i], r[i][1], r[i][2], w, r[i][0], d_y[i], d_w),
+                  lambda i: B.mxfp8_quantize(d_y[i], B.BOTH, P, E, *q[i], S)))
+        for name, call, reader in pairs:
+            print("| %d tokens, top-%d, %d columns: %s | %.1f | %.1f |" % (tokens, top_k, cols, name, us(call, n), us(lambda i: (call(i), reader(i)), n)), flush=True)
+        del x, y, q, wq, z, d_y, dst
+        torch.cuda.empty_cache()
+    print()
+    print("| 4-bit product, us (with mxfp8_gemm of E4M3 activations and the same weights in 16-byte slots, without and with the conversion of "
+          "the activations; BF16 library product) | 1 | 8 | 16 | 17 | 32 | 64 | 128 tokens |")
+    print("|---|---|---|---|---|---|---|---|")
+    for rows, cols in ((28672, 4096), (6144, 4096), (4096, 14336), (4096, 4096)):
+        n = max(3, -(-300 * 2 ** 20 // (rows * cols * 17 // 32)))      # copies of the weights: more than twice what L2 holds
+        weights = []
+        for _ in range(n):
+            w = torch.randn(rows, cols, generator=g, device="cuda").to(torch.bfloat16)
+            lin, sw = B.alloc_quantize_outputs(rows, cols, B.ROW, B.SF_LINEAR), B.alloc_quantize_outputs(rows, cols, B.ROW, S)
+            B.mxfp8_quantize(w, B.ROW, P, B.E2M1, *lin, B.SF_LINEAR)
+            B.mxfp8_quantize(w, B.ROW, P, B.E2M1, *sw, S)
+            packed = torch.empty(B.mxfp8_e2m1_packed_bytes(1, rows, cols), dtype=torch.uint8, device="cuda")
+            B.mxfp8_e2m1_pack(lin[0], lin[1], 1, packed)
+            weights.append((packed, sw[0], sw[1], w))
+        cells = []
+        for tokens in (1, 8, 16, 17, 32, 64, 128):
+            x = torch.randn(tokens, cols, generator=g, device="cuda").to(torch.bfloat16)
+            y = torch.empty(tokens, rows, dtype=torch.bfloat16, device="cuda")
+            qx = B.alloc_quantize_outputs(tokens, cols, B.ROW, S)
+            cast = lambda: B.mxfp8_quantize(x, B.ROW, P, E, *qx, S)
+            gemm = lambda i: B.mxfp8_gemm(qx[0], qx[1], weights[i][1], weights[i][2], tokens, rows, cols, B.K_MAJOR, B.K_MAJOR, E, B.E2M1, y)
+            cast()
+            cells.append("%.1f (%.1f, %.1f; %.1f)" % (us(lambda i: B.mxfp8_e2m1_matvec(x, weights[i][0], 1, None, y), n, n), us(gemm, n, n),
+                                                       us(lambda i: (cast(), gemm(i)), n, n), us(lambda i: torch.mm(x, weights[i][3].t(), out=y), n, n)))
+        print("| %d x %d | %s |" % (rows, cols, " | ".join(cells)), flush=True)
+        del weights
+        torch.cuda.empty_cache()
+    assert B.mxfp8_device_status() == 0
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -926,9 +1049,10 @@ def main():
     ap.add_argument("--impl", default="ours", choices=["ours", "reference"])
     ap.add_argument("--no-e2e", action="store_true")
     ap.add_argument("--no-cpu-baseline", action="store_true")
-    ap.add_argument("--case", default=None, choices=["quantize", "dequantize", "fake_quantize", "gemm", "gemm8k", "gemm_fused", "step", "grouped", "grouped_wgrad", "glu", "scatter"],
+    ap.add_argument("--case", default=None, choices=["quantize", "dequantize", "fake_quantize", "gemm", "gemm8k", "gemm_fused", "step", "grouped", "grouped_wgrad", "glu", "scatter", "operator"],
                     help="run one kernel on one small case and exit (for profiler captures)")
-    ap.add_argument("--sweep", default=None, choices=["cast", "gemm", "emu", "moe", "dp", "rules"],
+    ap.add_argument("--operator", default="dispatch layer", help="the listed case of perf/operators.py that --case operator runs")
+    ap.add_argument("--sweep", default=None, choices=["cast", "gemm", "emu", "moe", "dp", "rules", "operators"],
                     help="print the cast-bandwidth, GEMM-shape or round-trip (emu) sweep as a markdown table and exit")
     args = ap.parse_args()
     if args.sweep:
