@@ -439,9 +439,12 @@ int mxfp8_moe_combine_grad(const void* dy, int dy_dtype, int64_t tokens, int64_t
  *   with the codes and scale bytes of matrix matrix_ids[s] (slot s = token * slots_per_token + choice), or of the only
  *   matrix when matrix_ids is NULL (num_matrices and slots_per_token are 1 then).  A slot whose number is outside
  *   0 .. num_matrices - 1 gets zeros.  x [tokens, cols] BF16, 16-byte aligned; y [tokens * slots_per_token, rows] FP32 or BF16.
- *   Products are exact (below FP32's normal range they keep what FP32 keeps); 128 columns at a time are summed in the tensor
- *   cores' FP32 accumulators, these sums in FP32 in a fixed order; scale byte 0xFF gives NaN.
- *   At most 1024 slots and 65535 matrices (ERR_UNSUPPORTED): beyond that mxfp8_gemm / mxfp8_grouped_gemm are the tools.
+ *   Products are exact (below FP32's normal range they keep what FP32 keeps); 128 columns at a time (32 where a scale byte lies
+ *   outside 64 .. 127) are summed in the tensor cores' FP32 accumulators, these sums in FP32 in a fixed order; scale byte 0xFF gives NaN.
+ *   At least one token (ERR_SHAPE); at most 1024 slots and 65535 matrices (ERR_UNSUPPORTED).
+ *   Made for a few tokens: weights are read again for every 32 tokens (chosen matrices: for every eight slots of a matrix).  With more
+ *   than 16 to 32 tokens on one matrix, by its size, mxfp8_quantize of the activations and mxfp8_gemm with the codes as
+ *   mxfp8_quantize lays them out (E2M1, MXFP8_SF_SWIZZLED) take less time, at the precision of MXFP8 activations.
  */
 size_t mxfp8_e2m1_packed_bytes(int64_t num_matrices, int64_t rows, int64_t cols);
 int mxfp8_e2m1_pack(const void* q, const void* s, int64_t num_matrices, int64_t rows, int64_t cols, void* packed, void* stream);

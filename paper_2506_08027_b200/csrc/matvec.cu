@@ -4,9 +4,13 @@
 //
 //   y[s, n] = sum over groups g of 32 columns of  2^(b[n,g] - 127) * sum_{k in g} code[n,k] * x[s / slots_per_token, k]
 //
-// Bound by the weight bytes: 17/32 byte per weight, read once.  The codes become BF16 registers (exact) and go through
-// the warp-level tensor instructions with the tokens as the narrow side.  (The block-scaled tensor instructions would take the
-// 4-bit codes as they are, but not BF16 activations.)
+// The floor is the weight bytes, 17/32 byte per weight.  They are read and decoded once per eight slots of a matrix that is chosen, and
+// once per 8, 16 or 32 tokens of a matrix that serves all: made for a few tokens.  The codes become BF16 registers (exact) and go
+// through the warp-level tensor instructions with the tokens as the narrow side.  (The block-scaled tensor instructions would take
+// the 4-bit codes as they are, but not BF16 activations.)
+// Weights from HBM, us, beside mxfp8_gemm of E4M3 activations and the same codes in their 16-byte slots with the conversion of the
+// activations: 28672 x 4096, 1 token 19.8 (34.5), 16 tokens 27.6 (33.8), 17 tokens 40.7 (34.5), 32 tokens 44.7 (29.5), 128 tokens 160 (32);
+// 4096 x 4096, 1 token 5.9 (19.0), 32 tokens 11.1 (17.3), 64 tokens 19.1 (17.6), 128 tokens 35 (18).
 //
 // Packed layout: a matrix of N rows and K columns is cut into tiles of 16 rows x 128 columns, column tiles innermost,
 // rows and columns padded with zero codes under zero scale bytes.  A tile is 1088 bytes:
@@ -17,7 +21,9 @@
 //   64 bytes of scales: byte 4 r + g for row r, group g.
 // A BF16 number whose three value bits are its two lowest exponent bits and its highest mantissa bit (bits 8 .. 6) and whose
 // other exponent bits are zero is the E2M1 value times 2^-126, subnormals included: two shifts and two masks at most
-// and one exact product by 2^126 turn a pair of codes into a register of two BF16 values.
+// and one exact product by 2^126 turn a pair of codes into a register of two BF16 values.  (Widening a small float by placing its
+// bits across the exponent / mantissa boundary and multiplying by a power of two is a published method, used by open-source code for
+// 4-bit weights; the order of a word's bits and the scale inside the product are this file's.)
 #include "mxfp8_device.cuh"
 #include "mxfp8_host.h"
 
@@ -326,9 +332,9 @@ cudaError_t launch_matvec(MatvecArgs a, unsigned grid_y, cudaStream_t st)
     while ((1 << a.split_log) < WARPS && (1 << a.split_log) < a.col_tiles) ++a.split_log;
     a.per_token_magic = div_magic((uint32_t)a.per_token);
     auto ctas = [&](int log) { return (int64_t)((a.row_tiles + (WARPS >> log) * R - 1) / ((WARPS >> log) * R)); };
-    // Longer runs per warp wherever at least two full waves of CTAs remain: 2816 x 2048 matrices of six experts for eight
-    // tokens took 34 us with two warps to a row group and 43 us with eight; one 28672 x 4096 matrix, whose waves would
-    // run out, 25 us with two and 22 us with eight.
+    // Longer runs per warp wherever at least two full waves of CTAs (148 multiprocessors) remain: 2816 x 2048 matrices of six experts
+    // for eight tokens take 32.8 us with two warps to a row group, 36.4 us with four and 33.4 us with one; one 28672 x 4096 matrix
+    // for eight tokens, whose waves would run out, 19.5 us with four, 21.3 us with two and 25.8 us with one.
     while (a.split_log > 0 && ctas(a.split_log - 1) * grid_y >= 2 * PER_SM * 148) --a.split_log;
     kernel<<<dim3((unsigned)ctas(a.split_log), grid_y), 32 * WARPS, SUMS, st>>>(a);
     count_launch(1);
@@ -338,7 +344,8 @@ cudaError_t launch_matvec(MatvecArgs a, unsigned grid_y, cudaStream_t st)
 // Tokens worked on together: 8, 16 or 32 (a matrix's slots are seldom more than a few when they choose).  Many row tiles: two
 // to a warp, which halves the reads of the activations, in small CTAs that end one by one; few: one to a warp and eight
 // warps to its columns, which keeps more multiprocessors busy.  28672 x 4096: 8 tokens 19.3 us (eight-warp CTAs 21.6),
-// 16 tokens 26.6 us (29.7), 32 tokens 45 us (49); 6144 x 4096 for one token: 5.7 us with few, 6.5 us with many.
+// 16 tokens 26.6 us (29.7), 32 tokens 45 us (49); 6144 x 4096 for one token: 5.7 us with few, 6.5 us with many.  Chosen matrices take
+// the variant of eight slots whatever their number: most have a few, and one with more is walked again per eight.
 template <typename OUT>
 cudaError_t launch_matvec(const MatvecArgs& a, unsigned grid_y, cudaStream_t st)
 {

@@ -1,5 +1,5 @@
 // mxfp8_moe_dispatch_quantize: the conversion of rows gathered by an index (tokens in the order of their experts, App. A.4),
-// optionally weighted.  Tile, slab and staging of the scale bytes are those of the fast path (quantize_tma_kernel.cuh), and so
+// optionally weighted.  Tile, slab and order of the scale bytes are those of the fast path (quantize_tma_kernel.cuh), and so
 // is the careful path for slabs with Inf or NaN or columns behind the tensor; the rest is made for rows that mostly come from L2,
 // where the conversion's instructions, not its bytes, set the pace:
 //   loads  : a warp fetches its own 32-row slab with 16-byte asynchronous copies, two rows per instruction, straight from
@@ -15,9 +15,9 @@
 //   cast   : products of two elements per instruction
 // Measured at 53248 x 2048 BF16 rows of 8192 tokens, top-6, with the HBM time of the tokens read once and the outputs written:
 // 38 us for the row-blocked copy (22), 37 us by columns (22), 53 us for both (39), 63 us for both with weights; mxfp8_quantize
-// of the same rows already sorted takes 88 us for both.  6272 x 4096 FP32 rows of 2999 tokens, weighted, both: 27 us (15).
-// From BF16 62 % of the cycles issue to the integer pipe, the busiest, and L2 moves 8.3 TB/s (the six reads of every token and
-// the outputs).  One slab per warp instead of two, with 16 warps on a multiprocessor instead of 12, took 10 % more by columns and
+// of the same rows already sorted takes 88 us for both.  6272 x 4096 FP32 rows of 2999 tokens, weighted, both: 26.4 us (15).
+// No unit is at its limit: for both from BF16 the integer pipe, the busiest, is taken 62 % of the cycles, a multiprocessor issues 2.45
+// of four instructions a cycle from twelve warps, L2 works at 42 % of its throughput and HBM at 46 %.  One slab per warp instead of two, with 16 warps on a multiprocessor instead of 12, took 10 % more by columns and
 // 2 % less for both; 20 warps spill.
 #include "quantize_tma_kernel.cuh"
 
