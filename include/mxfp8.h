@@ -452,6 +452,101 @@ int mxfp8_e2m1_matvec(const void* x, int64_t tokens, int64_t cols, const void* p
                       const int32_t* matrix_ids, int slots_per_token, void* y, int y_dtype, void* stream);
 
 /*
+ * mxfp8_e2m1_moe -- a whole mixture-of-experts layer (App. A.4) for a few tokens with E2M1 matrices: the choice of the experts from the
+ * router's logits, the gate / up products, the activation, the down products and the weighted sum, in two launches.
+ *     chosen[t, :]  = the top_k experts with the largest logits of token t, the lowest number first among equals; an expert
+ *                     whose logit is -Inf or NaN is never chosen, so a token (an empty place of the batch, say) may have fewer, or none
+ *     weights[t, j] = exp(logits[t, chosen[t, j]] - max) / sum of the same over the chosen experts (renormalize) or over all
+ *     a = gate_up_e x[t];   m[i] = act(a[i]) * a[inner + i];   y[t, :] = sum over j of weights[t, j] * down_e m,   e = chosen[t, j]
+ *   x         [tokens, cols] BF16; logits [tokens, num_experts] FP32.
+ *   gate_up   mxfp8_e2m1_pack of num_experts matrices [2 * inner, cols], the gate's rows before the up projection's; down of
+ *             num_experts matrices [cols, inner].
+ *   act       MXFP8_ACT_NONE .. MXFP8_ACT_GELU_TANH, in FP32 as mxfp8_act_quantize evaluates it.
+ *   y         [tokens, cols] FP32 or BF16, zeros for a token without experts.
+ *   ids, weights  [tokens, top_k] int32 / FP32 outputs, or NULL: the choice, best first, -1 / 0 where there is none.
+ *   ws        mxfp8_e2m1_moe_ws_bytes() bytes, 16-byte aligned; calls that may overlap need their own.
+ *   Products and sums as mxfp8_e2m1_matvec; m is kept as the sum of two BF16 numbers (16 bits), the rest in FP32, in a fixed order.
+ *   cols and inner multiples of 32; at least one token (ERR_SHAPE); at most 64 tokens, 256 experts, top_k 16 (ERR_UNSUPPORTED).
+ */
+size_t mxfp8_e2m1_moe_ws_bytes(int64_t tokens, int top_k, int64_t inner);
+int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens, int64_t cols, int num_experts, int top_k,
+                   const void* gate_up, const void* down, int64_t inner, int act, int renormalize,
+                   void* y, int y_dtype, int32_t* ids, float* weights, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The seam between two blocks of a residual stream: the norm after a block, its gate, the residual sum and the norm before the
+ * next block, all of which the recipe keeps in high precision (Sec. 3.2; the paper names no particular arrangement).
+ *     rstd_post[r] = 1 / sqrt(mean_c y[r, c]^2 + eps);   n = (y * rstd_post) * gamma_post        (n = y without gamma_post)
+ *     h[r, c]      = residual_scale * h_in[r, c] + (branch_scale * gate[r / rows_per_gate, c]) * n    rounded once to the stream's type
+ *     rstd_pre[r]  = 1 / sqrt(mean_c h[r, c]^2 + eps)                                            of h as stored
+ *     x[r, c]      = (h[r, c] * rstd_pre[r]) * gamma_pre[c]                                       rounded once to the block's type
+ * Everything between the roundings is FP32.  Since the second norm reads h as it is stored, x can be computed again from h alone.
+ *
+ * The description of a seam (host memory, read during the call; its pointers are device pointers):
+ */
+typedef struct mxfp8_seam {
+    int64_t rows, cols;        /* cols <= 16384 */
+    int block_dtype;           /* of y, x and their gradients: MXFP8_FP32 or MXFP8_BF16                       */
+    int stream_dtype;          /* of h_in, h and their gradients                                               */
+    int param_dtype;           /* of gamma_post, gate and gamma_pre                                            */
+    const void* gamma_post;    /* [cols], or NULL: no norm after the block                                     */
+    const void* gate;          /* [ceil(rows / rows_per_gate), cols], or NULL: no gate (1)                     */
+    int64_t rows_per_gate;     /* rows (of one sequence, say) that share a row of the gate; >= 1; ignored without gate */
+    const void* gamma_pre;     /* [cols]                                                                       */
+    float branch_scale, residual_scale, eps;
+} mxfp8_seam;
+/*
+ * mxfp8_residual_rmsnorm -- the forward pass.  h may be h_in.  x may be NULL (rstd_pre is written all the same); rstd_post may be NULL where
+ *   there is no norm after the block; [rows] FP32 both.  Tensors are aligned to their elements; rows that start on 16-byte boundaries are faster.
+ * mxfp8_residual_rmsnorm_quantize -- the same with x converted to MXFP8 instead of stored: codes and scales are those of
+ *   mxfp8_rmsnorm_quantize of h with the statistics in rstd_pre (so x is rounded to the stream's type first).  param_dtype has to be stream_dtype
+ *   (ERR_UNSUPPORTED); h, gamma_pre and outputs 16-byte aligned; shapes, alignment and errors of the outputs as mxfp8_quantize, cols a multiple of 16.
+ * mxfp8_residual_rmsnorm_grad -- the backward pass.  dx is the gradient of x, dh that of h from the rest of the stream (either NULL: zero); y, h
+ *   and the statistics are the forward pass's.  With xh = h rstd_pre, yh = y rstd_post, w = branch_scale * gate:
+ *     G     = dh + rstd_pre (dx gamma_pre - xh mean_c(dx gamma_pre xh))
+ *     dh_in = residual_scale G                                               rounded once to the stream's type
+ *     dy    = rstd_post (w gamma_post G - yh mean_c(w gamma_post G yh))      rounded once to the block's type; w G without gamma_post
+ *     d_gamma_pre = sum_r dx xh,  d_gamma_post = sum_r w G yh,  d_gate[g] = sum over the rows of g of branch_scale G n     FP32
+ *   The FP32 sums over rows have a fixed order.  dh_in may be dh.  dy, dh_in and each of the parameters' gradients may be NULL when they are not wanted.
+ *   ws: mxfp8_residual_rmsnorm_grad_ws_bytes() bytes, 16-byte aligned; calls that may overlap need their own.
+ */
+int mxfp8_residual_rmsnorm(const mxfp8_seam* seam, const void* y, const void* h_in, void* h, void* x,
+                           float* rstd_post, float* rstd_pre, void* stream);
+int mxfp8_residual_rmsnorm_quantize(const mxfp8_seam* seam, const void* y, const void* h_in, void* h, float* rstd_post, float* rstd_pre,
+                                    int orientation, int scale_rule, int elem, void* q_row, void* s_row, void* q_col, void* s_col,
+                                    int sf_layout, void* stream);
+size_t mxfp8_residual_rmsnorm_grad_ws_bytes(const mxfp8_seam* seam);
+int mxfp8_residual_rmsnorm_grad(const mxfp8_seam* seam, const void* dx, const void* dh, const void* y, const void* h,
+                                const float* rstd_post, const float* rstd_pre, void* dy, void* dh_in,
+                                float* d_gamma_pre, float* d_gamma_post, float* d_gate, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The norm of all gradients of a step taken together, and clipping by it: what stands between WGRAD and the optimizer.
+ *     S = sum over all items and elements of src^2;   norm = sqrt(S);   factor = min(1, max_norm / (norm + 1e-6))
+ *     dst = factor * src   one FP32 product, rounded once to the item's type
+ * S is FP64 (squares of eight neighbours at a time are added in FP32 where that loses no range), in a fixed order: the result is the same every
+ * time.  A norm that is not finite leaves the values as they are (dst = src, factor = 1), so that the caller can skip the step.
+ *   items   HOST array of `count` entries, read during the call (it may change afterwards).  src and dst are aligned to their elements; dst may be
+ *           src, otherwise no dst may overlap another item.  numel may be 0; count may be 0 (norm 0).
+ * mxfp8_grad_sumsq -- S alone, to `sumsq` (device, one FP64): ranks that hold parts of the gradients add theirs before
+ * mxfp8_grad_scale -- computes norm and factor from *sumsq and scales; norm (device, two FP32): norm and factor.  With dst == src
+ *           everywhere and factor 1 nothing is read or written.
+ * mxfp8_grad_clip  -- both, without the detour over sumsq.
+ *   ws: mxfp8_grad_ws_bytes(items, count) bytes, 8-byte aligned; calls that may overlap need their own.
+ *   Errors: ERR_NULL, ERR_ENUM (dtype), ERR_SHAPE (negative count or numel, max_norm negative or NaN), ERR_ALIGN, ERR_WORKSPACE, ERR_CUDA.
+ */
+typedef struct mxfp8_grad_item {
+    const void* src;
+    void* dst;                 /* not used by mxfp8_grad_sumsq */
+    int64_t numel;
+    int dtype;                 /* MXFP8_FP32 or MXFP8_BF16 */
+} mxfp8_grad_item;
+size_t mxfp8_grad_ws_bytes(const mxfp8_grad_item* items, int count);
+int mxfp8_grad_sumsq(const mxfp8_grad_item* items, int count, double* sumsq, void* ws, size_t ws_bytes, void* stream);
+int mxfp8_grad_scale(const mxfp8_grad_item* items, int count, const double* sumsq, float max_norm, float* norm, void* stream);
+int mxfp8_grad_clip(const mxfp8_grad_item* items, int count, float max_norm, float* norm, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Data-parallel exchange.  The recipe casts weights, activations and output gradients (Sec. 3.2); when
  * the tokens of a step are split over GPUs and every GPU owns a row range of each weight, two exchanges
  * follow from that arithmetic: the MXFP8 copies of the weight shards are gathered (1 + 1/32 bytes per

@@ -33,7 +33,9 @@ EXPORTS = (
     "mxfp8_rmsnorm_quantize_static", "mxfp8_rmsnorm_quantize_static_max_rows", "mxfp8_glu_quantize",
     "mxfp8_sf_concat_k", "mxfp8_gemm_reduce_scatter", "mxfp8_enable_peer_access", "mxfp8_gemm_last_clock", "mxfp8_layernorm_quantize", "mxfp8_act_grad_quantize",
     "mxfp8_moe_rows", "mxfp8_moe_sort_ws_bytes", "mxfp8_moe_sort", "mxfp8_moe_dispatch_quantize", "mxfp8_moe_combine", "mxfp8_moe_combine_grad",
-    "mxfp8_e2m1_packed_bytes", "mxfp8_e2m1_pack", "mxfp8_e2m1_matvec",
+    "mxfp8_e2m1_packed_bytes", "mxfp8_e2m1_pack", "mxfp8_e2m1_matvec", "mxfp8_e2m1_moe_ws_bytes", "mxfp8_e2m1_moe",
+    "mxfp8_residual_rmsnorm", "mxfp8_residual_rmsnorm_quantize", "mxfp8_residual_rmsnorm_grad_ws_bytes", "mxfp8_residual_rmsnorm_grad",
+    "mxfp8_grad_ws_bytes", "mxfp8_grad_sumsq", "mxfp8_grad_scale", "mxfp8_grad_clip",
 )
 
 
@@ -54,6 +56,17 @@ class _GemmProblem(ctypes.Structure):
                 ("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
                 ("a_major", ctypes.c_int), ("b_major", ctypes.c_int), ("a_elem", ctypes.c_int), ("b_elem", ctypes.c_int),
                 ("D", ctypes.c_void_p)]
+
+
+class _Seam(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("block_dtype", ctypes.c_int), ("stream_dtype", ctypes.c_int), ("param_dtype", ctypes.c_int),
+                ("gamma_post", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("rows_per_gate", ctypes.c_int64), ("gamma_pre", ctypes.c_void_p),
+                ("branch_scale", ctypes.c_float), ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class _GradItem(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("numel", ctypes.c_int64), ("dtype", ctypes.c_int)]
 
 
 class _Epilogue(ctypes.Structure):
@@ -144,6 +157,28 @@ def load_library(path: str) -> ctypes.CDLL:
     L.mxfp8_e2m1_pack.argtypes = [p, p, i64, i64, i64, p, p]
     L.mxfp8_e2m1_matvec.restype = i
     L.mxfp8_e2m1_matvec.argtypes = [p, i64, i64, p, i64, i64, p, i, p, i, p]
+    L.mxfp8_e2m1_moe_ws_bytes.restype = sz
+    L.mxfp8_e2m1_moe_ws_bytes.argtypes = [i64, i, i64]
+    L.mxfp8_e2m1_moe.restype = i
+    L.mxfp8_e2m1_moe.argtypes = [p, p, i64, i64, i, i, p, p, i64, i, i, p, i, p, p, p, sz, p]
+    seam = ctypes.POINTER(_Seam)
+    L.mxfp8_residual_rmsnorm.restype = i
+    L.mxfp8_residual_rmsnorm.argtypes = [seam, p, p, p, p, p, p, p]
+    L.mxfp8_residual_rmsnorm_quantize.restype = i
+    L.mxfp8_residual_rmsnorm_quantize.argtypes = [seam, p, p, p, p, p, i, i, i, p, p, p, p, i, p]
+    L.mxfp8_residual_rmsnorm_grad_ws_bytes.restype = sz
+    L.mxfp8_residual_rmsnorm_grad_ws_bytes.argtypes = [seam]
+    L.mxfp8_residual_rmsnorm_grad.restype = i
+    L.mxfp8_residual_rmsnorm_grad.argtypes = [seam, p, p, p, p, p, p, p, p, p, p, p, p, sz, p]
+    items = ctypes.POINTER(_GradItem)
+    L.mxfp8_grad_ws_bytes.restype = sz
+    L.mxfp8_grad_ws_bytes.argtypes = [items, i]
+    L.mxfp8_grad_sumsq.restype = i
+    L.mxfp8_grad_sumsq.argtypes = [items, i, p, p, sz, p]
+    L.mxfp8_grad_scale.restype = i
+    L.mxfp8_grad_scale.argtypes = [items, i, p, ctypes.c_float, p, p]
+    L.mxfp8_grad_clip.restype = i
+    L.mxfp8_grad_clip.argtypes = [items, i, ctypes.c_float, p, p, sz, p]
     L.mxfp8_gemm_last_clock.restype = i
     L.mxfp8_gemm_last_clock.argtypes = [p, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)]
     L.mxfp8_enable_peer_access.restype = i
@@ -592,3 +627,193 @@ def mxfp8_e2m1_matvec(x: torch.Tensor, packed: torch.Tensor, num_matrices: int, 
         raise ValueError("packed is smaller than num_matrices matrices of [%d, %d]" % (rows, cols))
     _check(lib().mxfp8_e2m1_matvec(_ptr(x), tokens, cols, _ptr(packed), num_matrices, rows, _ptr(matrix_ids), per_token, _ptr(y),
                                    _dtype_code(y), st), "mxfp8_e2m1_matvec")
+
+
+def mxfp8_e2m1_moe_ws_bytes(tokens: int, top_k: int, inner: int) -> int:
+    return int(lib().mxfp8_e2m1_moe_ws_bytes(tokens, top_k, inner))
+
+
+def _nbytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def mxfp8_e2m1_moe(x: torch.Tensor, logits: torch.Tensor, top_k: int, gate_up: torch.Tensor, down: torch.Tensor, inner: int, act: int, renormalize: bool,
+                   y: torch.Tensor, ids, weights, ws: torch.Tensor, stream=None) -> None:
+    """x: BF16 [tokens, cols]; logits: FP32 [tokens, experts]; gate_up, down: packed [experts, 2 * inner, cols] and [experts, cols, inner];
+    y: [tokens, cols]; ids, weights: None or int32 / FP32 [tokens, top_k]; ws: mxfp8_e2m1_moe_ws_bytes(...) bytes."""
+    tokens, cols = x.shape
+    experts = logits.shape[1]
+    if x.dtype is not torch.bfloat16 or logits.dtype is not torch.float32:
+        raise TypeError("x must be bfloat16 and logits float32")
+    _int32(ids)
+    st = _stream_for(stream, x, logits, gate_up, down, y, ids, weights, ws)
+    _float_weights(weights, tokens, top_k)
+    if logits.shape[0] != tokens or y.shape != x.shape or (ids is not None and ids.shape != (tokens, top_k)):
+        raise ValueError("logits, y and ids hold one row per token")
+    if _nbytes(gate_up) < mxfp8_e2m1_packed_bytes(experts, 2 * inner, cols) or _nbytes(down) < mxfp8_e2m1_packed_bytes(experts, cols, inner):
+        raise ValueError("gate_up or down is smaller than %d matrices of [%d, %d] and [%d, %d]" % (experts, 2 * inner, cols, cols, inner))
+    _check(lib().mxfp8_e2m1_moe(_ptr(x), _ptr(logits), tokens, cols, experts, top_k, _ptr(gate_up), _ptr(down), inner, act, int(renormalize), _ptr(y),
+                                _dtype_code(y), _ptr(ids), _ptr(weights), _ptr(ws), _nbytes(ws), st), "mxfp8_e2m1_moe")
+
+
+class Seam:
+    """The parameters of a seam between two blocks (see make_seam); holds its tensors as long as it lives."""
+
+    __slots__ = ("gamma_pre", "gamma_post", "gate", "rows_per_gate", "c")
+
+    def describe(self, rows: int, cols: int, block: int, stream: int) -> "_Seam":
+        """The C description for tensors of this shape and types; a copy of its own, so that threads may share the seam."""
+        if cols != self.gamma_pre.numel():
+            raise ValueError("the seam's weights have %d columns, the tensors %d" % (self.gamma_pre.numel(), cols))
+        if self.gate is not None and self.gate.shape[0] != -(-rows // self.rows_per_gate):
+            raise ValueError("the gate has %d rows, %d rows of %d need %d" % (self.gate.shape[0], rows, self.rows_per_gate, -(-rows // self.rows_per_gate)))
+        c = _Seam.from_buffer_copy(self.c)
+        c.rows, c.cols, c.block_dtype, c.stream_dtype = rows, cols, block, stream
+        return c
+
+
+def make_seam(gamma_pre: torch.Tensor, gamma_post=None, gate=None, rows_per_gate: int = 1, branch_scale: float = 1.0, residual_scale: float = 1.0,
+              eps: float = 1e-5) -> Seam:
+    """gamma_pre, gamma_post (or None): [cols]; gate (or None): [ceil(rows / rows_per_gate), cols]; all of one type."""
+    given = [t for t in (gamma_pre, gamma_post, gate) if t is not None]
+    if any(t.dtype is not gamma_pre.dtype or t.shape[-1] != gamma_pre.numel() for t in given) or gamma_pre.dim() != 1 or \
+            (gamma_post is not None and gamma_post.dim() != 1) or (gate is not None and (gate.dim() != 2 or rows_per_gate < 1)):
+        raise ValueError("gamma_pre and gamma_post are [cols], gate is [rows of the gate, cols], all of one type")
+    s = Seam()
+    s.gamma_pre, s.gamma_post, s.gate, s.rows_per_gate = gamma_pre, gamma_post, gate, int(rows_per_gate)
+    s.c = _Seam(param_dtype=_dtype_code(gamma_pre), gamma_post=_ptr(gamma_post), gate=_ptr(gate), rows_per_gate=rows_per_gate, gamma_pre=_ptr(gamma_pre),
+                branch_scale=branch_scale, residual_scale=residual_scale, eps=eps)
+    return s
+
+
+def _row_statistics(rows: int, *tensors) -> None:
+    for t in tensors:
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != rows):
+            raise TypeError("row statistics are float32 [rows]")
+
+
+def _alike(what: str, like: torch.Tensor, *tensors) -> None:
+    for t in tensors:
+        if t is not None and (t.dtype is not like.dtype or t.shape != like.shape):
+            raise ValueError("%s have one shape and type" % what)
+
+
+def mxfp8_residual_rmsnorm(seam: Seam, y: torch.Tensor, h_in: torch.Tensor, h: torch.Tensor, x, rstd_post, rstd_pre: torch.Tensor, stream=None) -> None:
+    """y, x (or None): [rows, cols] of the block's type; h_in, h: of the stream's; rstd_post (or None), rstd_pre: FP32 [rows]."""
+    rows, cols = y.shape
+    st = _stream_for(stream, y, h_in, h, x, rstd_post, rstd_pre, seam.gamma_pre, seam.gamma_post, seam.gate)
+    _alike("y and x", y, x)
+    _alike("h_in and h", h_in, h)
+    _row_statistics(rows, rstd_post, rstd_pre)
+    if h_in.shape != y.shape:
+        raise ValueError("the block's output and the stream have one shape")
+    c = seam.describe(rows, cols, _dtype_code(y), _dtype_code(h_in))
+    _check(lib().mxfp8_residual_rmsnorm(c, _ptr(y), _ptr(h_in), _ptr(h), _ptr(x), _ptr(rstd_post), _ptr(rstd_pre), st), "mxfp8_residual_rmsnorm")
+
+
+def mxfp8_residual_rmsnorm_quantize(seam: Seam, y: torch.Tensor, h_in: torch.Tensor, h: torch.Tensor, rstd_post, rstd_pre: torch.Tensor,
+                                    orientation: int, scale_rule: int, elem: int, q_row, s_row, q_col, s_col, sf_layout: int, stream=None) -> None:
+    """As mxfp8_residual_rmsnorm, with the next block's input converted: outputs as mxfp8_quantize of [rows, cols]."""
+    rows, cols = y.shape
+    st = _stream_for(stream, y, h_in, h, rstd_post, rstd_pre, seam.gamma_pre, seam.gamma_post, seam.gate, q_row, s_row, q_col, s_col)
+    _alike("h_in and h", h_in, h)
+    _row_statistics(rows, rstd_post, rstd_pre)
+    if h_in.shape != y.shape:
+        raise ValueError("the block's output and the stream have one shape")
+    if orientation & ROW and q_row is not None and s_row is not None:
+        _holds(q_row, s_row, rows, cols, rows, cols // 32, sf_layout)
+    if orientation & COL and q_col is not None and s_col is not None:
+        _holds(q_col, s_col, rows, cols, cols, rows // 32, sf_layout)
+    c = seam.describe(rows, cols, _dtype_code(y), _dtype_code(h_in))
+    _check(lib().mxfp8_residual_rmsnorm_quantize(c, _ptr(y), _ptr(h_in), _ptr(h), _ptr(rstd_post), _ptr(rstd_pre), orientation, scale_rule, elem,
+                                                 _ptr(q_row), _ptr(s_row), _ptr(q_col), _ptr(s_col), sf_layout, st), "mxfp8_residual_rmsnorm_quantize")
+
+
+def mxfp8_residual_rmsnorm_grad_ws_bytes(seam: Seam, rows: int, cols: int) -> int:
+    """Bytes for any types of the tensors, on the current device."""
+    return int(lib().mxfp8_residual_rmsnorm_grad_ws_bytes(seam.describe(rows, cols, FP32, FP32)))
+
+
+def mxfp8_residual_rmsnorm_grad(seam: Seam, dx, dh, y: torch.Tensor, h: torch.Tensor, rstd_post, rstd_pre: torch.Tensor, dy, dh_in,
+                                d_gamma_pre, d_gamma_post, d_gate, ws: torch.Tensor, stream=None) -> None:
+    """dx, y, dy: [rows, cols] of the block's type; dh, h, dh_in: of the stream's; the weights' gradients: FP32 of their shapes.  dx, dh and
+    every output may be None."""
+    rows, cols = y.shape
+    st = _stream_for(stream, dx, dh, y, h, rstd_post, rstd_pre, dy, dh_in, d_gamma_pre, d_gamma_post, d_gate, ws, seam.gamma_pre, seam.gamma_post, seam.gate)
+    _alike("dx, y and dy", y, dx, dy)
+    _alike("dh, h and dh_in", h, dh, dh_in)
+    _row_statistics(rows, rstd_post, rstd_pre)
+    if h.shape != y.shape:
+        raise ValueError("the block's output and the stream have one shape")
+    for t, like in ((d_gamma_pre, seam.gamma_pre), (d_gamma_post, seam.gamma_post), (d_gate, seam.gate)):
+        if t is not None and (like is None or t.dtype is not torch.float32 or t.shape != like.shape):
+            raise ValueError("gradients of the seam's weights are float32 of the weights' shapes")
+    c = seam.describe(rows, cols, _dtype_code(y), _dtype_code(h))
+    _check(lib().mxfp8_residual_rmsnorm_grad(c, _ptr(dx), _ptr(dh), _ptr(y), _ptr(h), _ptr(rstd_post), _ptr(rstd_pre), _ptr(dy), _ptr(dh_in),
+                                             _ptr(d_gamma_pre), _ptr(d_gamma_post), _ptr(d_gate), _ptr(ws), _nbytes(ws), st),
+           "mxfp8_residual_rmsnorm_grad")
+
+
+class GradItems:
+    """The C table of a set of gradients (see make_grad_items); holds the tensors as long as it lives."""
+
+    __slots__ = ("c", "count", "keep", "device")
+
+
+def make_grad_items(grads, results=None) -> GradItems:
+    """grads: FP32 / BF16 tensors of one device; results: where the scaled values go (None: in place).  Build it once and reuse it while the
+    tensors live; mxfp8_grad_sumsq needs no results."""
+    grads, results = list(grads), None if results is None else list(results)
+    if results is not None and (len(results) != len(grads) or any(r.dtype is not g.dtype or r.shape != g.shape for g, r in zip(grads, results))):
+        raise ValueError("results have the gradients' shapes and types")
+    items = GradItems()
+    items.c, items.count, items.keep = (_GradItem * max(1, len(grads)))(), len(grads), (grads, results)
+    items.device = None
+    for k, g in enumerate(grads):
+        to = g if results is None else results[k]
+        for t in (g, to):
+            if not t.is_cuda or items.device not in (None, t.get_device()):
+                raise ValueError("gradients lie on one CUDA device")
+            items.device = t.get_device()
+        items.c[k].src, items.c[k].dst, items.c[k].numel, items.c[k].dtype = _ptr(g), _ptr(to), g.numel(), _dtype_code(g)
+    return items
+
+
+def _grad_stream(stream, items: GradItems, *tensors) -> int:
+    st = _stream_for(stream, *tensors)
+    if items.device is not None and items.device != _current_device():
+        raise ValueError("the gradients are on cuda:%d, the call runs on cuda:%d" % (items.device, _current_device()))
+    return st
+
+
+def mxfp8_grad_ws_bytes(items: GradItems) -> int:
+    return int(lib().mxfp8_grad_ws_bytes(items.c, items.count))
+
+
+def mxfp8_grad_sumsq(items: GradItems, sumsq: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """sumsq: one float64 on the device."""
+    st = _grad_stream(stream, items, sumsq, ws)
+    if sumsq.dtype is not torch.float64 or sumsq.numel() != 1:
+        raise TypeError("sumsq is one float64")
+    _check(lib().mxfp8_grad_sumsq(items.c, items.count, _ptr(sumsq), _ptr(ws), _nbytes(ws), st), "mxfp8_grad_sumsq")
+
+
+def _norm_and_factor(norm: torch.Tensor) -> None:
+    if norm.dtype is not torch.float32 or norm.numel() != 2:
+        raise TypeError("norm is two float32: the norm and the factor")
+
+
+def mxfp8_grad_scale(items: GradItems, sumsq: torch.Tensor, max_norm: float, norm: torch.Tensor, stream=None) -> None:
+    """sumsq: one float64; norm: two float32, the norm and the factor."""
+    st = _grad_stream(stream, items, sumsq, norm)
+    if sumsq.dtype is not torch.float64 or sumsq.numel() != 1:
+        raise TypeError("sumsq is one float64")
+    _norm_and_factor(norm)
+    _check(lib().mxfp8_grad_scale(items.c, items.count, _ptr(sumsq), max_norm, _ptr(norm), st), "mxfp8_grad_scale")
+
+
+def mxfp8_grad_clip(items: GradItems, max_norm: float, norm: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """norm: two float32, the norm and the factor."""
+    st = _grad_stream(stream, items, norm, ws)
+    _norm_and_factor(norm)
+    _check(lib().mxfp8_grad_clip(items.c, items.count, max_norm, _ptr(norm), _ptr(ws), _nbytes(ws), st), "mxfp8_grad_clip")

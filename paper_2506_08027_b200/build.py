@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libmxfp8.so")
 # the tests can watch a bounded wait run out without hanging anything.  Never loaded by the binding.
 LIB_TEST_HOOKS = os.path.join(HERE, "libmxfp8_testhooks.so")
 SOURCES = ["quantize.cu", "quantize_tma.cu", "quantize_tma_fp6_fp4.cu", "quantize_gather.cu", "dequantize.cu", "gemm.cu", "gemm_deep.cu", "moe.cu", "matvec.cu",
-           "api.cu"]
+           "moe_tokens.cu", "seam.cu", "grads.cu", "api.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-shared", "-Xcompiler", "-fPIC",

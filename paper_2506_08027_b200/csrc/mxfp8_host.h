@@ -202,6 +202,10 @@ int quantize_tma_batch(const QuantizeItem* items, int count, int src_dtype, int 
                        const float* mean = nullptr, const void* beta = nullptr, const void* second_src = nullptr);
 int quantize_read_and_clear_status();
 
+// Argument checks of a normalisation ahead of the conversion (quantize.cu).
+int rmsnorm_check(const void* src, int src_dtype, int64_t rows, int64_t cols, const void* gamma, float eps, const float* rstd,
+                  int orientation, int scale_rule, int elem, void* q_row, void* s_row, void* q_col, void* s_col, int sf_layout);
+
 // Device status word (bounded waits report here); defined in gemm.cu.
 int read_and_clear_device_status(cudaStream_t stream);
 // Its address on the current device (null if the runtime cannot say)

@@ -542,8 +542,8 @@ extern "C" int mxfp8_layernorm_quantize(const void* src, int src_dtype, int64_t 
 }
 
 namespace mxfp8 {
-namespace {
-// Argument checks shared by mxfp8_rmsnorm_quantize and its variant with the library's own statistics array.
+// Argument checks shared by mxfp8_rmsnorm_quantize, its variant with the library's own statistics array and
+// mxfp8_residual_rmsnorm_quantize.
 int rmsnorm_check(const void* src, int src_dtype, int64_t rows, int64_t cols, const void* gamma, float eps, const float* rstd,
                   int orientation, int scale_rule, int elem, void* q_row, void* s_row, void* q_col, void* s_col, int sf_layout)
 {
@@ -565,7 +565,6 @@ int rmsnorm_check(const void* src, int src_dtype, int64_t rows, int64_t cols, co
     if ((rows + 7) / 8 > 0x7FFFFFFFLL) return MXFP8_ERR_UNSUPPORTED;
     return MXFP8_OK;
 }
-}  // namespace
 }  // namespace mxfp8
 
 extern "C" int mxfp8_rmsnorm_quantize(const void* src, int src_dtype, int64_t rows, int64_t cols,

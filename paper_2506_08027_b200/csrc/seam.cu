@@ -1,0 +1,382 @@
+// The seam between two blocks of a residual stream, forward and backward (mxfp8_residual_rmsnorm and relatives).
+//
+//   rstd_post = 1 / sqrt(mean y^2 + eps);  n = (y rstd_post) gamma_post;  h = residual_scale h_in + (branch_scale gate) n
+//   rstd_pre  = 1 / sqrt(mean h^2 + eps);  x = (h rstd_pre) gamma_pre
+//
+// Bound by memory: forward y, h_in -> h, x; backward dx, dh, y, h -> dy, dh_in, each element once.
+#include <cuda_bf16.h>
+
+#include "mxfp8_device.cuh"
+#include "mxfp8_host.h"
+
+namespace mxfp8 {
+namespace {
+
+constexpr int SEAM_MAX_COLS = 16384;
+constexpr int SEAM_THREADS = 256, SEAM_WARPS = SEAM_THREADS / 32;
+
+struct SeamArgs {
+    int64_t rows;
+    int cols;
+    const void *gamma_post, *gate, *gamma_pre;
+    bool bf16_params;
+    int64_t rows_per_gate;
+    float branch_scale, residual_scale, eps;
+    const void *y, *h_in;                        // forward inputs; the backward pass reads y and h
+    void *h, *x;
+    float *rstd_post, *rstd_pre;
+    const void *dx, *dh;                         // backward
+    void *dy, *dh_in;
+    float *d_gamma_pre, *d_gamma_post, *d_gate;
+    float* ws;
+    int64_t chunk;                               // rows of a CTA
+    int64_t gates;
+};
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ float param(const void* p, int64_t at, bool bf16)
+{
+    return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]) : static_cast<const float*>(p)[at];
+}
+
+// Sums of N values over the CTA, the same in every thread and in a fixed order.  `turn` alternates between two areas, so that one
+// barrier per call is enough.
+template <int N>
+__device__ __forceinline__ void cta_sums(float (&v)[N], float (*area)[SEAM_WARPS][N], int& turn)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], off);
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) area[turn][threadIdx.x >> 5][i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        v[i] = 0.f;
+        for (int w = 0; w < SEAM_WARPS; ++w) v[i] += area[turn][w][i];
+    }
+    turn ^= 1;
+}
+
+// Any width and alignment: a CTA per row, one element per thread at a time, rows read again where a second pass needs them (from L2).
+template <typename Y, typename H>
+__global__ void __launch_bounds__(SEAM_THREADS) seam_forward_any_kernel(const SeamArgs a)
+{
+    __shared__ float area[2][SEAM_WARPS][1];
+    int turn = 0;
+    const float n_cols = (float)a.cols;
+    for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+        const Y* y = static_cast<const Y*>(a.y) + r * a.cols;
+        const H* h_in = static_cast<const H*>(a.h_in) + r * a.cols;
+        H* h = static_cast<H*>(a.h) + r * a.cols;
+        const int64_t gate = a.gate ? r / a.rows_per_gate * a.cols : 0;
+        float s[1] = {0.f}, rp = 1.f;
+        if (a.gamma_post) {
+            for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) s[0] = fmaf(to_float(y[c]), to_float(y[c]), s[0]);
+            cta_sums(s, area, turn);
+            rp = 1.0f / sqrtf(s[0] / n_cols + a.eps);
+            if (threadIdx.x == 0) a.rstd_post[r] = rp;
+        }
+        s[0] = 0.f;
+        for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) {
+            float n = to_float(y[c]);
+            if (a.gamma_post) n = (n * rp) * param(a.gamma_post, c, a.bf16_params);
+            const float w = a.gate ? a.branch_scale * param(a.gate, gate + c, a.bf16_params) : a.branch_scale;
+            const H v = from_float<H>(fmaf(w, n, a.residual_scale * to_float(h_in[c])));
+            h[c] = v;
+            s[0] = fmaf(to_float(v), to_float(v), s[0]);
+        }
+        cta_sums(s, area, turn);
+        const float rn = 1.0f / sqrtf(s[0] / n_cols + a.eps);
+        if (threadIdx.x == 0) a.rstd_pre[r] = rn;
+        if (a.x) {
+            Y* x = static_cast<Y*>(a.x) + r * a.cols;
+            for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS)              // the thread's own stores
+                x[c] = from_float<Y>((to_float(h[c]) * rn) * param(a.gamma_pre, c, a.bf16_params));
+        }
+    }
+}
+
+// Backward.  One reduction per row: with t = dx gamma_pre, w = branch_scale gate gamma_post,
+//   G = dh + rn (t - xh c1), c1 = S1 / cols,  S1 = sum t xh
+//   mean(w G yh) = (S2 - rn c1 S3) / cols,     S2 = sum w yh (dh + rn t),  S3 = sum w yh xh
+// A CTA takes `chunk` consecutive rows.  Its column sums go to the workspace ([CTA][cols] for each weight); those of the gate
+// are put down whenever the row of the gate changes, at place CTA + row of the gate (no two CTAs share one: the next CTA begins
+// with the same row of the gate or a later one), or in d_gate where one CTA holds all rows of it.
+__device__ __forceinline__ float* gate_part(const SeamArgs& a, int64_t g)
+{
+    const int64_t first = g * a.rows_per_gate, last = min(first + a.rows_per_gate, a.rows) - 1;
+    if (first / a.chunk == last / a.chunk) return a.d_gate + g * a.cols;
+    const int64_t weights = (int64_t)gridDim.x * a.cols * ((a.d_gamma_pre != nullptr) + (a.d_gamma_post != nullptr));
+    return a.ws + weights + (blockIdx.x + g) * a.cols;
+}
+
+template <typename Y, typename H>
+__global__ void __launch_bounds__(SEAM_THREADS) seam_grad_any_kernel(const SeamArgs a)
+{
+    extern __shared__ float column[];              // d_gamma_pre, d_gamma_post, d_gate: each column belongs to one thread
+    __shared__ float area[2][SEAM_WARPS][3];
+    int turn = 0;
+    float *pre = column, *post = column + a.cols, *gates = column + 2 * a.cols;
+    for (int c = threadIdx.x; c < 3 * a.cols; c += SEAM_THREADS) column[c] = 0.f;
+    __syncthreads();
+    const int64_t r0 = blockIdx.x * a.chunk, r1 = min(r0 + a.chunk, a.rows);
+    const float inv_cols = 1.0f / (float)a.cols;
+    for (int64_t r = r0; r < r1; ++r) {
+        const Y* y = static_cast<const Y*>(a.y) + r * a.cols;
+        const H* h = static_cast<const H*>(a.h) + r * a.cols;
+        const Y* dx = a.dx ? static_cast<const Y*>(a.dx) + r * a.cols : nullptr;
+        const H* dh = a.dh ? static_cast<const H*>(a.dh) + r * a.cols : nullptr;
+        Y* dy = a.dy ? static_cast<Y*>(a.dy) + r * a.cols : nullptr;
+        H* dh_in = a.dh_in ? static_cast<H*>(a.dh_in) + r * a.cols : nullptr;
+        const int64_t g = a.gate ? r / a.rows_per_gate : 0;
+        const float rn = a.rstd_pre[r], rp = a.gamma_post ? a.rstd_post[r] : 1.f;
+        float s[3] = {0.f, 0.f, 0.f};
+        for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) {
+            const float xh = to_float(h[c]) * rn, t = dx ? to_float(dx[c]) * param(a.gamma_pre, c, a.bf16_params) : 0.f;
+            s[0] = fmaf(t, xh, s[0]);
+            if (a.gamma_post) {
+                float w = a.branch_scale * param(a.gamma_post, c, a.bf16_params);
+                if (a.gate) w *= param(a.gate, g * a.cols + c, a.bf16_params);
+                const float wy = w * (to_float(y[c]) * rp);
+                s[1] = fmaf(wy, fmaf(rn, t, dh ? to_float(dh[c]) : 0.f), s[1]);
+                s[2] = fmaf(wy, xh, s[2]);
+            }
+        }
+        cta_sums(s, area, turn);
+        const float c1 = s[0] * inv_cols, c2 = (s[1] - rn * c1 * s[2]) * inv_cols;
+        for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) {
+            const float v = dx ? to_float(dx[c]) : 0.f, xh = to_float(h[c]) * rn;
+            const float t = v * param(a.gamma_pre, c, a.bf16_params);
+            const float G = fmaf(rn, t - xh * c1, dh ? to_float(dh[c]) : 0.f);
+            pre[c] = fmaf(v, xh, pre[c]);
+            if (dh_in) dh_in[c] = from_float<H>(a.residual_scale * G);
+            const float yh = to_float(y[c]) * rp, branch = a.branch_scale * G;
+            const float gamma = a.gamma_post ? param(a.gamma_post, c, a.bf16_params) : 1.f;
+            gates[c] = fmaf(branch, yh * gamma, gates[c]);
+            const float wG = a.gate ? branch * param(a.gate, g * a.cols + c, a.bf16_params) : branch;
+            post[c] = fmaf(wG, yh, post[c]);
+            if (dy) dy[c] = from_float<Y>(a.gamma_post ? rp * (wG * gamma - yh * c2) : wG);
+        }
+        if (a.d_gate && (r + 1 == r1 || (r + 1) / a.rows_per_gate != g)) {
+            float* to = gate_part(a, g);
+            for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) {
+                to[c] = gates[c];
+                gates[c] = 0.f;
+            }
+        }
+    }
+    float* to = a.ws + (int64_t)blockIdx.x * a.cols;
+    if (a.d_gamma_pre) {
+        for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) to[c] = pre[c];
+        to += (int64_t)gridDim.x * a.cols;
+    }
+    if (a.d_gamma_post)
+        for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) to[c] = post[c];
+}
+
+// Joins the CTAs' sums.  blockIdx.y: 0 / 1 the weights, then the rows of the gate that several CTAs hold.
+constexpr int JOIN_COLS = 32, JOIN_WARPS = 8;
+__global__ void __launch_bounds__(32 * JOIN_WARPS) seam_join_kernel(const SeamArgs a, int parts)
+{
+    __shared__ float area[JOIN_WARPS][JOIN_COLS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x * JOIN_COLS + lane, weights = (a.d_gamma_pre != nullptr) + (a.d_gamma_post != nullptr);
+    for (int64_t which = blockIdx.y; which < weights + (a.d_gate ? a.gates : 0); which += gridDim.y) {
+        const float* from;
+        float* to;
+        int64_t count = parts;
+        if (which < weights) {
+            from = a.ws + which * (int64_t)parts * a.cols;
+            to = (which == 0 && a.d_gamma_pre) ? a.d_gamma_pre : a.d_gamma_post;
+        } else {
+            const int64_t g = which - weights, first = g * a.rows_per_gate, last = min(first + a.rows_per_gate, a.rows) - 1;
+            const int64_t b0 = first / a.chunk;
+            count = last / a.chunk - b0 + 1;
+            if (count == 1) continue;
+            from = a.ws + ((int64_t)weights * parts + b0 + g) * a.cols;
+            to = a.d_gate + g * a.cols;
+        }
+        float s = 0.f;
+        if (c < a.cols)
+            for (int64_t p = warp; p < count; p += JOIN_WARPS) s += from[p * a.cols + c];
+        area[warp][lane] = s;
+        __syncthreads();
+        if (warp == 0) {
+            s = 0.f;
+            for (int w = 0; w < JOIN_WARPS; ++w) s += area[w][lane];
+            if (c < a.cols) to[c] = s;
+        }
+        __syncthreads();
+    }
+}
+
+int multiprocessors()
+{
+    static PerDeviceCache<int> cache;
+    int n = 0;
+    return cache.get(n, [](int dev, int& v) { return cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess; }) ? n : 148;
+}
+
+bool misaligned(const void* p, int dtype) { return (reinterpret_cast<uintptr_t>(p) & (dtype == MXFP8_BF16 ? 1u : 3u)) != 0; }
+
+int seam_check(const mxfp8_seam* s)
+{
+    if (!s) return MXFP8_ERR_NULL;
+    for (int d : {s->block_dtype, s->stream_dtype, s->param_dtype})
+        if (d != MXFP8_FP32 && d != MXFP8_BF16) return MXFP8_ERR_ENUM;
+    if (!s->gamma_pre) return MXFP8_ERR_NULL;
+    if (s->rows <= 0 || s->cols <= 0 || !(s->eps >= 0.f) || (s->gate && s->rows_per_gate < 1)) return MXFP8_ERR_SHAPE;
+    if (misaligned(s->gamma_pre, s->param_dtype) || misaligned(s->gamma_post, s->param_dtype) || misaligned(s->gate, s->param_dtype)) return MXFP8_ERR_ALIGN;
+    if (s->cols > SEAM_MAX_COLS || s->rows > (1LL << 40)) return MXFP8_ERR_UNSUPPORTED;
+    return MXFP8_OK;
+}
+
+SeamArgs seam_args(const mxfp8_seam* s)
+{
+    SeamArgs a{};
+    a.rows = s->rows; a.cols = (int)s->cols;
+    a.gamma_post = s->gamma_post; a.gate = s->gate; a.gamma_pre = s->gamma_pre;
+    a.bf16_params = s->param_dtype == MXFP8_BF16;
+    // one row of the gate for all is the same as rows_per_gate = rows
+    a.rows_per_gate = s->gate ? (s->rows_per_gate < s->rows ? s->rows_per_gate : s->rows) : s->rows;
+    a.gates = (s->rows + a.rows_per_gate - 1) / a.rows_per_gate;
+    a.branch_scale = s->branch_scale; a.residual_scale = s->residual_scale; a.eps = s->eps;
+    return a;
+}
+
+// Calls f with two null pointers of the block's and the stream's element types.
+template <typename F>
+cudaError_t by_types(const mxfp8_seam* s, F f)
+{
+    using B = __nv_bfloat16;
+    if (s->block_dtype == MXFP8_BF16)
+        return s->stream_dtype == MXFP8_BF16 ? f((B*)nullptr, (B*)nullptr) : f((B*)nullptr, (float*)nullptr);
+    return s->stream_dtype == MXFP8_BF16 ? f((float*)nullptr, (B*)nullptr) : f((float*)nullptr, (float*)nullptr);
+}
+
+template <typename Y, typename H>
+cudaError_t launch_forward(const SeamArgs& a, cudaStream_t st)
+{
+    const int64_t most = (int64_t)multiprocessors() * 8;
+    seam_forward_any_kernel<Y, H><<<(unsigned)(a.rows < most ? a.rows : most), SEAM_THREADS, 0, st>>>(a);
+    count_launch(1);
+    return cudaGetLastError();
+}
+
+// CTAs of the backward pass and their rows: two per multiprocessor while a row remains for each.
+int64_t grad_chunk(int64_t rows)
+{
+    const int64_t ctas = 2 * (int64_t)multiprocessors();
+    return (rows + ctas - 1) / ctas;
+}
+
+template <typename Y, typename H>
+cudaError_t launch_grad(SeamArgs a, cudaStream_t st)
+{
+    const unsigned ctas = (unsigned)((a.rows + a.chunk - 1) / a.chunk);
+    auto kernel = seam_grad_any_kernel<Y, H>;
+    static unsigned long long set = 0;
+    const cudaError_t err = ensure_dynamic_smem(kernel, 3 * SEAM_MAX_COLS * (int)sizeof(float), set);
+    if (err != cudaSuccess) return err;
+    kernel<<<ctas, SEAM_THREADS, 3 * a.cols * sizeof(float), st>>>(a);
+    count_launch(1);
+    cudaError_t rc = cudaGetLastError();
+    const int64_t joins = (a.d_gamma_pre != nullptr) + (a.d_gamma_post != nullptr) + (a.d_gate ? a.gates : 0);
+    if (rc != cudaSuccess || joins == 0) return rc;
+    seam_join_kernel<<<dim3((a.cols + JOIN_COLS - 1) / JOIN_COLS, (unsigned)(joins < 1024 ? joins : 1024)), 32 * JOIN_WARPS, 0, st>>>(a, (int)ctas);
+    count_launch(1);
+    return cudaGetLastError();
+}
+
+int seam_forward(const mxfp8_seam* s, const void* y, const void* h_in, void* h, void* x, float* rstd_post, float* rstd_pre, cudaStream_t st)
+{
+    SeamArgs a = seam_args(s);
+    a.y = y; a.h_in = h_in; a.h = h; a.x = x; a.rstd_post = rstd_post; a.rstd_pre = rstd_pre;
+    const cudaError_t err = by_types(s, [&](auto* yt, auto* ht) {
+        return launch_forward<std::remove_pointer_t<decltype(yt)>, std::remove_pointer_t<decltype(ht)>>(a, st);
+    });
+    return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
+}
+
+int forward_check(const mxfp8_seam* s, const void* y, const void* h_in, const void* h, const float* rstd_post, const float* rstd_pre)
+{
+    const int bad = seam_check(s);
+    if (bad != MXFP8_OK) return bad;
+    if (!y || !h_in || !h || !rstd_pre || (s->gamma_post && !rstd_post)) return MXFP8_ERR_NULL;
+    if (misaligned(y, s->block_dtype) || misaligned(h_in, s->stream_dtype) || misaligned(h, s->stream_dtype) ||
+        misaligned(rstd_post, MXFP8_FP32) || misaligned(rstd_pre, MXFP8_FP32)) return MXFP8_ERR_ALIGN;
+    return MXFP8_OK;
+}
+
+}  // namespace
+}  // namespace mxfp8
+
+using namespace mxfp8;
+
+extern "C" int mxfp8_residual_rmsnorm(const mxfp8_seam* seam, const void* y, const void* h_in, void* h, void* x,
+                                      float* rstd_post, float* rstd_pre, void* stream)
+{
+    const int bad = forward_check(seam, y, h_in, h, rstd_post, rstd_pre);
+    if (bad != MXFP8_OK) return bad;
+    if (misaligned(x, seam->block_dtype)) return MXFP8_ERR_ALIGN;
+    return seam_forward(seam, y, h_in, h, x, rstd_post, rstd_pre, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" int mxfp8_residual_rmsnorm_quantize(const mxfp8_seam* seam, const void* y, const void* h_in, void* h, float* rstd_post, float* rstd_pre,
+                                               int orientation, int scale_rule, int elem, void* q_row, void* s_row, void* q_col, void* s_col,
+                                               int sf_layout, void* stream)
+{
+    int bad = forward_check(seam, y, h_in, h, rstd_post, rstd_pre);
+    if (bad != MXFP8_OK) return bad;
+    if (seam->param_dtype != seam->stream_dtype) return MXFP8_ERR_UNSUPPORTED;
+    bad = rmsnorm_check(h, seam->stream_dtype, seam->rows, seam->cols, seam->gamma_pre, seam->eps, rstd_pre, orientation, scale_rule, elem,
+                        q_row, s_row, q_col, s_col, sf_layout);
+    if (bad != MXFP8_OK) return bad;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    bad = seam_forward(seam, y, h_in, h, nullptr, rstd_post, rstd_pre, st);
+    if (bad != MXFP8_OK) return bad;
+    const QuantizeItem item{h, seam->rows, seam->cols, q_row, s_row, q_col, s_col};
+    return quantize_tma_batch(&item, 1, seam->stream_dtype, orientation, scale_rule, elem, sf_layout, st, false, MXFP8_ACT_NONE, rstd_pre, seam->gamma_pre);
+}
+
+extern "C" size_t mxfp8_residual_rmsnorm_grad_ws_bytes(const mxfp8_seam* seam)
+{
+    if (seam_check(seam) != MXFP8_OK) return 0;
+    const SeamArgs a = seam_args(seam);
+    const int64_t chunk = grad_chunk(a.rows), ctas = (a.rows + chunk - 1) / chunk;
+    const int64_t parts = ctas * (1 + (seam->gamma_post != nullptr)) + (seam->gate ? ctas + a.gates : 0);
+    return (size_t)parts * (size_t)a.cols * sizeof(float);
+}
+
+extern "C" int mxfp8_residual_rmsnorm_grad(const mxfp8_seam* seam, const void* dx, const void* dh, const void* y, const void* h,
+                                           const float* rstd_post, const float* rstd_pre, void* dy, void* dh_in,
+                                           float* d_gamma_pre, float* d_gamma_post, float* d_gate, void* ws, size_t ws_bytes, void* stream)
+{
+    const int bad = seam_check(seam);
+    if (bad != MXFP8_OK) return bad;
+    if (!y || !h || !rstd_pre || (seam->gamma_post && !rstd_post) || (!seam->gamma_post && d_gamma_post) || (!seam->gate && d_gate)) return MXFP8_ERR_NULL;
+    for (const void* p : {dx, y, static_cast<const void*>(dy)}) if (misaligned(p, seam->block_dtype)) return MXFP8_ERR_ALIGN;
+    for (const void* p : {dh, h, static_cast<const void*>(dh_in)}) if (misaligned(p, seam->stream_dtype)) return MXFP8_ERR_ALIGN;
+    for (const float* p : {rstd_post, rstd_pre, static_cast<const float*>(d_gamma_pre), static_cast<const float*>(d_gamma_post), static_cast<const float*>(d_gate)})
+        if (misaligned(p, MXFP8_FP32)) return MXFP8_ERR_ALIGN;
+    if (!ws || ws_bytes < mxfp8_residual_rmsnorm_grad_ws_bytes(seam)) return MXFP8_ERR_WORKSPACE;
+    if (!aligned16(ws)) return MXFP8_ERR_ALIGN;
+    SeamArgs a = seam_args(seam);
+    a.dx = dx; a.dh = dh; a.y = y; a.h = const_cast<void*>(h);
+    a.rstd_post = const_cast<float*>(rstd_post); a.rstd_pre = const_cast<float*>(rstd_pre);
+    a.dy = dy; a.dh_in = dh_in; a.d_gamma_pre = d_gamma_pre; a.d_gamma_post = d_gamma_post; a.d_gate = d_gate;
+    a.ws = static_cast<float*>(ws);
+    a.chunk = grad_chunk(a.rows);
+    const cudaError_t err = by_types(seam, [&](auto* yt, auto* ht) {
+        return launch_grad<std::remove_pointer_t<decltype(yt)>, std::remove_pointer_t<decltype(ht)>>(a, static_cast<cudaStream_t>(stream));
+    });
+    return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
+}
