@@ -13,7 +13,8 @@ namespace mxfp8 {
 namespace {
 
 constexpr int SEAM_MAX_COLS = 16384;
-constexpr int SEAM_THREADS = 256, SEAM_WARPS = SEAM_THREADS / 32;
+constexpr int SEAM_THREADS = 256;                // of the kernels for any alignment
+constexpr int SEAM_MAX_WARPS = 32;
 
 struct SeamArgs {
     int64_t rows;
@@ -44,24 +45,29 @@ __device__ __forceinline__ float param(const void* p, int64_t at, bool bf16)
     return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]) : static_cast<const float*>(p)[at];
 }
 
-// Sums of N values over the CTA, the same in every thread and in a fixed order.  `turn` alternates between two areas, so that one
-// barrier per call is enough.
 template <int N>
-__device__ __forceinline__ void cta_sums(float (&v)[N], float (*area)[SEAM_WARPS][N], int& turn)
+__device__ __forceinline__ void warp_sums(float (&v)[N])
 {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1)
 #pragma unroll
         for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], off);
+}
+
+// Sums of N values over the CTA, the same in every thread and in a fixed order.  `turn` alternates between two areas, so that one
+// barrier per call is enough.
+template <int N>
+__device__ __forceinline__ void cta_sums(float (&v)[N], float (*area)[SEAM_MAX_WARPS][N], int& turn)
+{
+    warp_sums(v);
     if ((threadIdx.x & 31) == 0)
 #pragma unroll
         for (int i = 0; i < N; ++i) area[turn][threadIdx.x >> 5][i] = v[i];
     __syncthreads();
+    // every warp adds the warps' sums the same way
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        v[i] = 0.f;
-        for (int w = 0; w < SEAM_WARPS; ++w) v[i] += area[turn][w][i];
-    }
+    for (int i = 0; i < N; ++i) v[i] = (threadIdx.x & 31) < (blockDim.x >> 5) ? area[turn][threadIdx.x & 31][i] : 0.f;
+    warp_sums(v);
     turn ^= 1;
 }
 
@@ -69,7 +75,7 @@ __device__ __forceinline__ void cta_sums(float (&v)[N], float (*area)[SEAM_WARPS
 template <typename Y, typename H>
 __global__ void __launch_bounds__(SEAM_THREADS) seam_forward_any_kernel(const SeamArgs a)
 {
-    __shared__ float area[2][SEAM_WARPS][1];
+    __shared__ float area[2][SEAM_MAX_WARPS][1];
     int turn = 0;
     const float n_cols = (float)a.cols;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -122,7 +128,7 @@ template <typename Y, typename H>
 __global__ void __launch_bounds__(SEAM_THREADS) seam_grad_any_kernel(const SeamArgs a)
 {
     extern __shared__ float column[];              // d_gamma_pre, d_gamma_post, d_gate: each column belongs to one thread
-    __shared__ float area[2][SEAM_WARPS][3];
+    __shared__ float area[2][SEAM_MAX_WARPS][3];
     int turn = 0;
     float *pre = column, *post = column + a.cols, *gates = column + 2 * a.cols;
     for (int c = threadIdx.x; c < 3 * a.cols; c += SEAM_THREADS) column[c] = 0.f;
@@ -180,6 +186,338 @@ __global__ void __launch_bounds__(SEAM_THREADS) seam_grad_any_kernel(const SeamA
     }
     if (a.d_gamma_post)
         for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) to[c] = post[c];
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Rows that start on 16-byte boundaries.  A thread owns the vectors of eight columns threadIdx.x + i T of every row that its group
+// takes (a warp for short rows, else the CTA of T threads).  It copies them itself, asynchronously, into places of shared memory that no other
+// thread touches, STAGES rows ahead: no barrier guards them, only the thread's own wait for its copies.
+template <typename T> constexpr int PIECES = sizeof(T) / 2;            // 16-byte pieces of eight elements
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
+
+// Eight elements from 16-byte pieces, `apart` bytes from one another in shared memory / side by side in global memory
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4 (&w)[PIECES<T>], float (&v)[8])
+{
+    const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { v[2 * k] = __uint_as_float(u[k] << 16); v[2 * k + 1] = __uint_as_float(u[k] & 0xFFFF0000u); }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(u[k]);
+    }
+}
+template <typename T>
+__device__ __forceinline__ void load_staged(const uint8_t* at, int apart, float (&v)[8])
+{
+    uint4 w[PIECES<T>];
+#pragma unroll
+    for (int p = 0; p < PIECES<T>; ++p) w[p] = *reinterpret_cast<const uint4*>(at + p * apart);
+    unpack<T>(w, v);
+}
+// Rounds to T; v becomes the rounded values
+template <typename T>
+__device__ __forceinline__ void store8(T* to, float (&v)[8])
+{
+    uint4* out = reinterpret_cast<uint4*>(to);
+    if constexpr (sizeof(T) == 2) {
+        uint32_t u[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+            u[k] = *reinterpret_cast<const uint32_t*>(&b);
+            v[2 * k] = __uint_as_float(u[k] << 16);
+            v[2 * k + 1] = __uint_as_float(u[k] & 0xFFFF0000u);
+        }
+        out[0] = make_uint4(u[0], u[1], u[2], u[3]);
+    } else {
+        out[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        out[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    }
+}
+// Eight weights of a row of parameters; they stay in L1 from row to row
+__device__ __forceinline__ void params8(const void* p, int64_t at, bool bf16, float (&v)[8])
+{
+    if (bf16) {
+        const uint4 w[1] = {__ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + at))};
+        unpack<__nv_bfloat16>(w, v);
+    } else {
+        const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + at);
+        const uint4 w[2] = {__ldg(q), __ldg(q + 1)};
+        unpack<float>(w, v);
+    }
+}
+
+// Forward.  WARP: rows of a warp each (the CTA has four), else of the CTA.
+template <typename Y, typename H, int NV, bool WARP, int STAGES>
+__global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : 512), WARP ? 8 : (NV == 1 ? 1 : 2)) seam_forward_kernel(const SeamArgs a)
+{
+    extern __shared__ __align__(16) uint8_t stage_mem[];
+    __shared__ float area[2][SEAM_MAX_WARPS][1];
+    constexpr int Q = PIECES<Y> + PIECES<H>;                // 16-byte pieces of a vector of both inputs
+    int turn = 0;
+    const int T = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x;
+    const int64_t first = WARP ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x, step = WARP ? (int64_t)gridDim.x * 4 : gridDim.x;
+    const int piece = blockDim.x * 16;                      // bytes from a piece to the next one of the same thread
+    uint8_t* mine = stage_mem + threadIdx.x * 16;
+    const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
+    const float n_cols = (float)a.cols;
+    auto issue = [&](int64_t r, int stage) {
+        if (r < a.rows) {
+            const Y* y = static_cast<const Y*>(a.y) + r * a.cols;
+            const H* h_in = static_cast<const H*>(a.h_in) + r * a.cols;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * T) * 8;
+                if (c >= a.cols) break;
+                const uint32_t to = mine_at + (stage * NV + i) * Q * piece;
+#pragma unroll
+                for (int p = 0; p < PIECES<Y>; ++p) copy16(to + p * piece, reinterpret_cast<const uint4*>(y + c) + p);
+#pragma unroll
+                for (int p = 0; p < PIECES<H>; ++p) copy16(to + (PIECES<Y> + p) * piece, reinterpret_cast<const uint4*>(h_in + c) + p);
+            }
+        }
+        copies_issued();
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) issue(first + s * step, s);
+    int stage = 0;
+    for (int64_t r = first; r < a.rows; r += step) {
+        issue(r + (STAGES - 1) * step, (stage + STAGES - 1) % STAGES);
+        copies_done<STAGES - 1>();
+        const uint8_t* at = mine + stage * NV * Q * piece;
+        float s[1] = {0.f}, rp = 1.f;
+        if (a.gamma_post) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if ((t + i * T) * 8 >= a.cols) break;
+                float y[8];
+                load_staged<Y>(at + i * Q * piece, piece, y);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s[0] = fmaf(y[k], y[k], s[0]);
+            }
+            if constexpr (WARP) warp_sums(s);
+            else cta_sums(s, area, turn);
+            rp = 1.0f / sqrtf(s[0] / n_cols + a.eps);
+            if (t == 0) a.rstd_post[r] = rp;
+        }
+        s[0] = 0.f;
+        float h[NV][8];
+        const int64_t gate = a.gate ? r / a.rows_per_gate * a.cols : 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (t + i * T) * 8;
+            if (c >= a.cols) break;
+            float n[8], w[8];
+            load_staged<Y>(at + i * Q * piece, piece, n);
+            load_staged<H>(at + (i * Q + PIECES<Y>) * piece, piece, h[i]);
+            if (a.gamma_post) {
+                params8(a.gamma_post, c, a.bf16_params, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) n[k] = (n[k] * rp) * w[k];
+            }
+            if (a.gate) params8(a.gate, gate + c, a.bf16_params, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) h[i][k] = fmaf(a.gate ? a.branch_scale * w[k] : a.branch_scale, n[k], a.residual_scale * h[i][k]);
+            store8(static_cast<H*>(a.h) + r * a.cols + c, h[i]);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s[0] = fmaf(h[i][k], h[i][k], s[0]);
+        }
+        if constexpr (WARP) warp_sums(s);
+        else cta_sums(s, area, turn);
+        const float rn = 1.0f / sqrtf(s[0] / n_cols + a.eps);
+        if (t == 0) a.rstd_pre[r] = rn;
+        if (a.x) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * T) * 8;
+                if (c >= a.cols) break;
+                float w[8];
+                params8(a.gamma_pre, c, a.bf16_params, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) h[i][k] = (h[i][k] * rn) * w[k];
+                store8(static_cast<Y*>(a.x) + r * a.cols + c, h[i]);
+            }
+        }
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    copies_done<0>();
+}
+
+// Backward: same ownership and the same sums as seam_grad_any_kernel; column sums stay in registers.
+template <typename Y, typename H, int NV, int STAGES>
+__global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 2 : 1) seam_grad_kernel(const SeamArgs a)
+{
+    extern __shared__ __align__(16) uint8_t stage_mem[];
+    __shared__ float area[2][SEAM_MAX_WARPS][3];
+    constexpr int Q = 2 * (PIECES<Y> + PIECES<H>);          // dx, y, dh, h
+    constexpr int AT_Y = PIECES<Y>, AT_DH = 2 * PIECES<Y>, AT_H = 2 * PIECES<Y> + PIECES<H>;
+    int turn = 0;
+    const int T = blockDim.x, t = threadIdx.x, piece = T * 16;
+    uint8_t* mine = stage_mem + t * 16;
+    const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
+    const int64_t r0 = blockIdx.x * a.chunk, r1 = min(r0 + a.chunk, a.rows);
+    const float inv_cols = 1.0f / (float)a.cols;
+    auto fetch = [&](uint32_t to, const auto* from) {
+#pragma unroll
+        for (int p = 0; p < PIECES<std::remove_cv_t<std::remove_reference_t<decltype(*from)>>>; ++p)
+            copy16(to + p * piece, reinterpret_cast<const uint4*>(from) + p);
+    };
+    auto issue = [&](int64_t r, int stage) {
+        if (r < r1)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * T) * 8;
+                if (c >= a.cols) break;
+                const uint32_t to = mine_at + (stage * NV + i) * Q * piece;
+                const int64_t at = r * a.cols + c;
+                if (a.dx) fetch(to, static_cast<const Y*>(a.dx) + at);
+                fetch(to + AT_Y * piece, static_cast<const Y*>(a.y) + at);
+                if (a.dh) fetch(to + AT_DH * piece, static_cast<const H*>(a.dh) + at);
+                fetch(to + AT_H * piece, static_cast<const H*>(static_cast<const void*>(a.h)) + at);
+            }
+        copies_issued();
+    };
+    float pre[NV][8], post[NV][8], gates[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) pre[i][k] = post[i][k] = gates[i][k] = 0.f;
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) issue(r0 + s, s);
+    int stage = 0;
+    for (int64_t r = r0; r < r1; ++r) {
+        issue(r + STAGES - 1, (stage + STAGES - 1) % STAGES);
+        const int64_t g = a.gate ? r / a.rows_per_gate : 0;
+        const float rn = a.rstd_pre[r], rp = a.gamma_post ? a.rstd_post[r] : 1.f;
+        copies_done<STAGES - 1>();
+        const uint8_t* at = mine + stage * NV * Q * piece;
+        auto zero = [](float (&v)[8]) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = 0.f;
+        };
+        float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (t + i * T) * 8;
+            if (c >= a.cols) break;
+            const uint8_t* from = at + i * Q * piece;
+            float xh[8], d[8], w[8];
+            load_staged<H>(from + AT_H * piece, piece, xh);
+            if (a.dx) {
+                load_staged<Y>(from, piece, d);
+                params8(a.gamma_pre, c, a.bf16_params, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) d[k] *= w[k];
+            } else zero(d);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                xh[k] *= rn;
+                s[0] = fmaf(d[k], xh[k], s[0]);
+            }
+            if (a.gamma_post) {
+                float q[8];
+                params8(a.gamma_post, c, a.bf16_params, w);
+                if (a.gate) {
+                    params8(a.gate, g * a.cols + c, a.bf16_params, q);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) w[k] *= q[k];
+                }
+                load_staged<Y>(from + AT_Y * piece, piece, q);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[k] *= q[k];
+                if (a.dh) load_staged<H>(from + AT_DH * piece, piece, q);
+                else zero(q);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    s[1] = fmaf(w[k], fmaf(rn, d[k], q[k]), s[1]);
+                    s[2] = fmaf(w[k], xh[k], s[2]);
+                }
+            }
+        }
+        cta_sums(s, area, turn);
+        const float scale = a.branch_scale * rp;                    // of the last two sums' terms
+        const float c1 = s[0] * inv_cols, c2 = (s[1] - rn * c1 * s[2]) * scale * inv_cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (t + i * T) * 8;
+            if (c >= a.cols) break;
+            const uint8_t* from = at + i * Q * piece;
+            const int64_t to = r * a.cols + c;
+            float G[8], v[8], w[8];
+            load_staged<H>(from + AT_H * piece, piece, v);
+            if (a.dx) {
+                load_staged<Y>(from, piece, G);
+                params8(a.gamma_pre, c, a.bf16_params, w);
+            } else {
+                zero(G);
+                zero(w);
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float xh = v[k] * rn;
+                pre[i][k] = fmaf(G[k], xh, pre[i][k]);
+                v[k] = fmaf(G[k], w[k], -xh * c1);
+            }
+            if (a.dh) load_staged<H>(from + AT_DH * piece, piece, G);
+            else zero(G);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                G[k] = fmaf(rn, v[k], G[k]);
+                v[k] = a.residual_scale * G[k];
+                G[k] *= a.branch_scale;
+            }
+            if (a.dh_in) store8(static_cast<H*>(a.dh_in) + to, v);
+            load_staged<Y>(from + AT_Y * piece, piece, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= rp;
+            if (a.gamma_post) params8(a.gamma_post, c, a.bf16_params, w);
+            if (a.d_gate)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) gates[i][k] = fmaf(G[k], a.gamma_post ? v[k] * w[k] : v[k], gates[i][k]);
+            if (a.gate) {
+                float q[8];
+                params8(a.gate, g * a.cols + c, a.bf16_params, q);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) G[k] *= q[k];
+            }
+            if (a.gamma_post)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    post[i][k] = fmaf(G[k], v[k], post[i][k]);
+                    G[k] = rp * fmaf(G[k], w[k], -v[k] * c2);
+                }
+            if (a.dy) store8(static_cast<Y*>(a.dy) + to, G);
+        }
+        if (a.d_gate && (r + 1 == r1 || (r + 1) / a.rows_per_gate != g)) {
+            float* part = gate_part(a, g);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * T) * 8;
+                if (c >= a.cols) break;
+                store8(part + c, gates[i]);
+                zero(gates[i]);
+            }
+        }
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    copies_done<0>();
+    float* to = a.ws + (int64_t)blockIdx.x * a.cols;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (t + i * T) * 8;
+        if (c >= a.cols) break;
+        if (a.d_gamma_pre) store8(to + c, pre[i]);
+        if (a.d_gamma_post) store8(to + (a.d_gamma_pre ? (int64_t)gridDim.x * a.cols : 0) + c, post[i]);
+    }
 }
 
 // Joins the CTAs' sums.  blockIdx.y: 0 / 1 the weights, then the rows of the gate that several CTAs hold.
@@ -262,33 +600,88 @@ cudaError_t by_types(const mxfp8_seam* s, F f)
     return s->stream_dtype == MXFP8_BF16 ? f((float*)nullptr, (B*)nullptr) : f((float*)nullptr, (float*)nullptr);
 }
 
-template <typename Y, typename H>
-cudaError_t launch_forward(const SeamArgs& a, cudaStream_t st)
+// Rows on 16-byte boundaries everywhere
+template <typename... P>
+bool rows_aligned(const SeamArgs& a, const P*... p)
 {
-    const int64_t most = (int64_t)multiprocessors() * 8;
-    seam_forward_any_kernel<Y, H><<<(unsigned)(a.rows < most ? a.rows : most), SEAM_THREADS, 0, st>>>(a);
+    return a.cols % 8 == 0 && (aligned16(p) && ...) && aligned16(a.gamma_post) && aligned16(a.gate) && aligned16(a.gamma_pre);
+}
+
+constexpr int SMEM_PER_SM = 224 * 1024;
+
+template <typename Y, typename H, int NV, bool WARP, int STAGES>
+cudaError_t launch_forward_rows(const SeamArgs& a, int threads, cudaStream_t st)
+{
+    auto kernel = seam_forward_kernel<Y, H, NV, WARP, STAGES>;
+    const int smem = STAGES * NV * (PIECES<Y> + PIECES<H>) * 16 * threads;
+    static unsigned long long set = 0;
+    const cudaError_t err = ensure_dynamic_smem(kernel, SMEM_PER_SM, set);
+    if (err != cudaSuccess) return err;
+    const int by_threads = 1024 / threads, by_smem = SMEM_PER_SM / (smem + 1024), per_sm = by_threads < by_smem ? by_threads : by_smem;
+    const int64_t groups = WARP ? (a.rows + 3) / 4 : a.rows, most = (int64_t)multiprocessors() * (per_sm < 1 ? 1 : per_sm);
+    kernel<<<(unsigned)(groups < most ? groups : most), threads, smem, st>>>(a);
     count_launch(1);
     return cudaGetLastError();
 }
 
-// CTAs of the backward pass and their rows: two per multiprocessor while a row remains for each.
-int64_t grad_chunk(int64_t rows)
+template <typename Y, typename H>
+cudaError_t launch_forward(const SeamArgs& a, cudaStream_t st)
 {
-    const int64_t ctas = 2 * (int64_t)multiprocessors();
+    if (!rows_aligned(a, a.y, a.h_in, a.h, a.x)) {
+        const int64_t most = (int64_t)multiprocessors() * 8;
+        seam_forward_any_kernel<Y, H><<<(unsigned)(a.rows < most ? a.rows : most), SEAM_THREADS, 0, st>>>(a);
+        count_launch(1);
+        return cudaGetLastError();
+    }
+    const int vectors = a.cols / 8, warps = (vectors + 31) / 32;
+    if (warps == 1) return launch_forward_rows<Y, H, 1, true, 4>(a, 128, st);
+    if (warps <= 4 && a.rows >= 8 * multiprocessors())
+        return warps <= 2 ? launch_forward_rows<Y, H, 2, true, 3>(a, 128, st) : launch_forward_rows<Y, H, 4, true, 3>(a, 128, st);
+    if (a.rows <= multiprocessors() && warps <= 32) return launch_forward_rows<Y, H, 1, false, 2>(a, 32 * warps, st);
+    if (warps <= 32) return launch_forward_rows<Y, H, 2, false, 3>(a, 32 * ((warps + 1) / 2), st);
+    // 16384 columns of two FP32 inputs leave room for one row at a time
+    return launch_forward_rows<Y, H, 4, false, PIECES<Y> + PIECES<H> == 4 ? 1 : 2>(a, 32 * ((warps + 3) / 4), st);
+}
+
+// Rows of a CTA of the backward pass: two to eight CTAs per multiprocessor, by the width, while a row remains for each.
+int64_t grad_chunk(int64_t rows, int64_t cols)
+{
+    const int64_t per_sm = cols > 4096 ? 2 : (cols > 1024 ? 8192 / cols : 8), ctas = per_sm * multiprocessors();
     return (rows + ctas - 1) / ctas;
+}
+
+template <typename Y, typename H, int NV, int STAGES>
+cudaError_t launch_grad_rows(const SeamArgs& a, int threads, unsigned ctas, cudaStream_t st)
+{
+    auto kernel = seam_grad_kernel<Y, H, NV, STAGES>;
+    static unsigned long long set = 0;
+    const cudaError_t err = ensure_dynamic_smem(kernel, SMEM_PER_SM, set);
+    if (err != cudaSuccess) return err;
+    kernel<<<ctas, threads, STAGES * NV * 2 * (PIECES<Y> + PIECES<H>) * 16 * threads, st>>>(a);
+    return cudaGetLastError();
 }
 
 template <typename Y, typename H>
 cudaError_t launch_grad(SeamArgs a, cudaStream_t st)
 {
     const unsigned ctas = (unsigned)((a.rows + a.chunk - 1) / a.chunk);
-    auto kernel = seam_grad_any_kernel<Y, H>;
-    static unsigned long long set = 0;
-    const cudaError_t err = ensure_dynamic_smem(kernel, 3 * SEAM_MAX_COLS * (int)sizeof(float), set);
-    if (err != cudaSuccess) return err;
-    kernel<<<ctas, SEAM_THREADS, 3 * a.cols * sizeof(float), st>>>(a);
+    cudaError_t rc;
+    // a row of the four inputs has to fit shared memory (it does but for rows of 16384 FP32 numbers)
+    if (rows_aligned(a, a.dx, a.dh, a.y, a.h, a.dy, a.dh_in, a.d_gate) && a.cols * 2 * (int)(sizeof(Y) + sizeof(H)) <= SMEM_PER_SM) {
+        constexpr bool WIDE = PIECES<Y> + PIECES<H> == 4;
+        const int warps = (a.cols / 8 + 31) / 32;
+        if (warps <= 8) rc = launch_grad_rows<Y, H, 1, 3>(a, 32 * warps, ctas, st);
+        else if (warps <= (WIDE ? 24 : 32)) rc = launch_grad_rows<Y, H, 2, 2>(a, 32 * ((warps + 1) / 2), ctas, st);
+        else rc = launch_grad_rows<Y, H, 4, 1>(a, 32 * ((warps + 3) / 4), ctas, st);
+    } else {
+        auto kernel = seam_grad_any_kernel<Y, H>;
+        static unsigned long long set = 0;
+        const cudaError_t err = ensure_dynamic_smem(kernel, 3 * SEAM_MAX_COLS * (int)sizeof(float), set);
+        if (err != cudaSuccess) return err;
+        kernel<<<ctas, SEAM_THREADS, 3 * a.cols * sizeof(float), st>>>(a);
+        rc = cudaGetLastError();
+    }
     count_launch(1);
-    cudaError_t rc = cudaGetLastError();
     const int64_t joins = (a.d_gamma_pre != nullptr) + (a.d_gamma_post != nullptr) + (a.d_gate ? a.gates : 0);
     if (rc != cudaSuccess || joins == 0) return rc;
     seam_join_kernel<<<dim3((a.cols + JOIN_COLS - 1) / JOIN_COLS, (unsigned)(joins < 1024 ? joins : 1024)), 32 * JOIN_WARPS, 0, st>>>(a, (int)ctas);
@@ -351,7 +744,7 @@ extern "C" size_t mxfp8_residual_rmsnorm_grad_ws_bytes(const mxfp8_seam* seam)
 {
     if (seam_check(seam) != MXFP8_OK) return 0;
     const SeamArgs a = seam_args(seam);
-    const int64_t chunk = grad_chunk(a.rows), ctas = (a.rows + chunk - 1) / chunk;
+    const int64_t chunk = grad_chunk(a.rows, a.cols), ctas = (a.rows + chunk - 1) / chunk;
     const int64_t parts = ctas * (1 + (seam->gamma_post != nullptr)) + (seam->gate ? ctas + a.gates : 0);
     return (size_t)parts * (size_t)a.cols * sizeof(float);
 }
@@ -374,7 +767,7 @@ extern "C" int mxfp8_residual_rmsnorm_grad(const mxfp8_seam* seam, const void* d
     a.rstd_post = const_cast<float*>(rstd_post); a.rstd_pre = const_cast<float*>(rstd_pre);
     a.dy = dy; a.dh_in = dh_in; a.d_gamma_pre = d_gamma_pre; a.d_gamma_post = d_gamma_post; a.d_gate = d_gate;
     a.ws = static_cast<float*>(ws);
-    a.chunk = grad_chunk(a.rows);
+    a.chunk = grad_chunk(a.rows, a.cols);
     const cudaError_t err = by_types(seam, [&](auto* yt, auto* ht) {
         return launch_grad<std::remove_pointer_t<decltype(yt)>, std::remove_pointer_t<decltype(ht)>>(a, static_cast<cudaStream_t>(stream));
     });
