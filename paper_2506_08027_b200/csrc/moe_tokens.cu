@@ -10,7 +10,7 @@ namespace mxfp8 {
 namespace {
 
 constexpr int MOE_MAX_TOKENS = 64, MOE_MAX_EXPERTS = 256, MOE_MAX_TOP_K = 16;
-constexpr int MOE_WARPS = 8, MOE_THREADS = 32 * MOE_WARPS;
+constexpr int MOE_MAX_ROWS = MOE_MAX_TOKENS * MOE_MAX_TOP_K, MOE_MAX_ENTRIES = MOE_MAX_EXPERTS + MOE_MAX_ROWS / 8;
 
 struct MoeArgs {
     const __nv_bfloat16* x;          // [tokens, cols]
@@ -20,17 +20,24 @@ struct MoeArgs {
     bool bf16_out;
     int32_t* ids;
     float* weights;
-    __nv_bfloat16 *m_hi, *m_lo;      // [slots, inner]: m = m_hi + m_lo
+    __nv_bfloat16 *m_hi, *m_lo;      // [rows, inner]: m = m_hi + m_lo; rows: the chosen (token, expert) pairs by expert, then token
     int tokens, experts, top_k, act, renormalize;
     int cols, inner;
     int col_tiles, inner_tiles;      // column tiles of gate_up and of down
+    uint32_t pairs_magic;            // of inner / 16
 };
 
-// What a CTA knows of the choice.
+// What a CTA knows of the choice: rows of m by expert, and entries, each the rows (a few at most) of one expert.
 struct Choice {
-    float weight[MOE_MAX_TOKENS * MOE_MAX_TOP_K];
-    short expert[MOE_MAX_TOKENS * MOE_MAX_TOP_K];         // -1: none
-    uint32_t used[MOE_MAX_EXPERTS / 32];                  // one bit per expert
+    uint32_t who[MOE_MAX_EXPERTS][2];                     // one bit per token that chose the expert
+    float share[MOE_MAX_ROWS];                            // by slot, later (weight) by row
+    float weight[MOE_MAX_ROWS];
+    short expert[MOE_MAX_ROWS];                           // by slot; -1: none
+    short first[MOE_MAX_EXPERTS];                         // first row of an expert
+    uint8_t token[MOE_MAX_ROWS];                          // by row
+    short entry_expert[MOE_MAX_ENTRIES], entry_row[MOE_MAX_ENTRIES];
+    uint8_t entry_rows[MOE_MAX_ENTRIES];
+    int entries;
 };
 
 // Unsigned numbers in the order of the logits; 0 for one that is never chosen (-Inf, NaN).  Both zeros are equal.
@@ -44,82 +51,91 @@ __device__ __forceinline__ float logit_of(uint32_t o) { return __uint_as_float((
 // exp(l - top), with equal infinities at the top counting as equal
 __device__ __forceinline__ float share_of(uint32_t o, uint32_t top) { return o == top ? 1.f : expf(logit_of(o) - logit_of(top)); }
 
-// Chooses for all tokens, a warp for each in turn: top_k rounds of the largest remaining logit (the lowest expert among equals).
-// Ends with a barrier.
-__device__ __forceinline__ void choose(const MoeArgs& a, Choice& choice)
+// Chooses for all tokens, a warp for each in turn: top_k rounds of the largest remaining logit (the lowest expert among equals).  Then
+// orders the pairs by expert and cuts every expert's rows into entries of at most `most`.  Ends with a barrier.
+__device__ __forceinline__ void choose(const MoeArgs& a, Choice& choice, int most)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    if (threadIdx.x < MOE_MAX_EXPERTS / 32) choice.used[threadIdx.x] = 0u;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+    constexpr int I = MOE_MAX_EXPERTS / 32;
+    for (int e = tid; e < MOE_MAX_EXPERTS; e += blockDim.x) choice.who[e][0] = choice.who[e][1] = 0u;
     __syncthreads();
     for (int t = warp; t < a.tokens; t += warps) {
-        uint32_t left[MOE_MAX_EXPERTS / 32];
+        uint32_t left[I];
 #pragma unroll
-        for (int i = 0; i < MOE_MAX_EXPERTS / 32; ++i)
-            left[i] = lane + 32 * i < a.experts ? order_of(a.logits[t * a.experts + lane + 32 * i]) : 0u;
+        for (int i = 0; i < I; ++i) left[i] = lane + 32 * i < a.experts ? order_of(a.logits[t * a.experts + lane + 32 * i]) : 0u;
         uint32_t top = 0u;
         float mine = 0.f, total = 0.f;               // lane j: the share of choice j
         for (int j = 0; j < a.top_k; ++j) {
             uint32_t best = 0u;
             int at = 0;
 #pragma unroll
-            for (int i = 0; i < MOE_MAX_EXPERTS / 32; ++i)
+            for (int i = 0; i < I; ++i)
                 if (left[i] > best) { best = left[i]; at = lane + 32 * i; }
-            const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, best);
-            const int expert = (int)__reduce_min_sync(0xFFFFFFFFu, best == most ? (uint32_t)at : 0xFFFFu);
+            const uint32_t peak = __reduce_max_sync(0xFFFFFFFFu, best);
+            const int expert = (int)__reduce_min_sync(0xFFFFFFFFu, best == peak ? (uint32_t)at : 0xFFFFu);
             if (j == 0) {
-                top = most;
+                top = peak;
                 if (!a.renormalize && top != 0u) {
 #pragma unroll
-                    for (int i = 0; i < MOE_MAX_EXPERTS / 32; ++i)
+                    for (int i = 0; i < I; ++i)
                         if (left[i] != 0u) total += share_of(left[i], top);
 #pragma unroll
                     for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, off);
                 }
             }
-            const float share = most != 0u ? share_of(most, top) : 0.f;
+            const float share = peak != 0u ? share_of(peak, top) : 0.f;
             if (a.renormalize) total += share;
             if (lane == j) {
                 mine = share;
-                choice.expert[t * a.top_k + j] = (short)(most != 0u ? expert : -1);
-                if (most != 0u) atomicOr(&choice.used[expert >> 5], 1u << (expert & 31));
+                choice.expert[t * a.top_k + j] = (short)(peak != 0u ? expert : -1);
+                if (peak != 0u) atomicOr(&choice.who[expert][t >> 5], 1u << (t & 31));
             }
 #pragma unroll
-            for (int i = 0; i < MOE_MAX_EXPERTS / 32; ++i)
-                if (most != 0u && lane + 32 * i == expert) left[i] = 0u;
+            for (int i = 0; i < I; ++i)
+                if (peak != 0u && lane + 32 * i == expert) left[i] = 0u;
         }
-        if (lane < a.top_k) choice.weight[t * a.top_k + lane] = mine > 0.f ? mine / total : 0.f;
+        if (lane < a.top_k) choice.share[t * a.top_k + lane] = mine > 0.f ? mine / total : 0.f;
     }
     __syncthreads();
-}
-
-// The u-th used expert, or -1.
-__device__ __forceinline__ int used_expert(const Choice& choice, int u)
-{
-    for (int w = 0; w < MOE_MAX_EXPERTS / 32; ++w) {
-        uint32_t bits = choice.used[w];
-        const int n = __popc(bits);
-        if (u < n) {
-            for (; u > 0; --u) bits &= bits - 1u;
-            return 32 * w + __ffs(bits) - 1;
+    if (warp == 0) {                                  // first rows and entries, eight experts to a lane
+        int rows = 0, entries = 0;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int n = __popc(choice.who[lane * I + i][0]) + __popc(choice.who[lane * I + i][1]);
+            rows += n;
+            entries += (n + most - 1) / most;
         }
-        u -= n;
+        int before_rows = rows, before_entries = entries;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int r = __shfl_up_sync(0xFFFFFFFFu, before_rows, off), e = __shfl_up_sync(0xFFFFFFFFu, before_entries, off);
+            if (lane >= off) { before_rows += r; before_entries += e; }
+        }
+        if (lane == 31) choice.entries = before_entries;
+        before_rows -= rows;
+        before_entries -= entries;
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int e = lane * I + i, n = __popc(choice.who[e][0]) + __popc(choice.who[e][1]);
+            choice.first[e] = (short)before_rows;
+            for (int r = 0; r < n; r += most) {
+                choice.entry_expert[before_entries] = (short)e;
+                choice.entry_row[before_entries] = (short)(before_rows + r);
+                choice.entry_rows[before_entries++] = (uint8_t)min(most, n - r);
+            }
+            before_rows += n;
+        }
     }
-    return -1;
-}
-
-// The slots that chose an expert, ascending, by one warp; returns their number.
-__device__ __forceinline__ int slots_of(const MoeArgs& a, const Choice& choice, int expert, short* list)
-{
-    const int lane = threadIdx.x & 31, slots = a.tokens * a.top_k;
-    int found = 0;
-    for (int base = 0; base < slots; base += 32) {
-        const bool hit = base + lane < slots && choice.expert[base + lane] == expert;
-        const unsigned hits = __ballot_sync(0xFFFFFFFFu, hit);
-        if (hit) list[found + __popc(hits & ((1u << lane) - 1u))] = (short)(base + lane);
-        found += __popc(hits);
+    __syncthreads();
+    for (int s = tid; s < a.tokens * a.top_k; s += blockDim.x) {
+        const int e = choice.expert[s], t = s / a.top_k;
+        if (e < 0) continue;
+        const uint32_t below = (1u << (t & 31)) - 1u;
+        const int row = choice.first[e] + (t < 32 ? __popc(choice.who[e][0] & below) : __popc(choice.who[e][0]) + __popc(choice.who[e][1] & below));
+        choice.token[row] = (uint8_t)t;
+        choice.weight[row] = choice.share[s];
     }
-    __syncwarp();
-    return found;
+    __syncthreads();
 }
 
 __device__ __forceinline__ float activate(float x, int act)
@@ -133,128 +149,295 @@ __device__ __forceinline__ float activate(float x, int act)
     }
 }
 
-// Products of one warp's column tiles (every `step`-th from `first`) with R row tiles, for up to 8 NT rows of `from`.
-template <int R, int NT>
-__device__ __forceinline__ void run_products(const uint8_t* const (&tile)[R], const __nv_bfloat16* const (&from)[NT], const bool (&has)[NT],
-                                             int cols, int col_tiles, int first, int step, float (&acc)[R][NT][4])
+// A warp's ring of weight tiles in shared memory: R tiles (one column tile of R row tiles) to a stage, copied asynchronously by the warp's own
+// lanes STAGES - 1 steps ahead.  Nothing but the warp's own copies and __syncwarp guards them.
+__device__ __forceinline__ void copy_tile(uint32_t to, const uint8_t* tile, int lane)
 {
-    const int lane = threadIdx.x & 31, quarter = lane & 3;
+    const uint8_t* from = tile + lane * 16;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + lane * 16), "l"(from) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + lane * 16 + 512), "l"(from + 512) : "memory");
+    if (lane < 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + lane * 16 + 1024), "l"(from + 1024) : "memory");
+}
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
+
+template <int R, int NT>
+__device__ __forceinline__ void read_tiles(Operands<R, NT>& o, const uint8_t* stage, int lane)
+{
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint8_t* tile = stage + r * TILE_BYTES;
+        o.lo[r] = *reinterpret_cast<const uint4*>(tile + lane * 16);
+        o.hi[r] = *reinterpret_cast<const uint4*>(tile + lane * 16 + 512);
+        o.s_lo[r] = *reinterpret_cast<const uint32_t*>(tile + TILE_CODES + (lane >> 2) * 4);
+        o.s_hi[r] = *reinterpret_cast<const uint32_t*>(tile + TILE_CODES + (lane >> 2) * 4 + 32);
+    }
+}
+
+// Activations under column tile kt for rows `from` (null: none); columns behind the matrix are zeros
+template <int NT>
+__device__ __forceinline__ void read_rows(uint4 (&x)[NT][4], const __nv_bfloat16* const (&from)[NT], int kt, int cols, int lane)
+{
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int k = kt * TILE_COLS + g * 32;
+            x[t][g] = from[t] && k < cols ? *reinterpret_cast<const uint4*>(from[t] + k + (lane & 3) * 8) : make_uint4(0u, 0u, 0u, 0u);
+        }
+}
+
+template <int R, int NT>
+__device__ __forceinline__ void clear(float (&acc)[R][NT][4])
+{
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[r][t][i] = 0.f;
-    for (int kt = first; kt < col_tiles; kt += step) {
-        Operands<R, NT> o;
-        bool none[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) none[t] = false;
-        o.load(tile, (int64_t)kt * TILE_BYTES, from, none, 0, lane);
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int k = kt * TILE_COLS + g * 32;                  // columns behind the matrix are zeros
-                o.x[t][g] = has[t] && k < cols ? *reinterpret_cast<const uint4*>(from[t] + k + quarter * 8) : make_uint4(0u, 0u, 0u, 0u);
-            }
-        product<R, NT>(o, acc);
-    }
 }
 
-// CTA (p, u): rows 16 p .. of the gate and of the up projection of the u-th used expert.  Eight warps split the columns.
-__global__ void __launch_bounds__(MOE_THREADS) moe_gate_up_kernel(const MoeArgs a)
+// ---- first launch: units of 16 gate rows and the 16 up rows that belong to them, for the rows of one entry.  2^team warps share a
+// unit and split its columns; the teams of all CTAs take the units in turn.
+template <int NT, int WARPS, int STAGES>
+__global__ void __launch_bounds__(32 * WARPS, 1) moe_gate_up_kernel(const MoeArgs a)
 {
+    extern __shared__ __align__(16) uint8_t dynamic[];
     __shared__ Choice choice;
-    __shared__ short list[MOE_MAX_TOKENS];
-    __shared__ int listed;
-    __shared__ float sums[MOE_WARPS][2][TILE_ROWS][9];
-    choose(a, choice);
+    constexpr int P = 8 * NT + 1, WARP_SUMS = 2 * TILE_ROWS * P, STAGE = 2 * TILE_BYTES;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the second launch may choose, and fetch weights, beside this one
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (blockIdx.x == 0 && blockIdx.y == 0)
-        for (int s = tid; s < a.tokens * a.top_k; s += MOE_THREADS) {
+    uint8_t* ring = dynamic + warp * STAGES * STAGE;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    float* sums = reinterpret_cast<float*>(dynamic + WARPS * STAGES * STAGE);
+    choose(a, choice, 8 * NT);
+    if (blockIdx.x == 0)
+        for (int s = tid; s < a.tokens * a.top_k; s += 32 * WARPS) {
             if (a.ids) a.ids[s] = choice.expert[s];
-            if (a.weights) a.weights[s] = choice.weight[s];
+            if (a.weights) a.weights[s] = choice.share[s];
         }
-    const int expert = used_expert(choice, blockIdx.y);
-    if (expert < 0) return;
-    if (warp == 0) {
-        const int n = slots_of(a, choice, expert, list);
-        if (lane == 0) listed = n;
+    const int pairs = a.inner / TILE_ROWS, units = choice.entries * pairs, ctas = gridDim.x;
+    // the fewest steps for the team that has most: rounds of units times (column tiles of a warp + about two for the joining of the sums)
+    int team = 0;
+    for (int l = 0, least = 0x7FFFFFFF; (1 << l) <= WARPS; ++l) {
+        const int teams = ctas * (WARPS >> l), rounds = (units + teams - 1) / teams, cost = rounds * (((a.col_tiles + (1 << l) - 1) >> l) + 2);
+        if (cost < least) { least = cost; team = l; }
     }
-    __syncthreads();
-    const int pairs = a.inner / TILE_ROWS, count = listed;
-    const uint8_t* matrix = a.gate_up + (int64_t)expert * 2 * pairs * a.col_tiles * TILE_BYTES + lane * 16;
-    const uint8_t* tile[2] = {matrix + (int64_t)blockIdx.x * a.col_tiles * TILE_BYTES, matrix + (int64_t)(pairs + blockIdx.x) * a.col_tiles * TILE_BYTES};
-    for (int s0 = 0; s0 < count; s0 += 8) {
-        const bool has[1] = {s0 + (lane >> 2) < count};
-        const __nv_bfloat16* from[1] = {a.x + (int64_t)(has[0] ? list[s0 + (lane >> 2)] / a.top_k : 0) * a.cols};
-        float acc[2][1][4];
-        run_products<2, 1>(tile, from, has, a.cols, a.col_tiles, warp, MOE_WARPS, acc);
+    const int size = 1 << team, part = warp & (size - 1), unit0 = (warp >> team) * ctas + blockIdx.x, step = ctas * (WARPS >> team);
+    auto tile_of = [&](int unit) {
+        int v, p;
+        divmod((uint32_t)unit, (uint32_t)pairs, a.pairs_magic, v, p);
+        return a.gate_up + ((int64_t)choice.entry_expert[v] * 2 * pairs + p) * a.col_tiles * TILE_BYTES;
+    };
+    const int64_t to_up = (int64_t)pairs * a.col_tiles * TILE_BYTES;
+    // what is fetched next
+    int f_unit = unit0, f_kt = part, f_stage = 0;
+    const uint8_t* f_tile = unit0 < units ? tile_of(unit0) : nullptr;
+    auto fetch = [&]() {
+        while (f_unit < units && f_kt >= a.col_tiles) {
+            f_unit += step;
+            f_kt = part;
+            if (f_unit < units) f_tile = tile_of(f_unit);
+            if (part >= a.col_tiles) { f_unit = units; break; }             // this warp has no column tiles
+        }
+        if (f_unit < units) {
+            const uint8_t* from = f_tile + (int64_t)f_kt * TILE_BYTES;
+            copy_tile(ring_at + f_stage * STAGE, from, lane);
+            copy_tile(ring_at + f_stage * STAGE + TILE_BYTES, from + to_up, lane);
+            f_kt += size;
+        }
+        copies_issued();
+        f_stage = f_stage + 1 == STAGES ? 0 : f_stage + 1;
+    };
+#pragma unroll 1
+    for (int s = 0; s < STAGES - 1; ++s) fetch();
+    int stage = 0;
+    float* my_sums = sums + warp * WARP_SUMS;
+    const float* team_sums = sums + (warp - part) * WARP_SUMS;
+    for (int unit = unit0; unit < units; unit += step) {
+        int v, p;
+        divmod((uint32_t)unit, (uint32_t)pairs, a.pairs_magic, v, p);
+        const int row0 = choice.entry_row[v], rows = choice.entry_rows[v];
+        const __nv_bfloat16* from[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int i = 8 * t + (lane >> 2);
+            from[t] = i < rows ? a.x + (int64_t)choice.token[row0 + i] * a.cols : nullptr;
+        }
+        float acc[2][NT][4];
+        clear(acc);
+        for (int kt = part; kt < a.col_tiles; kt += size) {
+            Operands<2, NT> o;
+            read_rows<NT>(o.x, from, kt, a.cols, lane);
+            copies_done<STAGES - 2>();
+            __syncwarp();
+            fetch();
+            read_tiles(o, ring + stage * STAGE, lane);
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
+            product<2, NT>(o, acc);
+        }
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sums[warp][r][(lane >> 2) + 8 * (i >> 1)][2 * (lane & 3) + (i & 1)] = acc[r][0][i];
-        __syncthreads();
-        if (tid < 8 * TILE_ROWS && s0 + (tid >> 4) < count) {
-            const int n = tid & 15, s = tid >> 4;
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) my_sums[(r * TILE_ROWS + (lane >> 2) + 8 * (i >> 1)) * P + 8 * t + 2 * (lane & 3) + (i & 1)] = acc[r][t][i];
+        auto meet = [&]() {
+            if (team == 0) __syncwarp();
+            else asm volatile("bar.sync %0, %1;" :: "r"(1 + (warp >> team)), "r"(32 << team) : "memory");
+        };
+        meet();
+        for (int i = part * 32 + lane; i < rows * TILE_ROWS; i += 32 << team) {
+            const int n = i & (TILE_ROWS - 1), s = i >> 4;
             float g = 0.f, u = 0.f;
-            for (int w = 0; w < MOE_WARPS; ++w) {
-                g += sums[w][0][n][s];
-                u += sums[w][1][n][s];
+            for (int w = 0; w < size; ++w) {
+                g += team_sums[w * WARP_SUMS + n * P + s];
+                u += team_sums[w * WARP_SUMS + (TILE_ROWS + n) * P + s];
             }
             const float m = activate(g, a.act) * u;
             const __nv_bfloat16 hi = __float2bfloat16_rn(m);
-            const int64_t at = (int64_t)list[s0 + s] * a.inner + blockIdx.x * TILE_ROWS + n;
+            const int64_t at = (int64_t)(row0 + s) * a.inner + p * TILE_ROWS + n;
             a.m_hi[at] = hi;
             a.m_lo[at] = __float2bfloat16_rn(m - __bfloat162float(hi));
         }
-        __syncthreads();
+        meet();
     }
+    copies_done<0>();
 }
 
-// CTA p: rows 16 p .. of all used experts' down projections.  The warps split the columns; each holds the weighted sums of its
-// share for all tokens, and they are added at the end.
-__global__ void __launch_bounds__(MOE_THREADS) moe_down_kernel(const MoeArgs a)
+// ---- second launch: a CTA takes 16 rows of all entries' down projections at a time.  Its warps take the entries' column tiles in turn; each
+// holds the weighted sums of its share for all tokens, and they are added at the end.
+template <int NT, int WARPS, int STAGES>
+__global__ void __launch_bounds__(32 * WARPS, 1) moe_down_kernel(const MoeArgs a)
 {
-    extern __shared__ float total[];                     // [warp][token][row], rows padded to 17
+    extern __shared__ __align__(16) uint8_t dynamic[];
     __shared__ Choice choice;
-    __shared__ short list[MOE_WARPS][MOE_MAX_TOKENS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    for (int i = tid; i < MOE_WARPS * a.tokens * 17; i += MOE_THREADS) total[i] = 0.f;
-    choose(a, choice);
+    uint8_t* ring = dynamic + warp * STAGES * TILE_BYTES;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    float* total = reinterpret_cast<float*>(dynamic + WARPS * STAGES * TILE_BYTES);      // [warp][token][row], rows padded to 17
+    choose(a, choice, 8 * NT);
+    const int row_tiles = a.cols / TILE_ROWS, entries = choice.entries;
     float* mine = total + warp * a.tokens * 17;
-    const int row_tiles = (a.cols + TILE_ROWS - 1) / TILE_ROWS;
-    for (int w = 0; w < MOE_MAX_EXPERTS / 32; ++w)
-        for (uint32_t bits = choice.used[w]; bits != 0u; bits &= bits - 1u) {
-            const int expert = 32 * w + __ffs(bits) - 1;
-            const int count = slots_of(a, choice, expert, list[warp]);
-            const uint8_t* tile[1] = {a.down + ((int64_t)expert * row_tiles + blockIdx.x) * a.inner_tiles * TILE_BYTES + lane * 16};
-            for (int s0 = 0; s0 < count; s0 += 8) {
-                const bool in = s0 + (lane >> 2) < count, has[2] = {in, in};
-                const int64_t at = (int64_t)(in ? list[warp][s0 + (lane >> 2)] : 0) * a.inner;
-                const __nv_bfloat16* from[2] = {a.m_hi + at, a.m_lo + at};
-                float acc[1][2][4];
-                run_products<1, 2>(tile, from, has, a.inner, a.inner_tiles, warp, MOE_WARPS, acc);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int s = s0 + 2 * (lane & 3) + (i & 1);
-                    if (s < count) {
-                        float* to = mine + list[warp][s] / a.top_k * 17 + (lane >> 2) + 8 * (i >> 1);
-                        *to = fmaf(choice.weight[list[warp][s]], acc[0][0][i] + acc[0][1][i], *to);
-                    }
-                }
-                __syncwarp();
+    int f_rt = blockIdx.x, f_v = 0, f_kt = warp, f_stage = 0;
+    auto fetch = [&]() {
+        while (f_rt < row_tiles && f_kt >= a.inner_tiles) {                  // the warps go on where the entry before ended
+            f_kt -= a.inner_tiles;
+            if (++f_v >= entries) {
+                f_v = 0;
+                f_kt = warp;
+                f_rt += gridDim.x;
+                if (entries * a.inner_tiles <= warp) f_rt = row_tiles;       // nothing for this warp
             }
         }
-    __syncthreads();
-    for (int i = tid; i < a.tokens * TILE_ROWS; i += MOE_THREADS) {
-        const int n = i & 15, t = i >> 4, row = blockIdx.x * TILE_ROWS + n;
-        float v = 0.f;
-        for (int w = 0; w < MOE_WARPS; ++w) v += total[(w * a.tokens + t) * 17 + n];
-        if (a.bf16_out) static_cast<__nv_bfloat16*>(a.y)[(int64_t)t * a.cols + row] = __float2bfloat16_rn(v);
-        else static_cast<float*>(a.y)[(int64_t)t * a.cols + row] = v;
+        if (f_rt < row_tiles && entries > 0) {
+            copy_tile(ring_at + f_stage * TILE_BYTES, a.down + (((int64_t)choice.entry_expert[f_v] * row_tiles + f_rt) * a.inner_tiles + f_kt) * TILE_BYTES, lane);
+            f_kt += WARPS;
+        }
+        copies_issued();
+        f_stage = f_stage + 1 == STAGES ? 0 : f_stage + 1;
+    };
+#pragma unroll 1
+    for (int s = 0; s < STAGES - 1; ++s) fetch();
+    asm volatile("griddepcontrol.wait;" ::: "memory");                     // the first launch's m is there
+    int stage = 0;
+    for (int rt = blockIdx.x; rt < row_tiles; rt += gridDim.x) {
+        for (int i = lane; i < a.tokens * 17; i += 32) mine[i] = 0.f;
+        __syncwarp();
+        int kt = warp;
+        for (int v = 0; v < entries; ++v, kt -= a.inner_tiles) {
+            if (kt >= a.inner_tiles) continue;
+            const int row0 = choice.entry_row[v], rows = choice.entry_rows[v];
+            const __nv_bfloat16* from[2 * NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int i = 8 * t + (lane >> 2);
+                const int64_t at = (int64_t)(row0 + i) * a.inner;
+                from[t] = i < rows ? a.m_hi + at : nullptr;
+                from[NT + t] = i < rows ? a.m_lo + at : nullptr;
+            }
+            float acc[1][2 * NT][4];
+            clear(acc);
+            for (; kt < a.inner_tiles; kt += WARPS) {
+                Operands<1, 2 * NT> o;
+                read_rows<2 * NT>(o.x, from, kt, a.inner, lane);
+                copies_done<STAGES - 2>();
+                __syncwarp();
+                fetch();
+                read_tiles(o, ring + stage * TILE_BYTES, lane);
+                stage = stage + 1 == STAGES ? 0 : stage + 1;
+                product<1, 2 * NT>(o, acc);
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int s = 8 * t + 2 * (lane & 3) + (i & 1);
+                    if (s < rows) {
+                        float* to = mine + choice.token[row0 + s] * 17 + (lane >> 2) + 8 * (i >> 1);
+                        *to = fmaf(choice.weight[row0 + s], acc[0][t][i] + acc[0][NT + t][i], *to);
+                    }
+                }
+            __syncwarp();
+        }
+        __syncthreads();
+        for (int i = tid; i < a.tokens * TILE_ROWS; i += 32 * WARPS) {
+            const int n = i & (TILE_ROWS - 1), t = i >> 4;
+            float s = 0.f;
+            for (int w = 0; w < WARPS; ++w) s += total[(w * a.tokens + t) * 17 + n];
+            const int64_t at = (int64_t)t * a.cols + rt * TILE_ROWS + n;
+            if (a.bf16_out) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(s);
+            else static_cast<float*>(a.y)[at] = s;
+        }
+        __syncthreads();
     }
+    copies_done<0>();
+}
+
+int multiprocessors()
+{
+    static PerDeviceCache<int> cache;
+    int n = 0;
+    return cache.get(n, [](int dev, int& v) { return cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess; }) ? n : 148;
+}
+
+template <int NT, int WARPS, int STAGES>
+cudaError_t launch_gate_up(const MoeArgs& a, cudaStream_t st)
+{
+    auto kernel = moe_gate_up_kernel<NT, WARPS, STAGES>;
+    constexpr int SMEM = WARPS * (STAGES * 2 * TILE_BYTES + 2 * TILE_ROWS * (8 * NT + 1) * (int)sizeof(float));
+    static unsigned long long set = 0;
+    const cudaError_t err = ensure_dynamic_smem(kernel, SMEM, set);
+    if (err != cudaSuccess) return err;
+    kernel<<<multiprocessors(), 32 * WARPS, SMEM, st>>>(a);
+    count_launch(1);
+    return cudaGetLastError();
+}
+
+template <int NT, int WARPS, int STAGES>
+cudaError_t launch_down(const MoeArgs& a, cudaStream_t st)
+{
+    auto kernel = moe_down_kernel<NT, WARPS, STAGES>;
+    constexpr int MOST = WARPS * (STAGES * TILE_BYTES + MOE_MAX_TOKENS * 17 * (int)sizeof(float));
+    static unsigned long long set = 0;
+    const cudaError_t err = ensure_dynamic_smem(kernel, MOST, set);
+    if (err != cudaSuccess) return err;
+    const int row_tiles = a.cols / TILE_ROWS, sms = multiprocessors();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(row_tiles < sms ? row_tiles : sms));
+    cfg.blockDim = dim3(32 * WARPS);
+    cfg.dynamicSmemBytes = WARPS * (STAGES * TILE_BYTES + a.tokens * 17 * sizeof(float));
+    cfg.stream = st;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, a);
+    count_launch(1);
+    return rc;
 }
 
 }  // namespace
@@ -292,11 +475,8 @@ extern "C" int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens
     a.cols = (int)cols; a.inner = (int)inner;
     a.col_tiles = (int)((cols + TILE_COLS - 1) / TILE_COLS); a.inner_tiles = (int)((inner + TILE_COLS - 1) / TILE_COLS);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const int slots = a.tokens * a.top_k;
-    moe_gate_up_kernel<<<dim3((unsigned)(inner / TILE_ROWS), (unsigned)(slots < num_experts ? slots : num_experts)), MOE_THREADS, 0, st>>>(a);
-    count_launch(1);
-    if (cudaGetLastError() != cudaSuccess) return MXFP8_ERR_CUDA;
-    moe_down_kernel<<<(unsigned)(cols / TILE_ROWS), MOE_THREADS, MOE_WARPS * a.tokens * 17 * sizeof(float), st>>>(a);
-    count_launch(1);
-    return cudaGetLastError() == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
+    a.pairs_magic = div_magic((uint32_t)(a.inner / TILE_ROWS));
+    cudaError_t err = a.tokens <= 8 ? launch_gate_up<1, 16, 5>(a, st) : (a.tokens <= 16 ? launch_gate_up<2, 16, 4>(a, st) : launch_gate_up<4, 8, 8>(a, st));
+    if (err == cudaSuccess) err = a.tokens <= 8 ? launch_down<1, 16, 8>(a, st) : launch_down<2, 16, 7>(a, st);
+    return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
 }
