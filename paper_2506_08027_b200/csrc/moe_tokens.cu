@@ -63,38 +63,42 @@ __device__ __forceinline__ void choose(const MoeArgs& a, Choice& choice, int mos
         uint32_t left[I];
 #pragma unroll
         for (int i = 0; i < I; ++i) left[i] = lane + 32 * i < a.experts ? order_of(a.logits[t * a.experts + lane + 32 * i]) : 0u;
-        uint32_t top = 0u;
-        float mine = 0.f, total = 0.f;               // lane j: the share of choice j
+        float all = 0.f;
+        uint32_t mine = 0u, top = 0u;                // lane j: choice j
+        int expert = -1;
         for (int j = 0; j < a.top_k; ++j) {
             uint32_t best = 0u;
             int at = 0;
 #pragma unroll
             for (int i = 0; i < I; ++i)
-                if (left[i] > best) { best = left[i]; at = lane + 32 * i; }
+                if (32 * i < a.experts && left[i] > best) { best = left[i]; at = lane + 32 * i; }
             const uint32_t peak = __reduce_max_sync(0xFFFFFFFFu, best);
-            const int expert = (int)__reduce_min_sync(0xFFFFFFFFu, best == peak ? (uint32_t)at : 0xFFFFu);
+            if (peak == 0u) break;                   // none is left
+            const int e = (int)__reduce_min_sync(0xFFFFFFFFu, best == peak ? (uint32_t)at : 0xFFFFu);
             if (j == 0) {
                 top = peak;
-                if (!a.renormalize && top != 0u) {
+                if (!a.renormalize)
 #pragma unroll
                     for (int i = 0; i < I; ++i)
-                        if (left[i] != 0u) total += share_of(left[i], top);
-#pragma unroll
-                    for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, off);
-                }
+                        if (left[i] != 0u) all += share_of(left[i], top);
             }
-            const float share = peak != 0u ? share_of(peak, top) : 0.f;
-            if (a.renormalize) total += share;
             if (lane == j) {
-                mine = share;
-                choice.expert[t * a.top_k + j] = (short)(peak != 0u ? expert : -1);
-                if (peak != 0u) atomicOr(&choice.who[expert][t >> 5], 1u << (t & 31));
+                mine = peak;
+                expert = e;
             }
 #pragma unroll
             for (int i = 0; i < I; ++i)
-                if (peak != 0u && lane + 32 * i == expert) left[i] = 0u;
+                if (32 * i < a.experts && lane + 32 * i == e) left[i] = 0u;
         }
-        if (lane < a.top_k) choice.share[t * a.top_k + lane] = mine > 0.f ? mine / total : 0.f;
+        const float share = expert >= 0 ? share_of(mine, top) : 0.f;
+        float total = a.renormalize ? share : all;
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, off);
+        if (lane < a.top_k) {
+            choice.expert[t * a.top_k + lane] = (short)expert;
+            choice.share[t * a.top_k + lane] = share > 0.f ? share / total : 0.f;
+            if (expert >= 0) atomicOr(&choice.who[expert][t >> 5], 1u << (t & 31));
+        }
     }
     __syncthreads();
     if (warp == 0) {                                  // first rows and entries, eight experts to a lane
@@ -151,12 +155,11 @@ __device__ __forceinline__ float activate(float x, int act)
 
 // A warp's ring of weight tiles in shared memory: R tiles (one column tile of R row tiles) to a stage, copied asynchronously by the warp's own
 // lanes STAGES - 1 steps ahead.  Nothing but the warp's own copies and __syncwarp guards them.
-__device__ __forceinline__ void copy_tile(uint32_t to, const uint8_t* tile, int lane)
+__device__ __forceinline__ void copy_tile(uint32_t to, const uint8_t* from, int lane)          // both at the lane's 16 bytes
 {
-    const uint8_t* from = tile + lane * 16;
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + lane * 16), "l"(from) : "memory");
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + lane * 16 + 512), "l"(from + 512) : "memory");
-    if (lane < 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + lane * 16 + 1024), "l"(from + 1024) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + 512), "l"(from + 512) : "memory");
+    if (lane < 4) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + 1024), "l"(from + 1024) : "memory");
 }
 __device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>
@@ -175,17 +178,24 @@ __device__ __forceinline__ void read_tiles(Operands<R, NT>& o, const uint8_t* st
     }
 }
 
-// Activations under column tile kt for rows `from` (null: none); columns behind the matrix are zeros
+// Activations under column tile kt of the rows `from` (a lane without a row reads another one: its columns of the products are not used).
+// Columns behind the matrix are zeros.
 template <int NT>
-__device__ __forceinline__ void read_rows(uint4 (&x)[NT][4], const __nv_bfloat16* const (&from)[NT], int kt, int cols, int lane)
+__device__ __forceinline__ void read_rows(uint4 (&x)[NT][4], const __nv_bfloat16* const (&from)[NT], int kt, int cols)
 {
+    const int k = kt * TILE_COLS;
+    if (k + TILE_COLS <= cols) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-            const int k = kt * TILE_COLS + g * 32;
-            x[t][g] = from[t] && k < cols ? *reinterpret_cast<const uint4*>(from[t] + k + (lane & 3) * 8) : make_uint4(0u, 0u, 0u, 0u);
-        }
+            for (int g = 0; g < 4; ++g) x[t][g] = *reinterpret_cast<const uint4*>(from[t] + k + g * 32);
+    } else {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                x[t][g] = k + g * 32 < cols ? *reinterpret_cast<const uint4*>(from[t] + k + g * 32) : make_uint4(0u, 0u, 0u, 0u);
+    }
 }
 
 template <int R, int NT>
@@ -199,6 +209,25 @@ __device__ __forceinline__ void clear(float (&acc)[R][NT][4])
             for (int i = 0; i < 4; ++i) acc[r][t][i] = 0.f;
 }
 
+// A warp's next `last - first` tiles of its ring: column tiles first .. last - 1 of R row tiles, NX blocks of eight rows wide.
+template <int R, int NX, int STAGES, typename Fetch>
+__device__ __forceinline__ void run_tiles(const __nv_bfloat16* const (&from)[NX], int first, int last, int cols, const uint8_t* ring, int& stage, Fetch& fetch,
+                                          float (&acc)[R][NX][4])
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int kt = first; kt < last; ++kt) {
+        Operands<R, NX> o;
+        read_rows<NX>(o.x, from, kt, cols);
+        copies_done<STAGES - 2>();
+        __syncwarp();
+        fetch();
+        read_tiles(o, ring + stage * (R * TILE_BYTES), lane);
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        product<R, NX>(o, acc);
+    }
+}
+
 // ---- first launch: units of 16 gate rows and the 16 up rows that belong to them, for the rows of one entry.  2^team warps share a
 // unit and split its columns; the teams of all CTAs take the units in turn.
 template <int NT, int WARPS, int STAGES>
@@ -210,7 +239,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) moe_gate_up_kernel(const MoeArg
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the second launch may choose, and fetch weights, beside this one
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* ring = dynamic + warp * STAGES * STAGE;
-    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
     float* sums = reinterpret_cast<float*>(dynamic + WARPS * STAGES * STAGE);
     choose(a, choice, 8 * NT);
     if (blockIdx.x == 0)
@@ -226,27 +255,27 @@ __global__ void __launch_bounds__(32 * WARPS, 1) moe_gate_up_kernel(const MoeArg
         if (cost < least) { least = cost; team = l; }
     }
     const int size = 1 << team, part = warp & (size - 1), unit0 = (warp >> team) * ctas + blockIdx.x, step = ctas * (WARPS >> team);
+    const int kt0 = a.col_tiles * part >> team, kt1 = a.col_tiles * (part + 1) >> team;       // this warp's column tiles
     auto tile_of = [&](int unit) {
         int v, p;
         divmod((uint32_t)unit, (uint32_t)pairs, a.pairs_magic, v, p);
         return a.gate_up + ((int64_t)choice.entry_expert[v] * 2 * pairs + p) * a.col_tiles * TILE_BYTES;
     };
     const int64_t to_up = (int64_t)pairs * a.col_tiles * TILE_BYTES;
-    // what is fetched next
-    int f_unit = unit0, f_kt = part, f_stage = 0;
-    const uint8_t* f_tile = unit0 < units ? tile_of(unit0) : nullptr;
+    // what is fetched next: tiles left of f_unit, from f_tile
+    int f_unit = unit0 - step, f_left = 0, f_stage = 0;
+    const uint8_t* f_tile = nullptr;
     auto fetch = [&]() {
-        while (f_unit < units && f_kt >= a.col_tiles) {
+        if (f_left == 0 && kt1 > kt0 && f_unit + step < units) {
             f_unit += step;
-            f_kt = part;
-            if (f_unit < units) f_tile = tile_of(f_unit);
-            if (part >= a.col_tiles) { f_unit = units; break; }             // this warp has no column tiles
+            f_tile = tile_of(f_unit) + kt0 * TILE_BYTES + lane * 16;
+            f_left = kt1 - kt0;
         }
-        if (f_unit < units) {
-            const uint8_t* from = f_tile + (int64_t)f_kt * TILE_BYTES;
-            copy_tile(ring_at + f_stage * STAGE, from, lane);
-            copy_tile(ring_at + f_stage * STAGE + TILE_BYTES, from + to_up, lane);
-            f_kt += size;
+        if (f_left > 0) {
+            copy_tile(ring_at + f_stage * STAGE, f_tile, lane);
+            copy_tile(ring_at + f_stage * STAGE + TILE_BYTES, f_tile + to_up, lane);
+            f_tile += TILE_BYTES;
+            --f_left;
         }
         copies_issued();
         f_stage = f_stage + 1 == STAGES ? 0 : f_stage + 1;
@@ -264,26 +293,18 @@ __global__ void __launch_bounds__(32 * WARPS, 1) moe_gate_up_kernel(const MoeArg
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int i = 8 * t + (lane >> 2);
-            from[t] = i < rows ? a.x + (int64_t)choice.token[row0 + i] * a.cols : nullptr;
+            from[t] = a.x + (int64_t)choice.token[row0 + (i < rows ? i : 0)] * a.cols + (lane & 3) * 8;
         }
         float acc[2][NT][4];
         clear(acc);
-        for (int kt = part; kt < a.col_tiles; kt += size) {
-            Operands<2, NT> o;
-            read_rows<NT>(o.x, from, kt, a.cols, lane);
-            copies_done<STAGES - 2>();
-            __syncwarp();
-            fetch();
-            read_tiles(o, ring + stage * STAGE, lane);
-            stage = stage + 1 == STAGES ? 0 : stage + 1;
-            product<2, NT>(o, acc);
-        }
+        run_tiles<2, NT, STAGES>(from, kt0, kt1, a.cols, ring, stage, fetch, acc);
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) my_sums[(r * TILE_ROWS + (lane >> 2) + 8 * (i >> 1)) * P + 8 * t + 2 * (lane & 3) + (i & 1)] = acc[r][t][i];
+                for (int i = 0; i < 4; ++i)
+                    if (8 * t < rows) my_sums[(r * TILE_ROWS + (lane >> 2) + 8 * (i >> 1)) * P + 8 * t + 2 * (lane & 3) + (i & 1)] = acc[r][t][i];
         auto meet = [&]() {
             if (team == 0) __syncwarp();
             else asm volatile("bar.sync %0, %1;" :: "r"(1 + (warp >> team)), "r"(32 << team) : "memory");
@@ -316,25 +337,35 @@ __global__ void __launch_bounds__(32 * WARPS, 1) moe_down_kernel(const MoeArgs a
     __shared__ Choice choice;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* ring = dynamic + warp * STAGES * TILE_BYTES;
-    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
     float* total = reinterpret_cast<float*>(dynamic + WARPS * STAGES * TILE_BYTES);      // [warp][token][row], rows padded to 17
     choose(a, choice, 8 * NT);
     const int row_tiles = a.cols / TILE_ROWS, entries = choice.entries;
     float* mine = total + warp * a.tokens * 17;
-    int f_rt = blockIdx.x, f_v = 0, f_kt = warp, f_stage = 0;
+    // this warp's tiles of every row tile: a range of all entries' column tiles, one entry after the other
+    const int tiles = entries * a.inner_tiles, w0 = (int)((int64_t)tiles * warp / WARPS), w1 = (int)((int64_t)tiles * (warp + 1) / WARPS);
+    const int v0 = w0 / a.inner_tiles, k0 = w0 - v0 * a.inner_tiles;
+    int f_rt = blockIdx.x - gridDim.x, f_v = 0, f_left = 0, f_here = 0, f_stage = 0;          // tiles left of the row tile, of the entry
+    const uint8_t* f_tile = nullptr;
     auto fetch = [&]() {
-        while (f_rt < row_tiles && f_kt >= a.inner_tiles) {                  // the warps go on where the entry before ended
-            f_kt -= a.inner_tiles;
-            if (++f_v >= entries) {
-                f_v = 0;
-                f_kt = warp;
+        if (f_here == 0) {                                                  // on to the next entry, or to the next row tile
+            if (f_left == 0 && w1 > w0 && f_rt + (int)gridDim.x < row_tiles) {
                 f_rt += gridDim.x;
-                if (entries * a.inner_tiles <= warp) f_rt = row_tiles;       // nothing for this warp
+                f_v = v0 - 1;
+                f_left = w1 - w0;
+            }
+            if (f_left > 0) {
+                const bool begin = f_left == w1 - w0;
+                ++f_v;
+                f_tile = a.down + ((int64_t)choice.entry_expert[f_v] * row_tiles + f_rt) * a.inner_tiles * TILE_BYTES + (begin ? k0 * TILE_BYTES : 0) + lane * 16;
+                f_here = min(f_left, a.inner_tiles - (begin ? k0 : 0));
+                f_left -= f_here;
             }
         }
-        if (f_rt < row_tiles && entries > 0) {
-            copy_tile(ring_at + f_stage * TILE_BYTES, a.down + (((int64_t)choice.entry_expert[f_v] * row_tiles + f_rt) * a.inner_tiles + f_kt) * TILE_BYTES, lane);
-            f_kt += WARPS;
+        if (f_here > 0) {
+            copy_tile(ring_at + f_stage * TILE_BYTES, f_tile, lane);
+            f_tile += TILE_BYTES;
+            --f_here;
         }
         copies_issued();
         f_stage = f_stage + 1 == STAGES ? 0 : f_stage + 1;
@@ -346,30 +377,20 @@ __global__ void __launch_bounds__(32 * WARPS, 1) moe_down_kernel(const MoeArgs a
     for (int rt = blockIdx.x; rt < row_tiles; rt += gridDim.x) {
         for (int i = lane; i < a.tokens * 17; i += 32) mine[i] = 0.f;
         __syncwarp();
-        int kt = warp;
-        for (int v = 0; v < entries; ++v, kt -= a.inner_tiles) {
-            if (kt >= a.inner_tiles) continue;
-            const int row0 = choice.entry_row[v], rows = choice.entry_rows[v];
+        for (int v = v0, kt = k0, left = w1 - w0; left > 0; ++v, kt = 0) {
+            const int row0 = choice.entry_row[v], rows = choice.entry_rows[v], here = min(left, a.inner_tiles - kt);
+            left -= here;
             const __nv_bfloat16* from[2 * NT];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const int i = 8 * t + (lane >> 2);
-                const int64_t at = (int64_t)(row0 + i) * a.inner;
-                from[t] = i < rows ? a.m_hi + at : nullptr;
-                from[NT + t] = i < rows ? a.m_lo + at : nullptr;
+                const int64_t at = (int64_t)(row0 + (i < rows ? i : 0)) * a.inner + (lane & 3) * 8;
+                from[t] = a.m_hi + at;
+                from[NT + t] = a.m_lo + at;
             }
             float acc[1][2 * NT][4];
             clear(acc);
-            for (; kt < a.inner_tiles; kt += WARPS) {
-                Operands<1, 2 * NT> o;
-                read_rows<2 * NT>(o.x, from, kt, a.inner, lane);
-                copies_done<STAGES - 2>();
-                __syncwarp();
-                fetch();
-                read_tiles(o, ring + stage * TILE_BYTES, lane);
-                stage = stage + 1 == STAGES ? 0 : stage + 1;
-                product<1, 2 * NT>(o, acc);
-            }
+            run_tiles<1, 2 * NT, STAGES>(from, kt, kt + here, a.inner, ring, stage, fetch, acc);
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -476,7 +497,9 @@ extern "C" int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens
     a.col_tiles = (int)((cols + TILE_COLS - 1) / TILE_COLS); a.inner_tiles = (int)((inner + TILE_COLS - 1) / TILE_COLS);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     a.pairs_magic = div_magic((uint32_t)(a.inner / TILE_ROWS));
-    cudaError_t err = a.tokens <= 8 ? launch_gate_up<1, 16, 5>(a, st) : (a.tokens <= 16 ? launch_gate_up<2, 16, 4>(a, st) : launch_gate_up<4, 8, 8>(a, st));
-    if (err == cudaSuccess) err = a.tokens <= 8 ? launch_down<1, 16, 8>(a, st) : launch_down<2, 16, 7>(a, st);
+    // eight rows of an expert together, or sixteen where that many are expected of most
+    const bool few = a.tokens <= 8 || a.tokens * a.top_k <= 4 * num_experts;
+    cudaError_t err = few ? launch_gate_up<1, 16, 5>(a, st) : launch_gate_up<2, 16, 4>(a, st);
+    if (err == cudaSuccess) err = few ? launch_down<1, 16, 8>(a, st) : launch_down<2, 16, 7>(a, st);
     return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
 }
