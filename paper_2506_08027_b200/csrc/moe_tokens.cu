@@ -37,7 +37,7 @@ struct Choice {
     uint8_t token[MOE_MAX_ROWS];                          // by row
     short entry_expert[MOE_MAX_ENTRIES], entry_row[MOE_MAX_ENTRIES];
     uint8_t entry_rows[MOE_MAX_ENTRIES];
-    int entries;
+    int entries, scan[MOE_MAX_EXPERTS / 32];
 };
 
 // Unsigned numbers in the order of the logits; 0 for one that is never chosen (-Inf, NaN).  Both zeros are equal.
@@ -101,33 +101,37 @@ __device__ __forceinline__ void choose(const MoeArgs& a, Choice& choice, int mos
         }
     }
     __syncthreads();
-    if (warp == 0) {                                  // first rows and entries, eight experts to a lane
-        int rows = 0, entries = 0;
-#pragma unroll
-        for (int i = 0; i < I; ++i) {
-            const int n = __popc(choice.who[lane * I + i][0]) + __popc(choice.who[lane * I + i][1]);
-            rows += n;
-            entries += (n + most - 1) / most;
-        }
-        int before_rows = rows, before_entries = entries;
+    // first rows and entries: a thread per expert, both sums in one number
+    static_assert(MOE_MAX_ROWS < 65536 && MOE_MAX_EXPERTS == 256, "eight warps scan the experts");
+    int n = 0, cut = 0, before = 0;
+    if (warp < I) {
+        n = __popc(choice.who[tid][0]) + __popc(choice.who[tid][1]);
+        cut = (n + most - 1) / most;
+        before = n | cut << 16;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
-            const int r = __shfl_up_sync(0xFFFFFFFFu, before_rows, off), e = __shfl_up_sync(0xFFFFFFFFu, before_entries, off);
-            if (lane >= off) { before_rows += r; before_entries += e; }
+            const int v = __shfl_up_sync(0xFFFFFFFFu, before, off);
+            if (lane >= off) before += v;
         }
-        if (lane == 31) choice.entries = before_entries;
-        before_rows -= rows;
-        before_entries -= entries;
+        if (lane == 31) choice.scan[warp] = before;
+        before -= n | cut << 16;
+    }
+    __syncthreads();
+    if (warp < I) {
+        int all = 0;
 #pragma unroll
-        for (int i = 0; i < I; ++i) {
-            const int e = lane * I + i, n = __popc(choice.who[e][0]) + __popc(choice.who[e][1]);
-            choice.first[e] = (short)before_rows;
-            for (int r = 0; r < n; r += most) {
-                choice.entry_expert[before_entries] = (short)e;
-                choice.entry_row[before_entries] = (short)(before_rows + r);
-                choice.entry_rows[before_entries++] = (uint8_t)min(most, n - r);
-            }
-            before_rows += n;
+        for (int w = 0; w < I; ++w) {
+            const int v = choice.scan[w];
+            if (w < warp) before += v;
+            all += v;
+        }
+        if (tid == 0) choice.entries = all >> 16;
+        int row = before & 0xFFFF;
+        choice.first[tid] = (short)row;
+        for (int v = before >> 16; cut > 0; --cut, ++v, row += most, n -= most) {
+            choice.entry_expert[v] = (short)tid;
+            choice.entry_row[v] = (short)row;
+            choice.entry_rows[v] = (uint8_t)min(most, n);
         }
     }
     __syncthreads();
@@ -228,48 +232,64 @@ __device__ __forceinline__ void run_tiles(const __nv_bfloat16* const (&from)[NX]
     }
 }
 
-// ---- first launch: units of 16 gate rows and the 16 up rows that belong to them, for the rows of one entry.  2^team warps share a
-// unit and split its columns; the teams of all CTAs take the units in turn.
+// m of one (row of an entry, row of the matrix)
+__device__ __forceinline__ void put_m(const MoeArgs& a, int64_t row, int n, float gate, float up)
+{
+    const float m = activate(gate, a.act) * up;
+    const __nv_bfloat16 hi = __float2bfloat16_rn(m);
+    a.m_hi[row * a.inner + n] = hi;
+    a.m_lo[row * a.inner + n] = __float2bfloat16_rn(m - __bfloat162float(hi));
+}
+
+// ---- first launch: units of 16 gate rows and the 16 up rows that belong to them, for the rows of one entry.  The CTAs take the units in
+// turn.  A CTA's warps take a unit each while there is one for every warp; the column tiles of the units that are left are split evenly
+// over all warps (less than a unit each, so parts of two at most), whose sums meet in shared memory.
 template <int NT, int WARPS, int STAGES>
 __global__ void __launch_bounds__(32 * WARPS, 1) moe_gate_up_kernel(const MoeArgs a)
 {
     extern __shared__ __align__(16) uint8_t dynamic[];
     __shared__ Choice choice;
-    constexpr int P = 8 * NT + 1, WARP_SUMS = 2 * TILE_ROWS * P, STAGE = 2 * TILE_BYTES;
+    constexpr int P = 8 * NT + 1, UNIT_SUMS = 2 * TILE_ROWS * P, STAGE = 2 * TILE_BYTES;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the second launch may choose, and fetch weights, beside this one
+    asm volatile("griddepcontrol.wait;" ::: "memory");                    // all that was launched before this call is done
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* ring = dynamic + warp * STAGES * STAGE;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
-    float* sums = reinterpret_cast<float*>(dynamic + WARPS * STAGES * STAGE);
+    float* sums = reinterpret_cast<float*>(dynamic + WARPS * STAGES * STAGE);        // [warp][first, second unit]
     choose(a, choice, 8 * NT);
     if (blockIdx.x == 0)
         for (int s = tid; s < a.tokens * a.top_k; s += 32 * WARPS) {
             if (a.ids) a.ids[s] = choice.expert[s];
             if (a.weights) a.weights[s] = choice.share[s];
         }
-    const int pairs = a.inner / TILE_ROWS, units = choice.entries * pairs, ctas = gridDim.x;
-    // the fewest steps for the team that has most: rounds of units times (column tiles of a warp + about two for the joining of the sums)
-    int team = 0;
-    for (int l = 0, least = 0x7FFFFFFF; (1 << l) <= WARPS; ++l) {
-        const int teams = ctas * (WARPS >> l), rounds = (units + teams - 1) / teams, cost = rounds * (((a.col_tiles + (1 << l) - 1) >> l) + 2);
-        if (cost < least) { least = cost; team = l; }
-    }
-    const int size = 1 << team, part = warp & (size - 1), unit0 = (warp >> team) * ctas + blockIdx.x, step = ctas * (WARPS >> team);
-    const int kt0 = a.col_tiles * part >> team, kt1 = a.col_tiles * (part + 1) >> team;       // this warp's column tiles
-    auto tile_of = [&](int unit) {
-        int v, p;
-        divmod((uint32_t)unit, (uint32_t)pairs, a.pairs_magic, v, p);
-        return a.gate_up + ((int64_t)choice.entry_expert[v] * 2 * pairs + p) * a.col_tiles * TILE_BYTES;
+    const int pairs = a.inner / TILE_ROWS, units = choice.entries * pairs, ctas = gridDim.x, tiles = a.col_tiles;
+    const int mine = units > (int)blockIdx.x ? (units - blockIdx.x + ctas - 1) / ctas : 0;       // unit i of this CTA is blockIdx.x + i * ctas
+    const int whole = mine / WARPS, rest = mine % WARPS;
+    const int s0 = rest * tiles * warp / WARPS, s1 = rest * tiles * (warp + 1) / WARPS;          // this warp's share of the rest
+    const int r0 = s0 / tiles, k0 = s0 - r0 * tiles;
+    const int64_t to_up = (int64_t)pairs * tiles * TILE_BYTES;
+    // piece q of this warp: a whole unit, or one of the parts of the rest; its unit, first tile and number of tiles (0: there is none)
+    struct Part { int unit, first, count; };
+    auto part = [&](int q) {
+        Part p{0, 0, 0};
+        if (q < whole) return Part{(int)blockIdx.x + (q * WARPS + warp) * ctas, 0, tiles};
+        if (q > whole + 1) return p;
+        p.first = q == whole ? k0 : 0;
+        p.count = q == whole ? min(s1 - s0, tiles - k0) : s1 - s0 - min(s1 - s0, tiles - k0);
+        p.unit = blockIdx.x + (whole * WARPS + r0 + (q - whole)) * ctas;
+        return p;
     };
-    const int64_t to_up = (int64_t)pairs * a.col_tiles * TILE_BYTES;
-    // what is fetched next: tiles left of f_unit, from f_tile
-    int f_unit = unit0 - step, f_left = 0, f_stage = 0;
+    int f_q = -1, f_left = 0, f_stage = 0;
     const uint8_t* f_tile = nullptr;
     auto fetch = [&]() {
-        if (f_left == 0 && kt1 > kt0 && f_unit + step < units) {
-            f_unit += step;
-            f_tile = tile_of(f_unit) + kt0 * TILE_BYTES + lane * 16;
-            f_left = kt1 - kt0;
+        if (f_left == 0 && f_q < whole + 1) {
+            const Part p = part(++f_q);
+            if (p.count > 0) {
+                int v, i;
+                divmod((uint32_t)p.unit, (uint32_t)pairs, a.pairs_magic, v, i);
+                f_tile = a.gate_up + (((int64_t)choice.entry_expert[v] * 2 * pairs + i) * tiles + p.first) * TILE_BYTES + lane * 16;
+                f_left = p.count;
+            }
         }
         if (f_left > 0) {
             copy_tile(ring_at + f_stage * STAGE, f_tile, lane);
@@ -283,11 +303,12 @@ __global__ void __launch_bounds__(32 * WARPS, 1) moe_gate_up_kernel(const MoeArg
 #pragma unroll 1
     for (int s = 0; s < STAGES - 1; ++s) fetch();
     int stage = 0;
-    float* my_sums = sums + warp * WARP_SUMS;
-    const float* team_sums = sums + (warp - part) * WARP_SUMS;
-    for (int unit = unit0; unit < units; unit += step) {
-        int v, p;
-        divmod((uint32_t)unit, (uint32_t)pairs, a.pairs_magic, v, p);
+#pragma unroll 1
+    for (int q = 0; q < whole + 2; ++q) {
+        const Part p = part(q);
+        if (p.count == 0) continue;
+        int v, pair;
+        divmod((uint32_t)p.unit, (uint32_t)pairs, a.pairs_magic, v, pair);
         const int row0 = choice.entry_row[v], rows = choice.entry_rows[v];
         const __nv_bfloat16* from[NT];
 #pragma unroll
@@ -297,35 +318,42 @@ __global__ void __launch_bounds__(32 * WARPS, 1) moe_gate_up_kernel(const MoeArg
         }
         float acc[2][NT][4];
         clear(acc);
-        run_tiles<2, NT, STAGES>(from, kt0, kt1, a.cols, ring, stage, fetch, acc);
+        run_tiles<2, NT, STAGES>(from, p.first, p.first + p.count, a.cols, ring, stage, fetch, acc);
+        float* to = sums + (2 * warp + (q - whole)) * UNIT_SUMS;
 #pragma unroll
-        for (int r = 0; r < 2; ++r)
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (8 * t < rows) my_sums[(r * TILE_ROWS + (lane >> 2) + 8 * (i >> 1)) * P + 8 * t + 2 * (lane & 3) + (i & 1)] = acc[r][t][i];
-        auto meet = [&]() {
-            if (team == 0) __syncwarp();
-            else asm volatile("bar.sync %0, %1;" :: "r"(1 + (warp >> team)), "r"(32 << team) : "memory");
-        };
-        meet();
-        for (int i = part * 32 + lane; i < rows * TILE_ROWS; i += 32 << team) {
-            const int n = i & (TILE_ROWS - 1), s = i >> 4;
-            float g = 0.f, u = 0.f;
-            for (int w = 0; w < size; ++w) {
-                g += team_sums[w * WARP_SUMS + n * P + s];
-                u += team_sums[w * WARP_SUMS + (TILE_ROWS + n) * P + s];
+            for (int i = 0; i < 4; ++i) {
+                const int n = (lane >> 2) + 8 * (i >> 1), s = 8 * t + 2 * (lane & 3) + (i & 1);
+                if (q < whole) {
+                    if (s < rows) put_m(a, row0 + s, pair * TILE_ROWS + n, acc[0][t][i], acc[1][t][i]);
+                } else {
+                    to[n * P + s] = acc[0][t][i];
+                    to[(TILE_ROWS + n) * P + s] = acc[1][t][i];
+                }
             }
-            const float m = activate(g, a.act) * u;
-            const __nv_bfloat16 hi = __float2bfloat16_rn(m);
-            const int64_t at = (int64_t)(row0 + s) * a.inner + p * TILE_ROWS + n;
-            a.m_hi[at] = hi;
-            a.m_lo[at] = __float2bfloat16_rn(m - __bfloat162float(hi));
-        }
-        meet();
     }
     copies_done<0>();
+    if (rest == 0) return;
+    __syncthreads();
+    for (int r = warp; r < rest; r += WARPS) {
+        int v, pair;
+        divmod((uint32_t)(blockIdx.x + (whole * WARPS + r) * ctas), (uint32_t)pairs, a.pairs_magic, v, pair);
+        const int row0 = choice.entry_row[v], rows = choice.entry_rows[v];
+        // the warps with a part of unit r: those whose shares meet tiles r * tiles .. (r + 1) * tiles - 1
+        for (int i = lane; i < rows * TILE_ROWS; i += 32) {
+            const int n = i & (TILE_ROWS - 1), s = i >> 4;
+            float g = 0.f, u = 0.f;
+            for (int w = 0; w < WARPS; ++w) {
+                const int b0 = rest * tiles * w / WARPS, b1 = rest * tiles * (w + 1) / WARPS;
+                if (b1 <= b0 || b1 <= r * tiles || b0 >= (r + 1) * tiles) continue;
+                const float* from = sums + (2 * w + (b0 < r * tiles)) * UNIT_SUMS + n * P + s;
+                g += from[0];
+                u += from[TILE_ROWS * P];
+            }
+            put_m(a, row0 + s, pair * TILE_ROWS + n, g, u);
+        }
+    }
 }
 
 // ---- second launch: a CTA takes 16 rows of all entries' down projections at a time.  Its warps take the entries' column tiles in turn; each
@@ -424,32 +452,16 @@ int multiprocessors()
     return cache.get(n, [](int dev, int& v) { return cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess; }) ? n : 148;
 }
 
-template <int NT, int WARPS, int STAGES>
-cudaError_t launch_gate_up(const MoeArgs& a, cudaStream_t st)
+// Launched before the launches ahead of it have ended; the kernel waits for them itself.
+template <typename Kernel>
+cudaError_t launch_early(Kernel kernel, int ctas, int threads, int smem, int most_smem, unsigned long long& set, const MoeArgs& a, cudaStream_t st)
 {
-    auto kernel = moe_gate_up_kernel<NT, WARPS, STAGES>;
-    constexpr int SMEM = WARPS * (STAGES * 2 * TILE_BYTES + 2 * TILE_ROWS * (8 * NT + 1) * (int)sizeof(float));
-    static unsigned long long set = 0;
-    const cudaError_t err = ensure_dynamic_smem(kernel, SMEM, set);
+    const cudaError_t err = ensure_dynamic_smem(kernel, most_smem, set);
     if (err != cudaSuccess) return err;
-    kernel<<<multiprocessors(), 32 * WARPS, SMEM, st>>>(a);
-    count_launch(1);
-    return cudaGetLastError();
-}
-
-template <int NT, int WARPS, int STAGES>
-cudaError_t launch_down(const MoeArgs& a, cudaStream_t st)
-{
-    auto kernel = moe_down_kernel<NT, WARPS, STAGES>;
-    constexpr int MOST = WARPS * (STAGES * TILE_BYTES + MOE_MAX_TOKENS * 17 * (int)sizeof(float));
-    static unsigned long long set = 0;
-    const cudaError_t err = ensure_dynamic_smem(kernel, MOST, set);
-    if (err != cudaSuccess) return err;
-    const int row_tiles = a.cols / TILE_ROWS, sms = multiprocessors();
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(row_tiles < sms ? row_tiles : sms));
-    cfg.blockDim = dim3(32 * WARPS);
-    cfg.dynamicSmemBytes = WARPS * (STAGES * TILE_BYTES + a.tokens * 17 * sizeof(float));
+    cfg.gridDim = dim3((unsigned)ctas);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = st;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -457,8 +469,26 @@ cudaError_t launch_down(const MoeArgs& a, cudaStream_t st)
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, a);
-    count_launch(1);
+    if (rc == cudaSuccess) count_launch(1);
     return rc;
+}
+
+template <int NT, int WARPS, int STAGES>
+cudaError_t launch_gate_up(const MoeArgs& a, cudaStream_t st)
+{
+    constexpr int SMEM = WARPS * (STAGES * 2 * TILE_BYTES + 2 * 2 * TILE_ROWS * (8 * NT + 1) * (int)sizeof(float));
+    static unsigned long long set = 0;
+    return launch_early(moe_gate_up_kernel<NT, WARPS, STAGES>, multiprocessors(), 32 * WARPS, SMEM, SMEM, set, a, st);
+}
+
+template <int NT, int WARPS, int STAGES>
+cudaError_t launch_down(const MoeArgs& a, cudaStream_t st)
+{
+    constexpr int RING = WARPS * STAGES * TILE_BYTES, PER_TOKEN = WARPS * 17 * (int)sizeof(float);
+    static unsigned long long set = 0;
+    const int row_tiles = a.cols / TILE_ROWS, sms = multiprocessors();
+    return launch_early(moe_down_kernel<NT, WARPS, STAGES>, row_tiles < sms ? row_tiles : sms, 32 * WARPS, RING + a.tokens * PER_TOKEN,
+                        RING + MOE_MAX_TOKENS * PER_TOKEN, set, a, st);
 }
 
 }  // namespace
@@ -499,7 +529,7 @@ extern "C" int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens
     a.pairs_magic = div_magic((uint32_t)(a.inner / TILE_ROWS));
     // eight rows of an expert together, or sixteen where that many are expected of most
     const bool few = a.tokens <= 8 || a.tokens * a.top_k <= 4 * num_experts;
-    cudaError_t err = few ? launch_gate_up<1, 16, 5>(a, st) : launch_gate_up<2, 16, 4>(a, st);
+    cudaError_t err = few ? launch_gate_up<1, 16, 4>(a, st) : launch_gate_up<2, 16, 3>(a, st);
     if (err == cudaSuccess) err = few ? launch_down<1, 16, 8>(a, st) : launch_down<2, 16, 7>(a, st);
     return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
 }
