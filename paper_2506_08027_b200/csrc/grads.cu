@@ -4,7 +4,7 @@
 //
 // Bound by memory: every gradient is read once for S, then read and written once.  The items go to the kernels by value, as
 // a table in the launch's parameters (nothing to copy or to keep alive, and a captured launch holds its own).  Items are cut into
-// pieces of PIECE elements, counted from the 16-byte boundary at or before the item's first element, so that all
+// pieces of a few thousand elements, counted from the 16-byte boundary at or before the item's first element, so that all
 // vectors of a piece are aligned whatever the item's alignment.
 #include <cuda_bf16.h>
 
@@ -15,8 +15,8 @@ namespace mxfp8 {
 namespace {
 
 constexpr int GRAD_THREADS = 256, GRAD_WARPS = GRAD_THREADS / 32;
-constexpr int PIECE = 16384;                    // elements
 constexpr int GRAD_CTAS = 4 * 148;              // at most, of one launch: one partial sum each
+constexpr int UNROLL = 4;                       // vectors of 16 bytes in flight per thread; four CTAs per multiprocessor
 constexpr int MANY_ITEMS = 1024, FEW_ITEMS = 96;
 
 template <int N>
@@ -27,6 +27,8 @@ struct GradTable {
     uint32_t first[N + 1];       // first piece of every item; [count] is the number of pieces
     uint8_t bf16[N];
     int count;
+    int piece_log;               // elements of a piece
+    bool in_place;               // all items
 };
 
 // Where a piece lies: its item and the elements first .. last - 1 of it; vectors start at `base`, which is first or, at the item's
@@ -48,32 +50,48 @@ __device__ __forceinline__ Piece find_piece(const GradTable<N>& t, uint32_t piec
     const int64_t before = (int64_t)(reinterpret_cast<uintptr_t>(t.src[lo]) & 15u) / bytes;
     Piece p;
     p.item = lo;
-    p.base = (int64_t)(piece - t.first[lo]) * PIECE - before;
+    p.base = ((int64_t)(piece - t.first[lo]) << t.piece_log) - before;
     p.first = p.base < 0 ? 0 : p.base;
-    p.last = min(p.base + PIECE, t.numel[lo]);
+    p.last = min(p.base + (1 << t.piece_log), t.numel[lo]);
     return p;
 }
 
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
-// Sum of the squares of V values.  In FP32 where the largest lies between 2^-40 and 2^60 (eight squares stay in range, and what
+// Sum of the squares of eight values.  In FP32 where the largest lies between 2^-40 and 2^60 (eight squares stay in range, and what
 // falls below FP32's is less than 2^-46 of the sum), in FP64 elsewhere.
-template <int V>
-__device__ __forceinline__ double squares(const float (&v)[V])
+__device__ __forceinline__ double squares(const float (&v)[8])
 {
-    float peak = 0.f;
+    float peak = 0.f, s = 0.f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) peak = fmaxf(peak, fabsf(v[i]));
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < V; ++i) s = fmaf(v[i], v[i], s);
+    for (int i = 0; i < 8; ++i) {
+        peak = fmaxf(peak, fabsf(v[i]));
+        s = fmaf(v[i], v[i], s);
+    }
     if (peak < 0x1p60f && peak > 0x1p-40f) return (double)s;
     double d = 0.0;
 #pragma unroll
-    for (int i = 0; i < V; ++i) d = fma((double)v[i], (double)v[i], d);
+    for (int i = 0; i < 8; ++i) d = fma((double)v[i], (double)v[i], d);
     return d;
 }
+
+// The elements of a 16-byte vector: eight of BF16, four of FP32
+template <typename T> constexpr int PER = 16 / sizeof(T);
+template <typename T>
+__device__ __forceinline__ void unpack(const uint4& w, float* v)
+{
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (sizeof(T) == 2) { v[2 * k] = bf16_low(u[k]); v[2 * k + 1] = bf16_high(u[k]); }
+        else v[k] = __uint_as_float(u[k]);
+    }
+}
+__device__ __forceinline__ float element(const float* p) { return *p; }
+__device__ __forceinline__ float element(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 __device__ __forceinline__ double cta_sum(double v, double* area)
 {
@@ -86,42 +104,57 @@ __device__ __forceinline__ double cta_sum(double v, double* area)
     return v;
 }
 
+// The whole vectors of a piece, begin .. end - 1 in elements; a few elements at the item's first and last vector lie outside.
+template <typename T>
+__device__ __forceinline__ void whole_vectors(const Piece& p, int64_t& begin, int64_t& end)
+{
+    begin = p.base < p.first ? p.base + PER<T> : p.base;
+    end = max(begin, p.base + (p.last - p.base) / PER<T> * PER<T>);
+}
+// Calls f for those elements, a thread for each.
+template <typename T, typename F>
+__device__ __forceinline__ void other_elements(const Piece& p, int64_t begin, int64_t end, F f)
+{
+    const int64_t head = p.first + threadIdx.x, tail = end + threadIdx.x - PER<T>;
+    if (threadIdx.x < PER<T> && head < min(begin, p.last)) f(head);
+    if (threadIdx.x >= PER<T> && threadIdx.x < 2 * PER<T> && tail < p.last) f(tail);
+}
+
+template <typename T>
+__device__ __forceinline__ double piece_squares(const T* src, const Piece& p)
+{
+    constexpr int V = PER<T>, STEP = GRAD_THREADS * V;
+    int64_t begin, end;
+    whole_vectors<T>(p, begin, end);
+    double sum = 0.0;
+    for (int64_t i = begin + threadIdx.x * V; i < end; i += UNROLL * STEP) {
+        uint4 w[UNROLL];
+#pragma unroll
+        for (int k = 0; k < UNROLL; ++k) w[k] = i + k * STEP < end ? *reinterpret_cast<const uint4*>(src + i + k * STEP) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int k = 0; k < UNROLL; k += 8 / V) {
+            float v[8];
+            unpack<T>(w[k], v);
+            if constexpr (V == 4) unpack<T>(w[k + 1], v + 4);
+            sum += squares(v);
+        }
+    }
+    other_elements<T>(p, begin, end, [&](int64_t at) {
+        const double d = element(src + at);
+        sum = fma(d, d, sum);
+    });
+    return sum;
+}
+
 template <int N>
-__global__ void __launch_bounds__(GRAD_THREADS) grad_squares_kernel(const __grid_constant__ GradTable<N> t, double* partial)
+__global__ void __launch_bounds__(GRAD_THREADS, 4) grad_squares_kernel(const __grid_constant__ GradTable<N> t, double* partial)
 {
     __shared__ double area[GRAD_WARPS];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     double sum = 0.0;
     for (uint32_t piece = blockIdx.x; piece < t.first[t.count]; piece += gridDim.x) {
         const Piece p = find_piece(t, piece);
-        if (t.bf16[p.item]) {
-            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(t.src[p.item]);
-            for (int64_t i = p.base + threadIdx.x * 8; i < p.last; i += GRAD_THREADS * 8) {
-                float v[8];
-                if (i >= p.first && i + 8 <= p.last) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(src + i);
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) { v[2 * k] = bf16_low(u[k]); v[2 * k + 1] = bf16_high(u[k]); }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[k] = (i + k >= p.first && i + k < p.last) ? __bfloat162float(src[i + k]) : 0.f;
-                }
-                sum += squares(v);
-            }
-        } else {
-            const float* src = static_cast<const float*>(t.src[p.item]);
-            for (int64_t i = p.base + threadIdx.x * 4; i < p.last; i += GRAD_THREADS * 4) {
-                float v[4];
-                if (i >= p.first && i + 4 <= p.last) {
-                    const float4 w = *reinterpret_cast<const float4*>(src + i);
-                    v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] = (i + k >= p.first && i + k < p.last) ? src[i + k] : 0.f;
-                }
-                sum += squares(v);
-            }
-        }
+        sum += t.bf16[p.item] ? piece_squares(static_cast<const __nv_bfloat16*>(t.src[p.item]), p) : piece_squares(static_cast<const float*>(t.src[p.item]), p);
     }
     sum = cta_sum(sum, area);
     if (threadIdx.x == 0) partial[blockIdx.x] = sum;
@@ -138,15 +171,55 @@ __device__ __forceinline__ double sum_of(const double* partial, int count, doubl
 __global__ void __launch_bounds__(GRAD_THREADS) grad_sum_kernel(const double* partial, int count, double* sumsq)
 {
     __shared__ double area[GRAD_WARPS];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const double s = sum_of(partial, count, area);
     if (threadIdx.x == 0) *sumsq = s;
 }
 
+template <typename T>
+__device__ __forceinline__ void piece_scale(const T* src, T* dst, const Piece& p, float factor)
+{
+    constexpr int V = PER<T>, STEP = GRAD_THREADS * V;
+    // vectors of both need the same place within 16 bytes
+    const bool together = ((reinterpret_cast<uintptr_t>(src) ^ reinterpret_cast<uintptr_t>(dst)) & 15u) == 0;
+    auto scaled = [&](uint4 w) {
+        float v[V];
+        unpack<T>(w, v);
+        uint32_t u[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if constexpr (V == 8) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k] * factor, v[2 * k + 1] * factor);
+                u[k] = *reinterpret_cast<const uint32_t*>(&b);
+            } else u[k] = __float_as_uint(v[k] * factor);
+        }
+        return make_uint4(u[0], u[1], u[2], u[3]);
+    };
+    if (!together) {
+        for (int64_t i = p.first + threadIdx.x; i < p.last; i += GRAD_THREADS) put(dst + i, element(src + i) * factor);
+        return;
+    }
+    int64_t begin, end;
+    whole_vectors<T>(p, begin, end);
+    for (int64_t i = begin + threadIdx.x * V; i < end; i += UNROLL * STEP) {
+        uint4 w[UNROLL];
+#pragma unroll
+        for (int k = 0; k < UNROLL; ++k)
+            if (i + k * STEP < end) w[k] = __ldcs(reinterpret_cast<const uint4*>(src + i + k * STEP));
+#pragma unroll
+        for (int k = 0; k < UNROLL; ++k)
+            if (i + k * STEP < end) __stcs(reinterpret_cast<uint4*>(dst + i + k * STEP), scaled(w[k]));
+    }
+    other_elements<T>(p, begin, end, [&](int64_t at) { put(dst + at, element(src + at) * factor); });
+}
+
+// Pieces in the opposite order to the sums': what those read last is in L2 (126 MB) and is read again first, and leaves it at once.
 template <int N>
-__global__ void __launch_bounds__(GRAD_THREADS) grad_scale_kernel(const __grid_constant__ GradTable<N> t, const double* partial, int count, float max_norm,
-                                                                  float* result)
+__global__ void __launch_bounds__(GRAD_THREADS, 4) grad_scale_kernel(const __grid_constant__ GradTable<N> t, const double* partial, int count, float max_norm,
+                                                                     float* result)
 {
     __shared__ double area[GRAD_WARPS];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const float norm = (float)sqrt(sum_of(partial, count, area));
     float factor = fminf(1.0f, max_norm / (norm + 1e-6f));
     if (!(norm <= 3.402823466e38f)) factor = 1.0f;               // infinite or not a number
@@ -154,42 +227,13 @@ __global__ void __launch_bounds__(GRAD_THREADS) grad_scale_kernel(const __grid_c
         result[0] = norm;
         result[1] = factor;
     }
-    for (uint32_t piece = blockIdx.x; piece < t.first[t.count]; piece += gridDim.x) {
-        const Piece p = find_piece(t, piece);
+    if (factor == 1.0f && t.in_place) return;
+    const uint32_t pieces = t.first[t.count];
+    for (uint32_t i = blockIdx.x; i < pieces; i += gridDim.x) {
+        const Piece p = find_piece(t, pieces - 1 - i);
         if (factor == 1.0f && t.src[p.item] == t.dst[p.item]) continue;
-        const bool together = ((reinterpret_cast<uintptr_t>(t.src[p.item]) ^ reinterpret_cast<uintptr_t>(t.dst[p.item])) & 15u) == 0;
-        if (t.bf16[p.item]) {
-            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(t.src[p.item]);
-            __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(t.dst[p.item]);
-            for (int64_t i = p.base + threadIdx.x * 8; i < p.last; i += GRAD_THREADS * 8) {
-                if (together && i >= p.first && i + 8 <= p.last) {
-                    uint4 w = *reinterpret_cast<const uint4*>(src + i);
-                    uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const __nv_bfloat162 v = __floats2bfloat162_rn(bf16_low(u[k]) * factor, bf16_high(u[k]) * factor);
-                        u[k] = *reinterpret_cast<const uint32_t*>(&v);
-                    }
-                    *reinterpret_cast<uint4*>(dst + i) = make_uint4(u[0], u[1], u[2], u[3]);
-                } else {
-                    for (int k = 0; k < 8; ++k)
-                        if (i + k >= p.first && i + k < p.last) dst[i + k] = __float2bfloat16_rn(__bfloat162float(src[i + k]) * factor);
-                }
-            }
-        } else {
-            const float* src = static_cast<const float*>(t.src[p.item]);
-            float* dst = static_cast<float*>(t.dst[p.item]);
-            for (int64_t i = p.base + threadIdx.x * 4; i < p.last; i += GRAD_THREADS * 4) {
-                if (together && i >= p.first && i + 4 <= p.last) {
-                    float4 w = *reinterpret_cast<const float4*>(src + i);
-                    w.x *= factor; w.y *= factor; w.z *= factor; w.w *= factor;
-                    *reinterpret_cast<float4*>(dst + i) = w;
-                } else {
-                    for (int k = 0; k < 4; ++k)
-                        if (i + k >= p.first && i + k < p.last) dst[i + k] = src[i + k] * factor;
-                }
-            }
-        }
+        if (t.bf16[p.item]) piece_scale(static_cast<const __nv_bfloat16*>(t.src[p.item]), static_cast<__nv_bfloat16*>(t.dst[p.item]), p, factor);
+        else piece_scale(static_cast<const float*>(t.src[p.item]), static_cast<float*>(t.dst[p.item]), p, factor);
     }
 }
 
@@ -198,17 +242,24 @@ template <typename F>
 cudaError_t by_tables(const mxfp8_grad_item* items, int count, F f)
 {
     auto fill = [](auto& t, const mxfp8_grad_item* from, int n) {
+        int64_t elements = 0;
+        for (int i = 0; i < n; ++i) elements += from[i].numel;
+        // a piece is a round of all threads' BF16 vectors (UNROLL each), or two of them while that leaves every CTA eight pieces
+        t.piece_log = (elements >> 14) >= 8 * GRAD_CTAS ? 14 : 13;
         t.count = 0;
+        t.in_place = true;
         uint32_t pieces = 0;
         for (int i = 0; i < n; ++i) {
             if (from[i].numel == 0) continue;
             const int bytes = from[i].dtype == MXFP8_BF16 ? 2 : 4, k = t.count++;
             t.src[k] = from[i].src; t.dst[k] = from[i].dst; t.numel[k] = from[i].numel; t.bf16[k] = bytes == 2;
+            t.in_place = t.in_place && from[i].src == from[i].dst;
             t.first[k] = pieces;
-            pieces += (uint32_t)((from[i].numel + (int64_t)(reinterpret_cast<uintptr_t>(from[i].src) & 15u) / bytes + PIECE - 1) / PIECE);
+            pieces += (uint32_t)((from[i].numel + (int64_t)(reinterpret_cast<uintptr_t>(from[i].src) & 15u) / bytes + (1 << t.piece_log) - 1) >> t.piece_log);
         }
         t.first[t.count] = pieces;
-        return pieces < (uint32_t)GRAD_CTAS ? (pieces ? pieces : 1u) : (uint32_t)GRAD_CTAS;
+        const uint32_t rounds = pieces / GRAD_CTAS + (pieces % GRAD_CTAS != 0);             // as few CTAs as take no more rounds
+        return rounds ? (pieces + rounds - 1) / rounds : 1u;
     };
     if (count <= FEW_ITEMS) {
         GradTable<FEW_ITEMS> t;
@@ -222,6 +273,24 @@ cudaError_t by_tables(const mxfp8_grad_item* items, int count, F f)
         if (err != cudaSuccess) return err;
     }
     return cudaSuccess;
+}
+
+// A launch that may begin before the one ahead of it has ended; its kernel waits for that one itself.
+template <typename Kernel, typename... Args>
+cudaError_t launch_early(Kernel kernel, unsigned ctas, cudaStream_t st, const Args&... args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(GRAD_THREADS);
+    cfg.stream = st;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, args...);
+    if (rc == cudaSuccess) count_launch(1);
+    return rc;
 }
 
 int tables_of(int count) { return count <= FEW_ITEMS ? 1 : (count + MANY_ITEMS - 1) / MANY_ITEMS; }
@@ -259,10 +328,9 @@ cudaError_t launch_scale(const mxfp8_grad_item* items, int count, const double* 
 {
     return by_tables(items, count, [&](auto& t, unsigned ctas) {
         constexpr int N = sizeof(t.bf16);
-        grad_scale_kernel<N><<<ctas, GRAD_THREADS, 0, st>>>(t, partial, parts, max_norm, norm);
+        const cudaError_t rc = launch_early(grad_scale_kernel<N>, ctas, st, t, partial, parts, max_norm, norm);
         norm = nullptr;                                     // the first launch writes it
-        count_launch(1);
-        return cudaGetLastError();
+        return rc;
     });
 }
 
@@ -293,9 +361,7 @@ extern "C" int mxfp8_grad_sumsq(const mxfp8_grad_item* items, int count, double*
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int parts = 0;
     if (launch_squares(items, count, static_cast<double*>(ws), parts, st) != cudaSuccess) return MXFP8_ERR_CUDA;
-    grad_sum_kernel<<<1, GRAD_THREADS, 0, st>>>(static_cast<const double*>(ws), parts, sumsq);
-    count_launch(1);
-    return cudaGetLastError() == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
+    return launch_early(grad_sum_kernel, 1, st, static_cast<const double*>(ws), parts, sumsq) == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
 }
 
 extern "C" int mxfp8_grad_scale(const mxfp8_grad_item* items, int count, const double* sumsq, float max_norm, float* norm, void* stream)
