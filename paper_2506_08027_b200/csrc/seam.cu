@@ -6,6 +6,8 @@
 // Bound by memory: forward y, h_in -> h, x; backward dx, dh, y, h -> dy, dh_in, each element once.
 #include <cuda_bf16.h>
 
+#include <initializer_list>
+
 #include "mxfp8_device.cuh"
 #include "mxfp8_host.h"
 
@@ -71,42 +73,103 @@ __device__ __forceinline__ void cta_sums(float (&v)[N], float (*area)[SEAM_MAX_W
     turn ^= 1;
 }
 
-// Any width and alignment: a CTA per row, one element per thread at a time, rows read again where a second pass needs them (from L2).
-template <typename Y, typename H>
-__global__ void __launch_bounds__(SEAM_THREADS) seam_forward_any_kernel(const SeamArgs a)
+// ---------------------------------------------------------------------------------------------------------------------
+// Any width and alignment: a CTA per row, NE elements of it in every thread's registers, V neighbours at a time (two where rows have an even
+// number of elements).  All loads of a row are asked for at once; other CTAs cover their latency.
+template <typename T, int V>
+__device__ __forceinline__ void load_few(const T* p, float (&v)[V])
+{
+    if constexpr (V == 1) v[0] = to_float(*p);
+    else if constexpr (sizeof(T) == 2) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(p);
+        v[0] = __uint_as_float(w << 16);
+        v[1] = __uint_as_float(w & 0xFFFF0000u);
+    } else {
+        const float2 w = *reinterpret_cast<const float2*>(p);
+        v[0] = w.x; v[1] = w.y;
+    }
+}
+// Rounds to T; v becomes the rounded values
+template <typename T, int V>
+__device__ __forceinline__ void store_few(T* p, float (&v)[V])
+{
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = __bfloat162float(__float2bfloat16_rn(v[k]));
+    }
+    if constexpr (V == 1) *p = from_float<T>(v[0]);
+    else if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(p) = __float_as_uint(v[0]) >> 16 | (__float_as_uint(v[1]) & 0xFFFF0000u);
+    else *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+}
+template <int V>
+__device__ __forceinline__ void params_few(const void* p, int64_t at, bool bf16, float (&v)[V])
+{
+    if (bf16) load_few<__nv_bfloat16, V>(static_cast<const __nv_bfloat16*>(p) + at, v);
+    else load_few<float, V>(static_cast<const float*>(p) + at, v);
+}
+
+template <typename Y, typename H, int V, int NE>
+__global__ void __launch_bounds__(1024) seam_forward_any_kernel(const SeamArgs a)
 {
     __shared__ float area[2][SEAM_MAX_WARPS][1];
+    constexpr int NV = NE / V;
     int turn = 0;
+    const int T = blockDim.x, t = threadIdx.x;
     const float n_cols = (float)a.cols;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const Y* y = static_cast<const Y*>(a.y) + r * a.cols;
-        const H* h_in = static_cast<const H*>(a.h_in) + r * a.cols;
-        H* h = static_cast<H*>(a.h) + r * a.cols;
-        const int64_t gate = a.gate ? r / a.rows_per_gate * a.cols : 0;
-        float s[1] = {0.f}, rp = 1.f;
+        const int64_t row = r * a.cols, gate = a.gate ? r / a.rows_per_gate * a.cols : 0;
+        float n[NV][V], h[NV][V], s[1] = {0.f}, rp = 1.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (t + i * T) * V;
+            if (c < a.cols) {
+                load_few<Y, V>(static_cast<const Y*>(a.y) + row + c, n[i]);
+                load_few<H, V>(static_cast<const H*>(a.h_in) + row + c, h[i]);
+            } else
+#pragma unroll
+                for (int k = 0; k < V; ++k) n[i][k] = h[i][k] = 0.f;
+        }
         if (a.gamma_post) {
-            for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) s[0] = fmaf(to_float(y[c]), to_float(y[c]), s[0]);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < V; ++k) s[0] = fmaf(n[i][k], n[i][k], s[0]);
             cta_sums(s, area, turn);
             rp = 1.0f / sqrtf(s[0] / n_cols + a.eps);
-            if (threadIdx.x == 0) a.rstd_post[r] = rp;
+            if (t == 0) a.rstd_post[r] = rp;
         }
         s[0] = 0.f;
-        for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) {
-            float n = to_float(y[c]);
-            if (a.gamma_post) n = (n * rp) * param(a.gamma_post, c, a.bf16_params);
-            const float w = a.gate ? a.branch_scale * param(a.gate, gate + c, a.bf16_params) : a.branch_scale;
-            const H v = from_float<H>(fmaf(w, n, a.residual_scale * to_float(h_in[c])));
-            h[c] = v;
-            s[0] = fmaf(to_float(v), to_float(v), s[0]);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (t + i * T) * V;
+            if (c >= a.cols) break;
+            float w[V];
+            if (a.gamma_post) {
+                params_few<V>(a.gamma_post, c, a.bf16_params, w);
+#pragma unroll
+                for (int k = 0; k < V; ++k) n[i][k] = (n[i][k] * rp) * w[k];
+            }
+            if (a.gate) params_few<V>(a.gate, gate + c, a.bf16_params, w);
+#pragma unroll
+            for (int k = 0; k < V; ++k) h[i][k] = fmaf(a.gate ? a.branch_scale * w[k] : a.branch_scale, n[i][k], a.residual_scale * h[i][k]);
+            store_few<H, V>(static_cast<H*>(a.h) + row + c, h[i]);
+#pragma unroll
+            for (int k = 0; k < V; ++k) s[0] = fmaf(h[i][k], h[i][k], s[0]);
         }
         cta_sums(s, area, turn);
         const float rn = 1.0f / sqrtf(s[0] / n_cols + a.eps);
-        if (threadIdx.x == 0) a.rstd_pre[r] = rn;
-        if (a.x) {
-            Y* x = static_cast<Y*>(a.x) + r * a.cols;
-            for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS)              // the thread's own stores
-                x[c] = from_float<Y>((to_float(h[c]) * rn) * param(a.gamma_pre, c, a.bf16_params));
-        }
+        if (t == 0) a.rstd_pre[r] = rn;
+        if (a.x)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * T) * V;
+                if (c >= a.cols) break;
+                float w[V];
+                params_few<V>(a.gamma_pre, c, a.bf16_params, w);
+#pragma unroll
+                for (int k = 0; k < V; ++k) w[k] = (h[i][k] * rn) * w[k];
+                store_few<Y, V>(static_cast<Y*>(a.x) + row + c, w);
+            }
     }
 }
 
@@ -124,6 +187,133 @@ __device__ __forceinline__ float* gate_part(const SeamArgs& a, int64_t g)
     return a.ws + weights + (blockIdx.x + g) * a.cols;
 }
 
+// The CTA's column sums of the weights, [CTA][cols] for each
+__device__ __forceinline__ float* weights_part(const SeamArgs& a, bool post)
+{
+    return a.ws + ((int64_t)blockIdx.x + (post && a.d_gamma_pre ? gridDim.x : 0)) * a.cols;
+}
+
+template <typename Y, typename H, int V, int NE>
+__global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(const SeamArgs a)
+{
+    __shared__ float area[2][SEAM_MAX_WARPS][3];
+    constexpr int NV = NE / V;
+    int turn = 0;
+    const int T = blockDim.x, t = threadIdx.x;
+    const int64_t r0 = blockIdx.x * a.chunk, r1 = min(r0 + a.chunk, a.rows);
+    const float inv_cols = 1.0f / (float)a.cols;
+    float pre[NV][V], post[NV][V], gates[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < V; ++k) pre[i][k] = post[i][k] = gates[i][k] = 0.f;
+    for (int64_t r = r0; r < r1; ++r) {
+        const int64_t row = r * a.cols, g = a.gate ? r / a.rows_per_gate : 0;
+        const float rn = a.rstd_pre[r], rp = a.gamma_post ? a.rstd_post[r] : 1.f;
+        float dx[NV][V], dh[NV][V], y[NV][V], h[NV][V], s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (t + i * T) * V;
+#pragma unroll
+            for (int k = 0; k < V; ++k) dx[i][k] = dh[i][k] = y[i][k] = h[i][k] = 0.f;
+            if (c >= a.cols) continue;
+            if (a.dx) load_few<Y, V>(static_cast<const Y*>(a.dx) + row + c, dx[i]);
+            load_few<Y, V>(static_cast<const Y*>(a.y) + row + c, y[i]);
+            if (a.dh) load_few<H, V>(static_cast<const H*>(a.dh) + row + c, dh[i]);
+            load_few<H, V>(static_cast<const H*>(static_cast<const void*>(a.h)) + row + c, h[i]);
+        }
+        // y, h become yh, xh
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (t + i * T) * V;
+            if (c >= a.cols) break;
+            float w[V], q[V];
+            params_few<V>(a.gamma_pre, c, a.bf16_params, w);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                h[i][k] *= rn;
+                y[i][k] *= rp;
+                w[k] *= dx[i][k];
+                s[0] = fmaf(w[k], h[i][k], s[0]);
+            }
+            if (a.gamma_post) {
+                float u[V];
+                params_few<V>(a.gamma_post, c, a.bf16_params, u);
+                if (a.gate) {
+                    params_few<V>(a.gate, g * a.cols + c, a.bf16_params, q);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) u[k] *= q[k];
+                }
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    u[k] *= y[i][k];
+                    s[1] = fmaf(u[k], fmaf(rn, w[k], dh[i][k]), s[1]);
+                    s[2] = fmaf(u[k], h[i][k], s[2]);
+                }
+            }
+        }
+        cta_sums(s, area, turn);
+        const float c1 = s[0] * inv_cols, c2 = (s[1] - rn * c1 * s[2]) * a.branch_scale * inv_cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (t + i * T) * V;
+            if (c >= a.cols) break;
+            float w[V], G[V];
+            params_few<V>(a.gamma_pre, c, a.bf16_params, w);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                pre[i][k] = fmaf(dx[i][k], h[i][k], pre[i][k]);
+                G[k] = fmaf(rn, fmaf(dx[i][k], w[k], -h[i][k] * c1), dh[i][k]);
+                w[k] = a.residual_scale * G[k];
+                G[k] *= a.branch_scale;
+            }
+            if (a.dh_in) store_few<H, V>(static_cast<H*>(a.dh_in) + row + c, w);
+#pragma unroll
+            for (int k = 0; k < V; ++k) w[k] = 1.f;
+            if (a.gamma_post) params_few<V>(a.gamma_post, c, a.bf16_params, w);
+            if (a.d_gate)
+#pragma unroll
+                for (int k = 0; k < V; ++k) gates[i][k] = fmaf(G[k], y[i][k] * w[k], gates[i][k]);
+            if (a.gate) {
+                float q[V];
+                params_few<V>(a.gate, g * a.cols + c, a.bf16_params, q);
+#pragma unroll
+                for (int k = 0; k < V; ++k) G[k] *= q[k];
+            }
+            if (a.gamma_post)
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    post[i][k] = fmaf(G[k], y[i][k], post[i][k]);
+                    G[k] = rp * fmaf(G[k], w[k], -y[i][k] * c2);
+                }
+            if (a.dy) store_few<Y, V>(static_cast<Y*>(a.dy) + row + c, G);
+        }
+        if (a.d_gate && (r + 1 == r1 || (r + 1) / a.rows_per_gate != g)) {
+            float* part = gate_part(a, g);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * T) * V;
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    if (c < a.cols) part[c + k] = gates[i][k];
+                    gates[i][k] = 0.f;
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (t + i * T) * V;
+        if (c >= a.cols) break;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            if (a.d_gamma_pre) weights_part(a, false)[c + k] = pre[i][k];
+            if (a.d_gamma_post) weights_part(a, true)[c + k] = post[i][k];
+        }
+    }
+}
+
+// The same for rows of any length: one element per thread at a time, column sums in shared memory, rows read a second time (from L2).
 template <typename Y, typename H>
 __global__ void __launch_bounds__(SEAM_THREADS) seam_grad_any_kernel(const SeamArgs a)
 {
@@ -179,13 +369,10 @@ __global__ void __launch_bounds__(SEAM_THREADS) seam_grad_any_kernel(const SeamA
             }
         }
     }
-    float* to = a.ws + (int64_t)blockIdx.x * a.cols;
-    if (a.d_gamma_pre) {
-        for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) to[c] = pre[c];
-        to += (int64_t)gridDim.x * a.cols;
+    for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) {
+        if (a.d_gamma_pre) weights_part(a, false)[c] = pre[c];
+        if (a.d_gamma_post) weights_part(a, true)[c] = post[c];
     }
-    if (a.d_gamma_post)
-        for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) to[c] = post[c];
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -354,7 +541,7 @@ __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : 512), WARP ? 8 
 
 // Backward: same ownership and the same sums as seam_grad_any_kernel; column sums stay in registers.
 template <typename Y, typename H, int NV, int STAGES>
-__global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 2 : 1) seam_grad_kernel(const SeamArgs a)
+__global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 3 : 1) seam_grad_kernel(const SeamArgs a)
 {
     extern __shared__ __align__(16) uint8_t stage_mem[];
     __shared__ float area[2][SEAM_MAX_WARPS][3];
@@ -510,21 +697,21 @@ __global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 2 : 1) seam_gra
         stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
     copies_done<0>();
-    float* to = a.ws + (int64_t)blockIdx.x * a.cols;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (t + i * T) * 8;
         if (c >= a.cols) break;
-        if (a.d_gamma_pre) store8(to + c, pre[i]);
-        if (a.d_gamma_post) store8(to + (a.d_gamma_pre ? (int64_t)gridDim.x * a.cols : 0) + c, post[i]);
+        if (a.d_gamma_pre) store8(weights_part(a, false) + c, pre[i]);
+        if (a.d_gamma_post) store8(weights_part(a, true) + c, post[i]);
     }
 }
 
 // Joins the CTAs' sums.  blockIdx.y: 0 / 1 the weights, then the rows of the gate that several CTAs hold.
-constexpr int JOIN_COLS = 32, JOIN_WARPS = 8;
+constexpr int JOIN_COLS = 32, JOIN_WARPS = 32;
 __global__ void __launch_bounds__(32 * JOIN_WARPS) seam_join_kernel(const SeamArgs a, int parts)
 {
-    __shared__ float area[JOIN_WARPS][JOIN_COLS];
+    __shared__ float area[JOIN_WARPS][JOIN_COLS + 1];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * JOIN_COLS + lane, weights = (a.d_gamma_pre != nullptr) + (a.d_gamma_post != nullptr);
     for (int64_t which = blockIdx.y; which < weights + (a.d_gate ? a.gates : 0); which += gridDim.y) {
@@ -543,15 +730,16 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) seam_join_kernel(const SeamAr
             to = a.d_gate + g * a.cols;
         }
         float s = 0.f;
-        if (c < a.cols)
+        if (c < a.cols) {
+#pragma unroll 8
             for (int64_t p = warp; p < count; p += JOIN_WARPS) s += from[p * a.cols + c];
+        }
         area[warp][lane] = s;
         __syncthreads();
-        if (warp == 0) {
-            s = 0.f;
-            for (int w = 0; w < JOIN_WARPS; ++w) s += area[w][lane];
-            if (c < a.cols) to[c] = s;
-        }
+        s = area[lane][warp];                               // warp w adds column w
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, off);
+        if (lane == 0 && blockIdx.x * JOIN_COLS + warp < a.cols) to[blockIdx.x * JOIN_COLS + warp] = s;
         __syncthreads();
     }
 }
@@ -607,6 +795,17 @@ bool rows_aligned(const SeamArgs& a, const P*... p)
     return a.cols % 8 == 0 && (aligned16(p) && ...) && aligned16(a.gamma_post) && aligned16(a.gate) && aligned16(a.gamma_pre);
 }
 
+// Rows of an even number of elements that start on boundaries of two elements
+template <typename Y, typename H>
+bool even_rows(const SeamArgs& a, std::initializer_list<const void*> block, std::initializer_list<const void*> stream)
+{
+    uintptr_t off = 0;
+    for (const void* p : block) off |= reinterpret_cast<uintptr_t>(p) & (2 * sizeof(Y) - 1);
+    for (const void* p : stream) off |= reinterpret_cast<uintptr_t>(p) & (2 * sizeof(H) - 1);
+    for (const void* p : {a.gamma_post, a.gate, a.gamma_pre}) off |= reinterpret_cast<uintptr_t>(p) & (a.bf16_params ? 3u : 7u);
+    return a.cols % 2 == 0 && off == 0;
+}
+
 constexpr int SMEM_PER_SM = 224 * 1024;
 
 template <typename Y, typename H, int NV, bool WARP, int STAGES>
@@ -628,8 +827,15 @@ template <typename Y, typename H>
 cudaError_t launch_forward(const SeamArgs& a, cudaStream_t st)
 {
     if (!rows_aligned(a, a.y, a.h_in, a.h, a.x)) {
-        const int64_t most = (int64_t)multiprocessors() * 8;
-        seam_forward_any_kernel<Y, H><<<(unsigned)(a.rows < most ? a.rows : most), SEAM_THREADS, 0, st>>>(a);
+        const int few = a.cols <= 2048 ? 8 : 16, threads = (a.cols + 32 * few - 1) / (32 * few) * 32;
+        const int per_sm = 1536 / threads < 16 ? 1536 / threads : 16;
+        const int64_t most = (int64_t)multiprocessors() * (per_sm < 1 ? 1 : per_sm);
+        const unsigned ctas = (unsigned)(a.rows < most ? a.rows : most);
+        const bool two = even_rows<Y, H>(a, {a.y, a.x}, {a.h_in, a.h});
+        if (few == 8 && two) seam_forward_any_kernel<Y, H, 2, 8><<<ctas, threads, 0, st>>>(a);
+        else if (few == 8) seam_forward_any_kernel<Y, H, 1, 8><<<ctas, threads, 0, st>>>(a);
+        else if (two) seam_forward_any_kernel<Y, H, 2, 16><<<ctas, threads, 0, st>>>(a);
+        else seam_forward_any_kernel<Y, H, 1, 16><<<ctas, threads, 0, st>>>(a);
         count_launch(1);
         return cudaGetLastError();
     }
@@ -643,10 +849,11 @@ cudaError_t launch_forward(const SeamArgs& a, cudaStream_t st)
     return launch_forward_rows<Y, H, 4, false, PIECES<Y> + PIECES<H> == 4 ? 1 : 2>(a, 32 * ((warps + 3) / 4), st);
 }
 
-// Rows of a CTA of the backward pass: two to eight CTAs per multiprocessor, by the width, while a row remains for each.
+// CTAs of the backward pass per multiprocessor, by the width alone (the workspace's size follows from it): as many as registers allow.
+int grad_ctas_per_sm(int64_t cols) { return cols > 4096 ? 1 : (cols > 2048 ? 2 : (cols > 1024 ? 3 : (cols > 512 ? 5 : 8))); }
 int64_t grad_chunk(int64_t rows, int64_t cols)
 {
-    const int64_t per_sm = cols > 4096 ? 2 : (cols > 1024 ? 8192 / cols : 8), ctas = per_sm * multiprocessors();
+    const int64_t ctas = (int64_t)grad_ctas_per_sm(cols) * multiprocessors();
     return (rows + ctas - 1) / ctas;
 }
 
@@ -668,11 +875,24 @@ cudaError_t launch_grad(SeamArgs a, cudaStream_t st)
     cudaError_t rc;
     // a row of the four inputs has to fit shared memory (it does but for rows of 16384 FP32 numbers)
     if (rows_aligned(a, a.dx, a.dh, a.y, a.h, a.dy, a.dh_in, a.d_gate) && a.cols * 2 * (int)(sizeof(Y) + sizeof(H)) <= SMEM_PER_SM) {
-        constexpr bool WIDE = PIECES<Y> + PIECES<H> == 4;
+        constexpr int Q = PIECES<Y> + PIECES<H>;
         const int warps = (a.cols / 8 + 31) / 32;
-        if (warps <= 8) rc = launch_grad_rows<Y, H, 1, 3>(a, 32 * warps, ctas, st);
-        else if (warps <= (WIDE ? 24 : 32)) rc = launch_grad_rows<Y, H, 2, 2>(a, 32 * ((warps + 1) / 2), ctas, st);
+        if (warps <= 8) rc = launch_grad_rows<Y, H, 1, Q == 4 ? 2 : 3>(a, 32 * warps, ctas, st);
+        else if (warps <= 16) rc = launch_grad_rows<Y, H, 2, Q == 2 ? 3 : (Q == 3 ? 2 : 1)>(a, 32 * ((warps + 1) / 2), ctas, st);
+        else if (warps <= 32) rc = launch_grad_rows<Y, H, 2, Q == 2 ? 3 : (Q == 3 ? 2 : 1)>(a, 32 * ((warps + 1) / 2), ctas, st);
         else rc = launch_grad_rows<Y, H, 4, 1>(a, 32 * ((warps + 3) / 4), ctas, st);
+    } else if (a.cols <= 8192) {
+        const int few = a.cols <= 2048 ? 4 : 8, threads = (a.cols + 32 * few - 1) / (32 * few) * 32;
+        const bool two = even_rows<Y, H>(a, {a.dx, a.y, a.dy}, {a.dh, a.h, a.dh_in});
+        if (threads > 512) {
+            if (two) seam_grad_few_kernel<Y, H, 2, 16><<<ctas, (a.cols + 511) / 512 * 32, 0, st>>>(a);
+            else seam_grad_few_kernel<Y, H, 1, 16><<<ctas, (a.cols + 511) / 512 * 32, 0, st>>>(a);
+        } else if (few == 4) {
+            if (two) seam_grad_few_kernel<Y, H, 2, 4><<<ctas, threads, 0, st>>>(a);
+            else seam_grad_few_kernel<Y, H, 1, 4><<<ctas, threads, 0, st>>>(a);
+        } else if (two) seam_grad_few_kernel<Y, H, 2, 8><<<ctas, threads, 0, st>>>(a);
+        else seam_grad_few_kernel<Y, H, 1, 8><<<ctas, threads, 0, st>>>(a);
+        rc = cudaGetLastError();
     } else {
         auto kernel = seam_grad_any_kernel<Y, H>;
         static unsigned long long set = 0;
@@ -684,9 +904,18 @@ cudaError_t launch_grad(SeamArgs a, cudaStream_t st)
     count_launch(1);
     const int64_t joins = (a.d_gamma_pre != nullptr) + (a.d_gamma_post != nullptr) + (a.d_gate ? a.gates : 0);
     if (rc != cudaSuccess || joins == 0) return rc;
-    seam_join_kernel<<<dim3((a.cols + JOIN_COLS - 1) / JOIN_COLS, (unsigned)(joins < 1024 ? joins : 1024)), 32 * JOIN_WARPS, 0, st>>>(a, (int)ctas);
-    count_launch(1);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};                               // begins while the first launch ends, and waits for it itself
+    cfg.gridDim = dim3((a.cols + JOIN_COLS - 1) / JOIN_COLS, (unsigned)(joins < 1024 ? joins : 1024));
+    cfg.blockDim = dim3(32 * JOIN_WARPS);
+    cfg.stream = st;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    rc = cudaLaunchKernelEx(&cfg, seam_join_kernel, a, (int)ctas);
+    if (rc == cudaSuccess) count_launch(1);
+    return rc;
 }
 
 int seam_forward(const mxfp8_seam* s, const void* y, const void* h_in, void* h, void* x, float* rstd_post, float* rstd_pre, cudaStream_t st)
