@@ -34,6 +34,7 @@ struct SeamArgs {
     float* ws;
     int64_t chunk;                               // rows of a CTA
     int64_t gates;
+    uint32_t gate_magic;                         // of rows_per_gate, where rows fit 31 bits
 };
 
 __device__ __forceinline__ float to_float(float v) { return v; }
@@ -47,31 +48,91 @@ __device__ __forceinline__ float param(const void* p, int64_t at, bool bf16)
     return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]) : static_cast<const float*>(p)[at];
 }
 
-template <int N>
-__device__ __forceinline__ void warp_sums(float (&v)[N])
+__device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], off);
+    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
+    return v;
 }
 
-// Sums of N values over the CTA, the same in every thread and in a fixed order.  `turn` alternates between two areas, so that one
-// barrier per call is enough.
-template <int N>
-__device__ __forceinline__ void cta_sums(float (&v)[N], float (*area)[SEAM_MAX_WARPS][N], int& turn)
+// Sums over the CTA, the same in every thread and in a fixed order.  `turn` alternates between two areas, so that one barrier per call is
+// enough.  Every warp adds the warps' sums the same way.
+__device__ __forceinline__ float cta_sum(float v, float (*area)[SEAM_MAX_WARPS], int& turn)
 {
-    warp_sums(v);
-    if ((threadIdx.x & 31) == 0)
-#pragma unroll
-        for (int i = 0; i < N; ++i) area[turn][threadIdx.x >> 5][i] = v[i];
-    __syncthreads();
-    // every warp adds the warps' sums the same way
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = (threadIdx.x & 31) < (blockDim.x >> 5) ? area[turn][threadIdx.x & 31][i] : 0.f;
-    warp_sums(v);
+    v = warp_sum(v);
+    float* here = area[turn];
     turn ^= 1;
+    if ((threadIdx.x & 31) == 0) here[threadIdx.x >> 5] = v;
+    __syncthreads();
+    const int warps = blockDim.x >> 5;
+    if (warps <= 4) {
+        v = here[0];
+        for (int w = 1; w < warps; ++w) v += here[w];
+        return v;
+    }
+    v = (threadIdx.x & 31) < warps ? here[threadIdx.x & 31] : 0.f;
+    if (warps > 8) {
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
+    }
+#pragma unroll
+    for (int off = 4; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);
+    return __shfl_sync(0xFFFFFFFFu, v, 0);
 }
+
+// Three sums at once.  The first two steps of the tree hand half of the values to the other half of the lanes, so that the warp needs six
+// shuffles instead of fifteen; lanes 0, 8 and 16 end with the sums.
+__device__ __forceinline__ void cta_sums(float (&v)[3], float4 (*area)[SEAM_MAX_WARPS], int& turn)
+{
+    const int lane = threadIdx.x & 31;
+    const bool high = lane & 16, odd = lane & 8;
+    float a = high ? v[2] : v[0], b = high ? 0.f : v[1];
+    a += __shfl_xor_sync(0xFFFFFFFFu, high ? v[0] : v[2], 16);
+    b += __shfl_xor_sync(0xFFFFFFFFu, high ? v[1] : 0.f, 16);
+    float s = odd ? b : a;
+    s += __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 8);
+#pragma unroll
+    for (int off = 4; off > 0; off >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, off);
+    float4* here = area[turn];
+    turn ^= 1;
+    if ((lane & 7) == 0) reinterpret_cast<float*>(here + (threadIdx.x >> 5))[lane >> 3] = s;          // sums 0, 1, 2 and nothing
+    __syncthreads();
+    const int warps = blockDim.x >> 5;
+    float4 all = here[0];
+#pragma unroll 4
+    for (int w = 1; w < warps; ++w) {
+        const float4 more = here[w];
+        all.x += more.x; all.y += more.y; all.z += more.z;
+    }
+    v[0] = all.x; v[1] = all.y; v[2] = all.z;
+}
+
+// 1 / sqrt(mean + eps), within two units of the last place
+__device__ __forceinline__ float rstd_of(float sum, float cols, float eps) { return rsqrtf(sum / cols + eps); }
+
+// The row of the gate for row r
+__device__ __forceinline__ int64_t gate_row(const SeamArgs& a, int64_t r)
+{
+    if (a.rows > 0x7FFFFFFFLL) return r / a.rows_per_gate;
+    int g, rest;
+    divmod((uint32_t)r, (uint32_t)a.rows_per_gate, a.gate_magic, g, rest);
+    return g;
+}
+
+// What a kernel may know of a seam when it is compiled: nothing (0), or that all tensors and both norms are there, the parameters have
+// the stream's type and there is no gate (1) or one whose gradient is wanted (2).
+template <int MODE, typename H>
+struct Known {
+    const SeamArgs& a;
+    __device__ __forceinline__ bool post() const { return MODE != 0 || a.gamma_post != nullptr; }
+    __device__ __forceinline__ bool gate() const { return MODE == 2 || (MODE == 0 && a.gate != nullptr); }
+    __device__ __forceinline__ bool d_gate() const { return MODE == 2 || (MODE == 0 && a.d_gate != nullptr); }
+    __device__ __forceinline__ bool dx() const { return MODE != 0 || a.dx != nullptr; }
+    __device__ __forceinline__ bool dh() const { return MODE != 0 || a.dh != nullptr; }
+    __device__ __forceinline__ bool dy() const { return MODE != 0 || a.dy != nullptr; }
+    __device__ __forceinline__ bool dh_in() const { return MODE != 0 || a.dh_in != nullptr; }
+    __device__ __forceinline__ bool bf16() const { return MODE != 0 ? sizeof(H) == 2 : a.bf16_params; }
+};
 
 // ---------------------------------------------------------------------------------------------------------------------
 // Any width and alignment: a CTA per row, NE elements of it in every thread's registers, V neighbours at a time (two where rows have an even
@@ -109,16 +170,16 @@ __device__ __forceinline__ void params_few(const void* p, int64_t at, bool bf16,
 }
 
 template <typename Y, typename H, int V, int NE>
-__global__ void __launch_bounds__(1024) seam_forward_any_kernel(const SeamArgs a)
+__global__ void __launch_bounds__(NE == 8 ? 256 : 1024, NE == 8 ? 6 : 1) seam_forward_any_kernel(const SeamArgs a)
 {
-    __shared__ float area[2][SEAM_MAX_WARPS][1];
+    __shared__ float area[2][SEAM_MAX_WARPS];
     constexpr int NV = NE / V;
     int turn = 0;
     const int T = blockDim.x, t = threadIdx.x;
     const float n_cols = (float)a.cols;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const int64_t row = r * a.cols, gate = a.gate ? r / a.rows_per_gate * a.cols : 0;
-        float n[NV][V], h[NV][V], s[1] = {0.f}, rp = 1.f;
+        const int64_t row = r * a.cols, gate = a.gate ? gate_row(a, r) * a.cols : 0;
+        float n[NV][V], h[NV][V], s = 0.f, rp = 1.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (t + i * T) * V;
@@ -133,12 +194,11 @@ __global__ void __launch_bounds__(1024) seam_forward_any_kernel(const SeamArgs a
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int k = 0; k < V; ++k) s[0] = fmaf(n[i][k], n[i][k], s[0]);
-            cta_sums(s, area, turn);
-            rp = 1.0f / sqrtf(s[0] / n_cols + a.eps);
+                for (int k = 0; k < V; ++k) s = fmaf(n[i][k], n[i][k], s);
+            rp = rstd_of(cta_sum(s, area, turn), n_cols, a.eps);
             if (t == 0) a.rstd_post[r] = rp;
         }
-        s[0] = 0.f;
+        s = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (t + i * T) * V;
@@ -149,15 +209,18 @@ __global__ void __launch_bounds__(1024) seam_forward_any_kernel(const SeamArgs a
 #pragma unroll
                 for (int k = 0; k < V; ++k) n[i][k] = (n[i][k] * rp) * w[k];
             }
-            if (a.gate) params_few<V>(a.gate, gate + c, a.bf16_params, w);
+            if (a.gate) {
+                params_few<V>(a.gate, gate + c, a.bf16_params, w);
 #pragma unroll
-            for (int k = 0; k < V; ++k) h[i][k] = fmaf(a.gate ? a.branch_scale * w[k] : a.branch_scale, n[i][k], a.residual_scale * h[i][k]);
+                for (int k = 0; k < V; ++k) n[i][k] *= w[k];
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) h[i][k] = fmaf(a.branch_scale, n[i][k], a.residual_scale * h[i][k]);
             store_few<H, V>(static_cast<H*>(a.h) + row + c, h[i]);
 #pragma unroll
-            for (int k = 0; k < V; ++k) s[0] = fmaf(h[i][k], h[i][k], s[0]);
+            for (int k = 0; k < V; ++k) s = fmaf(h[i][k], h[i][k], s);
         }
-        cta_sums(s, area, turn);
-        const float rn = 1.0f / sqrtf(s[0] / n_cols + a.eps);
+        const float rn = rstd_of(cta_sum(s, area, turn), n_cols, a.eps);
         if (t == 0) a.rstd_pre[r] = rn;
         if (a.x)
 #pragma unroll
@@ -196,7 +259,7 @@ __device__ __forceinline__ float* weights_part(const SeamArgs& a, bool post)
 template <typename Y, typename H, int V, int NE>
 __global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(const SeamArgs a)
 {
-    __shared__ float area[2][SEAM_MAX_WARPS][3];
+    __shared__ float4 area[2][SEAM_MAX_WARPS];
     constexpr int NV = NE / V;
     int turn = 0;
     const int T = blockDim.x, t = threadIdx.x;
@@ -208,7 +271,7 @@ __global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(con
 #pragma unroll
         for (int k = 0; k < V; ++k) pre[i][k] = post[i][k] = gates[i][k] = 0.f;
     for (int64_t r = r0; r < r1; ++r) {
-        const int64_t row = r * a.cols, g = a.gate ? r / a.rows_per_gate : 0;
+        const int64_t row = r * a.cols, g = a.gate ? gate_row(a, r) : 0;
         const float rn = a.rstd_pre[r], rp = a.gamma_post ? a.rstd_post[r] : 1.f;
         float dx[NV][V], dh[NV][V], y[NV][V], h[NV][V], s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
@@ -288,7 +351,7 @@ __global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(con
                 }
             if (a.dy) store_few<Y, V>(static_cast<Y*>(a.dy) + row + c, G);
         }
-        if (a.d_gate && (r + 1 == r1 || (r + 1) / a.rows_per_gate != g)) {
+        if (a.d_gate && (r + 1 == r1 || (g + 1) * a.rows_per_gate == r + 1)) {
             float* part = gate_part(a, g);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -318,7 +381,7 @@ template <typename Y, typename H>
 __global__ void __launch_bounds__(SEAM_THREADS) seam_grad_any_kernel(const SeamArgs a)
 {
     extern __shared__ float column[];              // d_gamma_pre, d_gamma_post, d_gate: each column belongs to one thread
-    __shared__ float area[2][SEAM_MAX_WARPS][3];
+    __shared__ float4 area[2][SEAM_MAX_WARPS];
     int turn = 0;
     float *pre = column, *post = column + a.cols, *gates = column + 2 * a.cols;
     for (int c = threadIdx.x; c < 3 * a.cols; c += SEAM_THREADS) column[c] = 0.f;
@@ -332,7 +395,7 @@ __global__ void __launch_bounds__(SEAM_THREADS) seam_grad_any_kernel(const SeamA
         const H* dh = a.dh ? static_cast<const H*>(a.dh) + r * a.cols : nullptr;
         Y* dy = a.dy ? static_cast<Y*>(a.dy) + r * a.cols : nullptr;
         H* dh_in = a.dh_in ? static_cast<H*>(a.dh_in) + r * a.cols : nullptr;
-        const int64_t g = a.gate ? r / a.rows_per_gate : 0;
+        const int64_t g = a.gate ? gate_row(a, r) : 0;
         const float rn = a.rstd_pre[r], rp = a.gamma_post ? a.rstd_post[r] : 1.f;
         float s[3] = {0.f, 0.f, 0.f};
         for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) {
@@ -361,7 +424,7 @@ __global__ void __launch_bounds__(SEAM_THREADS) seam_grad_any_kernel(const SeamA
             post[c] = fmaf(wG, yh, post[c]);
             if (dy) dy[c] = from_float<Y>(a.gamma_post ? rp * (wG * gamma - yh * c2) : wG);
         }
-        if (a.d_gate && (r + 1 == r1 || (r + 1) / a.rows_per_gate != g)) {
+        if (a.d_gate && (r + 1 == r1 || (g + 1) * a.rows_per_gate == r + 1)) {
             float* to = gate_part(a, g);
             for (int c = threadIdx.x; c < a.cols; c += SEAM_THREADS) {
                 to[c] = gates[c];
@@ -389,67 +452,104 @@ __device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_
 template <int LEFT>
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" :: "n"(LEFT) : "memory"); }
 
+// Eight FP32 values as four pairs: one instruction works on a pair (the same roundings as one at a time, half the issue slots).
+struct Eight {
+    float2 v[4];
+};
+__device__ __forceinline__ uint64_t bits(float2 v)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+    return r;
+}
+__device__ __forceinline__ float2 pair(uint64_t b)
+{
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(b));
+    return v;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+    return pair(r);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return pair(r);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ Eight zero8()
+{
+    Eight e;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e.v[k] = make_float2(0.f, 0.f);
+    return e;
+}
+
 // Eight elements from 16-byte pieces, `apart` bytes from one another in shared memory / side by side in global memory
 template <typename T>
-__device__ __forceinline__ void unpack(const uint4 (&w)[PIECES<T>], float (&v)[8])
+__device__ __forceinline__ Eight unpack(const uint4 (&w)[PIECES<T>])
 {
     const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
-    if constexpr (sizeof(T) == 2) {
+    Eight e;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { v[2 * k] = __uint_as_float(u[k] << 16); v[2 * k + 1] = __uint_as_float(u[k] & 0xFFFF0000u); }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(u[k]);
-    }
+    for (int k = 0; k < 4; ++k)
+        e.v[k] = sizeof(T) == 2 ? make_float2(__uint_as_float(u[k] << 16), __uint_as_float(u[k] & 0xFFFF0000u))
+                                : make_float2(__uint_as_float(u[(2 * k) % (4 * PIECES<T>)]), __uint_as_float(u[(2 * k + 1) % (4 * PIECES<T>)]));
+    return e;
 }
 template <typename T>
-__device__ __forceinline__ void load_staged(const uint8_t* at, int apart, float (&v)[8])
+__device__ __forceinline__ Eight load_staged(const uint8_t* at, int apart)
 {
     uint4 w[PIECES<T>];
 #pragma unroll
     for (int p = 0; p < PIECES<T>; ++p) w[p] = *reinterpret_cast<const uint4*>(at + p * apart);
-    unpack<T>(w, v);
+    return unpack<T>(w);
 }
-// Rounds to T; v becomes the rounded values
+// Stores as T and returns the rounded values
 template <typename T>
-__device__ __forceinline__ void store8(T* to, float (&v)[8])
+__device__ __forceinline__ Eight store8(T* to, const Eight& e)
 {
     uint4* out = reinterpret_cast<uint4*>(to);
     if constexpr (sizeof(T) == 2) {
         uint32_t u[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+            const __nv_bfloat162 b = __floats2bfloat162_rn(e.v[k].x, e.v[k].y);
             u[k] = *reinterpret_cast<const uint32_t*>(&b);
-            v[2 * k] = __uint_as_float(u[k] << 16);
-            v[2 * k + 1] = __uint_as_float(u[k] & 0xFFFF0000u);
         }
-        out[0] = make_uint4(u[0], u[1], u[2], u[3]);
+        const uint4 w[1] = {make_uint4(u[0], u[1], u[2], u[3])};
+        out[0] = w[0];
+        return unpack<__nv_bfloat16>(w);
     } else {
-        out[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-        out[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+        out[0] = make_uint4(__float_as_uint(e.v[0].x), __float_as_uint(e.v[0].y), __float_as_uint(e.v[1].x), __float_as_uint(e.v[1].y));
+        out[1] = make_uint4(__float_as_uint(e.v[2].x), __float_as_uint(e.v[2].y), __float_as_uint(e.v[3].x), __float_as_uint(e.v[3].y));
+        return e;
     }
 }
 // Eight weights of a row of parameters; they stay in L1 from row to row
-__device__ __forceinline__ void params8(const void* p, int64_t at, bool bf16, float (&v)[8])
+__device__ __forceinline__ Eight params8(const void* p, int64_t at, bool bf16)
 {
     if (bf16) {
         const uint4 w[1] = {__ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + at))};
-        unpack<__nv_bfloat16>(w, v);
-    } else {
-        const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + at);
-        const uint4 w[2] = {__ldg(q), __ldg(q + 1)};
-        unpack<float>(w, v);
+        return unpack<__nv_bfloat16>(w);
     }
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + at);
+    const uint4 w[2] = {__ldg(q), __ldg(q + 1)};
+    return unpack<float>(w);
 }
 
 // Forward.  WARP: rows of a warp each (the CTA has four), else of the CTA.
-template <typename Y, typename H, int NV, bool WARP, int STAGES>
-__global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : 512), WARP ? 8 : (NV == 1 ? 1 : 2)) seam_forward_kernel(const SeamArgs a)
+template <typename Y, typename H, int NV, bool WARP, int STAGES, int MODE>
+__global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 : 256)), WARP ? 8 : (NV == 1 ? 1 : (NV == 8 ? 2 : (NV == 2 ? 2 : 4)))) seam_forward_kernel(const SeamArgs a)
 {
     extern __shared__ __align__(16) uint8_t stage_mem[];
-    __shared__ float area[2][SEAM_MAX_WARPS][1];
+    __shared__ float area[2][SEAM_MAX_WARPS];
     constexpr int Q = PIECES<Y> + PIECES<H>;                // 16-byte pieces of a vector of both inputs
+    const Known<MODE, H> known{a};
     int turn = 0;
     const int T = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x;
     const int64_t first = WARP ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5) : blockIdx.x, step = WARP ? (int64_t)gridDim.x * 4 : gridDim.x;
@@ -481,56 +581,54 @@ __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : 512), WARP ? 8 
         issue(r + (STAGES - 1) * step, (stage + STAGES - 1) % STAGES);
         copies_done<STAGES - 1>();
         const uint8_t* at = mine + stage * NV * Q * piece;
-        float s[1] = {0.f}, rp = 1.f;
-        if (a.gamma_post) {
+        float2 s = make_float2(0.f, 0.f);
+        float rp = 1.f;
+        if (known.post()) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 if ((t + i * T) * 8 >= a.cols) break;
-                float y[8];
-                load_staged<Y>(at + i * Q * piece, piece, y);
+                const Eight y = load_staged<Y>(at + i * Q * piece, piece);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) s[0] = fmaf(y[k], y[k], s[0]);
+                for (int k = 0; k < 4; ++k) s = fma2(y.v[k], y.v[k], s);
             }
-            if constexpr (WARP) warp_sums(s);
-            else cta_sums(s, area, turn);
-            rp = 1.0f / sqrtf(s[0] / n_cols + a.eps);
+            rp = rstd_of(WARP ? warp_sum(s.x + s.y) : cta_sum(s.x + s.y, area, turn), n_cols, a.eps);
             if (t == 0) a.rstd_post[r] = rp;
         }
-        s[0] = 0.f;
-        float h[NV][8];
-        const int64_t gate = a.gate ? r / a.rows_per_gate * a.cols : 0;
+        s = make_float2(0.f, 0.f);
+        Eight h[NV];
+        const int64_t gate = known.gate() ? gate_row(a, r) * a.cols : 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (t + i * T) * 8;
             if (c >= a.cols) break;
-            float n[8], w[8];
-            load_staged<Y>(at + i * Q * piece, piece, n);
-            load_staged<H>(at + (i * Q + PIECES<Y>) * piece, piece, h[i]);
-            if (a.gamma_post) {
-                params8(a.gamma_post, c, a.bf16_params, w);
+            Eight n = load_staged<Y>(at + i * Q * piece, piece);
+            h[i] = load_staged<H>(at + (i * Q + PIECES<Y>) * piece, piece);
+            if (known.post()) {
+                const Eight w = params8(a.gamma_post, c, known.bf16());
 #pragma unroll
-                for (int k = 0; k < 8; ++k) n[k] = (n[k] * rp) * w[k];
+                for (int k = 0; k < 4; ++k) n.v[k] = mul2(mul2(n.v[k], both(rp)), w.v[k]);
             }
-            if (a.gate) params8(a.gate, gate + c, a.bf16_params, w);
+            if (known.gate()) {
+                const Eight w = params8(a.gate, gate + c, known.bf16());
 #pragma unroll
-            for (int k = 0; k < 8; ++k) h[i][k] = fmaf(a.gate ? a.branch_scale * w[k] : a.branch_scale, n[k], a.residual_scale * h[i][k]);
-            store8(static_cast<H*>(a.h) + r * a.cols + c, h[i]);
+                for (int k = 0; k < 4; ++k) n.v[k] = mul2(n.v[k], w.v[k]);
+            }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s[0] = fmaf(h[i][k], h[i][k], s[0]);
+            for (int k = 0; k < 4; ++k) h[i].v[k] = fma2(both(a.branch_scale), n.v[k], mul2(both(a.residual_scale), h[i].v[k]));
+            h[i] = store8(static_cast<H*>(a.h) + r * a.cols + c, h[i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s = fma2(h[i].v[k], h[i].v[k], s);
         }
-        if constexpr (WARP) warp_sums(s);
-        else cta_sums(s, area, turn);
-        const float rn = 1.0f / sqrtf(s[0] / n_cols + a.eps);
+        const float rn = rstd_of(WARP ? warp_sum(s.x + s.y) : cta_sum(s.x + s.y, area, turn), n_cols, a.eps);
         if (t == 0) a.rstd_pre[r] = rn;
         if (a.x) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (t + i * T) * 8;
                 if (c >= a.cols) break;
-                float w[8];
-                params8(a.gamma_pre, c, a.bf16_params, w);
+                const Eight w = params8(a.gamma_pre, c, known.bf16());
 #pragma unroll
-                for (int k = 0; k < 8; ++k) h[i][k] = (h[i][k] * rn) * w[k];
+                for (int k = 0; k < 4; ++k) h[i].v[k] = mul2(mul2(h[i].v[k], both(rn)), w.v[k]);
                 store8(static_cast<Y*>(a.x) + r * a.cols + c, h[i]);
             }
         }
@@ -540,13 +638,14 @@ __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : 512), WARP ? 8 
 }
 
 // Backward: same ownership and the same sums as seam_grad_any_kernel; column sums stay in registers.
-template <typename Y, typename H, int NV, int STAGES>
+template <typename Y, typename H, int NV, int STAGES, int MODE>
 __global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 3 : 1) seam_grad_kernel(const SeamArgs a)
 {
     extern __shared__ __align__(16) uint8_t stage_mem[];
-    __shared__ float area[2][SEAM_MAX_WARPS][3];
+    __shared__ float4 area[2][SEAM_MAX_WARPS];
     constexpr int Q = 2 * (PIECES<Y> + PIECES<H>);          // dx, y, dh, h
     constexpr int AT_Y = PIECES<Y>, AT_DH = 2 * PIECES<Y>, AT_H = 2 * PIECES<Y> + PIECES<H>;
+    const Known<MODE, H> known{a};
     int turn = 0;
     const int T = blockDim.x, t = threadIdx.x, piece = T * 16;
     uint8_t* mine = stage_mem + t * 16;
@@ -566,132 +665,118 @@ __global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 3 : 1) seam_gra
                 if (c >= a.cols) break;
                 const uint32_t to = mine_at + (stage * NV + i) * Q * piece;
                 const int64_t at = r * a.cols + c;
-                if (a.dx) fetch(to, static_cast<const Y*>(a.dx) + at);
+                if (known.dx()) fetch(to, static_cast<const Y*>(a.dx) + at);
                 fetch(to + AT_Y * piece, static_cast<const Y*>(a.y) + at);
-                if (a.dh) fetch(to + AT_DH * piece, static_cast<const H*>(a.dh) + at);
+                if (known.dh()) fetch(to + AT_DH * piece, static_cast<const H*>(a.dh) + at);
                 fetch(to + AT_H * piece, static_cast<const H*>(static_cast<const void*>(a.h)) + at);
             }
         copies_issued();
     };
-    float pre[NV][8], post[NV][8], gates[NV][8];
+    Eight pre[NV], post[NV], gates[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int k = 0; k < 8; ++k) pre[i][k] = post[i][k] = gates[i][k] = 0.f;
+    for (int i = 0; i < NV; ++i) pre[i] = post[i] = gates[i] = zero8();
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) issue(r0 + s, s);
     int stage = 0;
     for (int64_t r = r0; r < r1; ++r) {
         issue(r + STAGES - 1, (stage + STAGES - 1) % STAGES);
-        const int64_t g = a.gate ? r / a.rows_per_gate : 0;
-        const float rn = a.rstd_pre[r], rp = a.gamma_post ? a.rstd_post[r] : 1.f;
+        const int64_t g = known.gate() ? gate_row(a, r) : 0;
+        const float rn = a.rstd_pre[r], rp = known.post() ? a.rstd_post[r] : 1.f;
         copies_done<STAGES - 1>();
         const uint8_t* at = mine + stage * NV * Q * piece;
-        auto zero = [](float (&v)[8]) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = 0.f;
-        };
-        float s[3] = {0.f, 0.f, 0.f};
+        // the sums without the factors that all their terms share
+        float2 s0 = make_float2(0.f, 0.f), s1 = s0, s2 = s0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (t + i * T) * 8;
             if (c >= a.cols) break;
             const uint8_t* from = at + i * Q * piece;
-            float xh[8], d[8], w[8];
-            load_staged<H>(from + AT_H * piece, piece, xh);
-            if (a.dx) {
-                load_staged<Y>(from, piece, d);
-                params8(a.gamma_pre, c, a.bf16_params, w);
+            const Eight h = load_staged<H>(from + AT_H * piece, piece);
+            Eight d = zero8();
+            if (known.dx()) {
+                d = load_staged<Y>(from, piece);
+                const Eight w = params8(a.gamma_pre, c, known.bf16());
 #pragma unroll
-                for (int k = 0; k < 8; ++k) d[k] *= w[k];
-            } else zero(d);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                xh[k] *= rn;
-                s[0] = fmaf(d[k], xh[k], s[0]);
+                for (int k = 0; k < 4; ++k) d.v[k] = mul2(d.v[k], w.v[k]);
             }
-            if (a.gamma_post) {
-                float q[8];
-                params8(a.gamma_post, c, a.bf16_params, w);
-                if (a.gate) {
-                    params8(a.gate, g * a.cols + c, a.bf16_params, q);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) w[k] *= q[k];
+            for (int k = 0; k < 4; ++k) s0 = fma2(d.v[k], h.v[k], s0);
+            if (known.post()) {
+                Eight w = params8(a.gamma_post, c, known.bf16());
+                if (known.gate()) {
+                    const Eight q = params8(a.gate, g * a.cols + c, known.bf16());
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) w.v[k] = mul2(w.v[k], q.v[k]);
                 }
-                load_staged<Y>(from + AT_Y * piece, piece, q);
+                const Eight y = load_staged<Y>(from + AT_Y * piece, piece), e = known.dh() ? load_staged<H>(from + AT_DH * piece, piece) : zero8();
 #pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] *= q[k];
-                if (a.dh) load_staged<H>(from + AT_DH * piece, piece, q);
-                else zero(q);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    s[1] = fmaf(w[k], fmaf(rn, d[k], q[k]), s[1]);
-                    s[2] = fmaf(w[k], xh[k], s[2]);
+                for (int k = 0; k < 4; ++k) {
+                    w.v[k] = mul2(w.v[k], y.v[k]);
+                    s1 = fma2(w.v[k], fma2(both(rn), d.v[k], e.v[k]), s1);
+                    s2 = fma2(w.v[k], h.v[k], s2);
                 }
             }
         }
+        float s[3] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y};
         cta_sums(s, area, turn);
-        const float scale = a.branch_scale * rp;                    // of the last two sums' terms
-        const float c1 = s[0] * inv_cols, c2 = (s[1] - rn * c1 * s[2]) * scale * inv_cols;
+        // G = (dh + rn t) - k1 h;  dy = k G w - k2 y
+        const float c1 = rn * s[0] * inv_cols, k1 = rn * rn * c1, k = a.branch_scale * rp, c2 = (s[1] - rn * rn * c1 * s[2]) * k * inv_cols, k2 = rp * rp * c2;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (t + i * T) * 8;
             if (c >= a.cols) break;
             const uint8_t* from = at + i * Q * piece;
             const int64_t to = r * a.cols + c;
-            float G[8], v[8], w[8];
-            load_staged<H>(from + AT_H * piece, piece, v);
-            if (a.dx) {
-                load_staged<Y>(from, piece, G);
-                params8(a.gamma_pre, c, a.bf16_params, w);
-            } else {
-                zero(G);
-                zero(w);
-            }
+            const Eight h = load_staged<H>(from + AT_H * piece, piece);
+            Eight G = known.dh() ? load_staged<H>(from + AT_DH * piece, piece) : zero8();
+            if (known.dx()) {
+                const Eight d = load_staged<Y>(from, piece), w = params8(a.gamma_pre, c, known.bf16());
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float xh = v[k] * rn;
-                pre[i][k] = fmaf(G[k], xh, pre[i][k]);
-                v[k] = fmaf(G[k], w[k], -xh * c1);
-            }
-            if (a.dh) load_staged<H>(from + AT_DH * piece, piece, G);
-            else zero(G);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                G[k] = fmaf(rn, v[k], G[k]);
-                v[k] = a.residual_scale * G[k];
-                G[k] *= a.branch_scale;
-            }
-            if (a.dh_in) store8(static_cast<H*>(a.dh_in) + to, v);
-            load_staged<Y>(from + AT_Y * piece, piece, v);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] *= rp;
-            if (a.gamma_post) params8(a.gamma_post, c, a.bf16_params, w);
-            if (a.d_gate)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) gates[i][k] = fmaf(G[k], a.gamma_post ? v[k] * w[k] : v[k], gates[i][k]);
-            if (a.gate) {
-                float q[8];
-                params8(a.gate, g * a.cols + c, a.bf16_params, q);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) G[k] *= q[k];
-            }
-            if (a.gamma_post)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    post[i][k] = fmaf(G[k], v[k], post[i][k]);
-                    G[k] = rp * fmaf(G[k], w[k], -v[k] * c2);
+                for (int k = 0; k < 4; ++k) {
+                    const float2 scaled = mul2(d.v[k], both(rn));
+                    pre[i].v[k] = fma2(scaled, h.v[k], pre[i].v[k]);
+                    G.v[k] = fma2(scaled, w.v[k], G.v[k]);
                 }
-            if (a.dy) store8(static_cast<Y*>(a.dy) + to, G);
+            }
+            Eight out;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                G.v[k] = fma2(both(-k1), h.v[k], G.v[k]);
+                out.v[k] = mul2(both(a.residual_scale), G.v[k]);
+            }
+            if (known.dh_in()) store8(static_cast<H*>(a.dh_in) + to, out);
+            const Eight y = load_staged<Y>(from + AT_Y * piece, piece);
+            const Eight w = known.post() ? params8(a.gamma_post, c, known.bf16()) : zero8();
+            if (known.d_gate())
+#pragma unroll
+                for (int k_ = 0; k_ < 4; ++k_) {
+                    const float2 n = mul2(both(k), y.v[k_]);
+                    gates[i].v[k_] = fma2(G.v[k_], known.post() ? mul2(n, w.v[k_]) : n, gates[i].v[k_]);
+                }
+            if (known.gate()) {
+                const Eight q = params8(a.gate, g * a.cols + c, known.bf16());
+#pragma unroll
+                for (int k = 0; k < 4; ++k) G.v[k] = mul2(G.v[k], q.v[k]);
+            }
+#pragma unroll
+            for (int k_ = 0; k_ < 4; ++k_) {
+                const float2 scaled = mul2(both(k), G.v[k_]);                  // without a norm after the block, dy
+                out.v[k_] = scaled;
+                if (known.post()) {
+                    post[i].v[k_] = fma2(scaled, y.v[k_], post[i].v[k_]);
+                    out.v[k_] = fma2(scaled, w.v[k_], mul2(both(-k2), y.v[k_]));
+                }
+            }
+            if (known.dy()) store8(static_cast<Y*>(a.dy) + to, out);
         }
-        if (a.d_gate && (r + 1 == r1 || (r + 1) / a.rows_per_gate != g)) {
+        if (known.d_gate() && (r + 1 == r1 || (g + 1) * a.rows_per_gate == r + 1)) {
             float* part = gate_part(a, g);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (t + i * T) * 8;
                 if (c >= a.cols) break;
                 store8(part + c, gates[i]);
-                zero(gates[i]);
+                gates[i] = zero8();
             }
         }
         stage = stage + 1 == STAGES ? 0 : stage + 1;
@@ -774,6 +859,7 @@ SeamArgs seam_args(const mxfp8_seam* s)
     // one row of the gate for all is the same as rows_per_gate = rows
     a.rows_per_gate = s->gate ? (s->rows_per_gate < s->rows ? s->rows_per_gate : s->rows) : s->rows;
     a.gates = (s->rows + a.rows_per_gate - 1) / a.rows_per_gate;
+    if (a.rows <= 0x7FFFFFFFLL) a.gate_magic = div_magic((uint32_t)a.rows_per_gate);
     a.branch_scale = s->branch_scale; a.residual_scale = s->residual_scale; a.eps = s->eps;
     return a;
 }
@@ -808,15 +894,25 @@ bool even_rows(const SeamArgs& a, std::initializer_list<const void*> block, std:
 
 constexpr int SMEM_PER_SM = 224 * 1024;
 
-template <typename Y, typename H, int NV, bool WARP, int STAGES>
+// Whether the kernels that know the usual seam fit (see Known)
+template <typename H>
+int mode_of(const SeamArgs& a, bool backward)
+{
+    if (!a.gamma_post || a.bf16_params != (sizeof(H) == 2)) return 0;
+    if (backward && (!a.dx || !a.dh || !a.dy || !a.dh_in || (a.gate != nullptr) != (a.d_gate != nullptr))) return 0;
+    return a.gate ? 2 : 1;
+}
+
+template <typename Y, typename H, int NV, bool WARP, int STAGES, int MODE = 0>
 cudaError_t launch_forward_rows(const SeamArgs& a, int threads, cudaStream_t st)
 {
-    auto kernel = seam_forward_kernel<Y, H, NV, WARP, STAGES>;
+    if (MODE == 0 && !WARP && mode_of<H>(a, false) == 1) return launch_forward_rows<Y, H, NV, WARP, STAGES, MODE == 0 && !WARP ? 1 : MODE>(a, threads, st);
+    auto kernel = seam_forward_kernel<Y, H, NV, WARP, STAGES, MODE>;
     const int smem = STAGES * NV * (PIECES<Y> + PIECES<H>) * 16 * threads;
     static unsigned long long set = 0;
     const cudaError_t err = ensure_dynamic_smem(kernel, SMEM_PER_SM, set);
     if (err != cudaSuccess) return err;
-    const int by_threads = 1024 / threads, by_smem = SMEM_PER_SM / (smem + 1024), per_sm = by_threads < by_smem ? by_threads : by_smem;
+    const int by_threads = (NV == 8 ? 512 : 1024) / threads, by_smem = SMEM_PER_SM / (smem + 1024), per_sm = by_threads < by_smem ? by_threads : by_smem;
     const int64_t groups = WARP ? (a.rows + 3) / 4 : a.rows, most = (int64_t)multiprocessors() * (per_sm < 1 ? 1 : per_sm);
     kernel<<<(unsigned)(groups < most ? groups : most), threads, smem, st>>>(a);
     count_launch(1);
@@ -844,9 +940,9 @@ cudaError_t launch_forward(const SeamArgs& a, cudaStream_t st)
     if (warps <= 4 && a.rows >= 8 * multiprocessors())
         return warps <= 2 ? launch_forward_rows<Y, H, 2, true, 3>(a, 128, st) : launch_forward_rows<Y, H, 4, true, 3>(a, 128, st);
     if (a.rows <= multiprocessors() && warps <= 32) return launch_forward_rows<Y, H, 1, false, 2>(a, 32 * warps, st);
-    if (warps <= 32) return launch_forward_rows<Y, H, 2, false, 3>(a, 32 * ((warps + 1) / 2), st);
+    if (warps <= 32) return launch_forward_rows<Y, H, 2, false, 2>(a, 32 * ((warps + 1) / 2), st);
     // 16384 columns of two FP32 inputs leave room for one row at a time
-    return launch_forward_rows<Y, H, 4, false, PIECES<Y> + PIECES<H> == 4 ? 1 : 2>(a, 32 * ((warps + 3) / 4), st);
+    return launch_forward_rows<Y, H, 8, false, PIECES<Y> + PIECES<H> == 4 ? 1 : 2>(a, 32 * ((warps + 7) / 8), st);
 }
 
 // CTAs of the backward pass per multiprocessor, by the width alone (the workspace's size follows from it): as many as registers allow.
@@ -857,10 +953,12 @@ int64_t grad_chunk(int64_t rows, int64_t cols)
     return (rows + ctas - 1) / ctas;
 }
 
-template <typename Y, typename H, int NV, int STAGES>
+template <typename Y, typename H, int NV, int STAGES, int MODE = 0>
 cudaError_t launch_grad_rows(const SeamArgs& a, int threads, unsigned ctas, cudaStream_t st)
 {
-    auto kernel = seam_grad_kernel<Y, H, NV, STAGES>;
+    if (MODE == 0 && mode_of<H>(a, true) == 1) return launch_grad_rows<Y, H, NV, STAGES, MODE == 0 ? 1 : MODE>(a, threads, ctas, st);
+    if (MODE == 0 && mode_of<H>(a, true) == 2) return launch_grad_rows<Y, H, NV, STAGES, MODE == 0 ? 2 : MODE>(a, threads, ctas, st);
+    auto kernel = seam_grad_kernel<Y, H, NV, STAGES, MODE>;
     static unsigned long long set = 0;
     const cudaError_t err = ensure_dynamic_smem(kernel, SMEM_PER_SM, set);
     if (err != cudaSuccess) return err;
