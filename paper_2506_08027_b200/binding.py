@@ -692,9 +692,9 @@ def _row_statistics(rows: int, *tensors) -> None:
             raise TypeError("row statistics are float32 [rows]")
 
 
-def _alike(what: str, like: torch.Tensor, *tensors) -> None:
+def _alike(what: str, shape, dtype, *tensors) -> None:
     for t in tensors:
-        if t is not None and (t.dtype is not like.dtype or t.shape != like.shape):
+        if t is not None and (t.dtype is not dtype or t.shape != shape):
             raise ValueError("%s have one shape and type" % what)
 
 
@@ -702,11 +702,10 @@ def mxfp8_residual_rmsnorm(seam: Seam, y: torch.Tensor, h_in: torch.Tensor, h: t
     """y, x (or None): [rows, cols] of the block's type; h_in, h: of the stream's; rstd_post (or None), rstd_pre: FP32 [rows]."""
     rows, cols = y.shape
     st = _stream_for(stream, y, h_in, h, x, rstd_post, rstd_pre, seam.gamma_pre, seam.gamma_post, seam.gate)
-    _alike("y and x", y, x)
-    _alike("h_in and h", h_in, h)
+    if x is not None:
+        _alike("y and x", y.shape, y.dtype, x)
+    _alike("y, h_in and h", y.shape, h_in.dtype, h_in, h)
     _row_statistics(rows, rstd_post, rstd_pre)
-    if h_in.shape != y.shape:
-        raise ValueError("the block's output and the stream have one shape")
     c = seam.describe(rows, cols, _dtype_code(y), _dtype_code(h_in))
     _check(lib().mxfp8_residual_rmsnorm(c, _ptr(y), _ptr(h_in), _ptr(h), _ptr(x), _ptr(rstd_post), _ptr(rstd_pre), st), "mxfp8_residual_rmsnorm")
 
@@ -716,10 +715,8 @@ def mxfp8_residual_rmsnorm_quantize(seam: Seam, y: torch.Tensor, h_in: torch.Ten
     """As mxfp8_residual_rmsnorm, with the next block's input converted: outputs as mxfp8_quantize of [rows, cols]."""
     rows, cols = y.shape
     st = _stream_for(stream, y, h_in, h, rstd_post, rstd_pre, seam.gamma_pre, seam.gamma_post, seam.gate, q_row, s_row, q_col, s_col)
-    _alike("h_in and h", h_in, h)
+    _alike("y, h_in and h", y.shape, h_in.dtype, h_in, h)
     _row_statistics(rows, rstd_post, rstd_pre)
-    if h_in.shape != y.shape:
-        raise ValueError("the block's output and the stream have one shape")
     if orientation & ROW and q_row is not None and s_row is not None:
         _holds(q_row, s_row, rows, cols, rows, cols // 32, sf_layout)
     if orientation & COL and q_col is not None and s_col is not None:
@@ -740,11 +737,9 @@ def mxfp8_residual_rmsnorm_grad(seam: Seam, dx, dh, y: torch.Tensor, h: torch.Te
     every output may be None."""
     rows, cols = y.shape
     st = _stream_for(stream, dx, dh, y, h, rstd_post, rstd_pre, dy, dh_in, d_gamma_pre, d_gamma_post, d_gate, ws, seam.gamma_pre, seam.gamma_post, seam.gate)
-    _alike("dx, y and dy", y, dx, dy)
-    _alike("dh, h and dh_in", h, dh, dh_in)
+    _alike("dx, y and dy", y.shape, y.dtype, dx, dy)
+    _alike("y, dh, h and dh_in", y.shape, h.dtype, dh, h, dh_in)
     _row_statistics(rows, rstd_post, rstd_pre)
-    if h.shape != y.shape:
-        raise ValueError("the block's output and the stream have one shape")
     for t, like in ((d_gamma_pre, seam.gamma_pre), (d_gamma_post, seam.gamma_post), (d_gate, seam.gate)):
         if t is not None and (like is None or t.dtype is not torch.float32 or t.shape != like.shape):
             raise ValueError("gradients of the seam's weights are float32 of the weights' shapes")

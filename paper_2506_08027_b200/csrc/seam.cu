@@ -80,24 +80,37 @@ __device__ __forceinline__ float cta_sum(float v, float (*area)[SEAM_MAX_WARPS],
     return __shfl_sync(0xFFFFFFFFu, v, 0);
 }
 
-// Three sums at once.  The first two steps of the tree hand half of the values to the other half of the lanes, so that the warp needs six
+// Three sums at once.  The first two steps of the tree hand half of the values to the other half of the lanes, so that a warp needs six
 // shuffles instead of fifteen; lanes 0, 8 and 16 end with the sums.
-__device__ __forceinline__ void cta_sums(float (&v)[3], float4 (*area)[SEAM_MAX_WARPS], int& turn)
+__device__ __forceinline__ float three_sums(float v0, float v1, float v2)
 {
     const int lane = threadIdx.x & 31;
     const bool high = lane & 16, odd = lane & 8;
-    float a = high ? v[2] : v[0], b = high ? 0.f : v[1];
-    a += __shfl_xor_sync(0xFFFFFFFFu, high ? v[0] : v[2], 16);
-    b += __shfl_xor_sync(0xFFFFFFFFu, high ? v[1] : 0.f, 16);
+    float a = high ? v2 : v0, b = high ? 0.f : v1;
+    a += __shfl_xor_sync(0xFFFFFFFFu, high ? v0 : v2, 16);
+    b += __shfl_xor_sync(0xFFFFFFFFu, high ? v1 : 0.f, 16);
     float s = odd ? b : a;
     s += __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 8);
 #pragma unroll
     for (int off = 4; off > 0; off >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, off);
+    return s;
+}
+__device__ __forceinline__ void cta_sums(float (&v)[3], float4 (*area)[SEAM_MAX_WARPS], int& turn)
+{
+    const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    float s = three_sums(v[0], v[1], v[2]);
     float4* here = area[turn];
     turn ^= 1;
     if ((lane & 7) == 0) reinterpret_cast<float*>(here + (threadIdx.x >> 5))[lane >> 3] = s;          // sums 0, 1, 2 and nothing
     __syncthreads();
-    const int warps = blockDim.x >> 5;
+    if (warps > 8) {
+        const float4 one = lane < warps ? here[lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+        s = three_sums(one.x, one.y, one.z);
+        v[0] = __shfl_sync(0xFFFFFFFFu, s, 0);
+        v[1] = __shfl_sync(0xFFFFFFFFu, s, 8);
+        v[2] = __shfl_sync(0xFFFFFFFFu, s, 16);
+        return;
+    }
     float4 all = here[0];
 #pragma unroll 4
     for (int w = 1; w < warps; ++w) {
@@ -640,9 +653,11 @@ __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 
     copies_done<0>();
 }
 
-// Backward: same ownership and the same sums as seam_grad_any_kernel; column sums stay in registers.
+// Backward: same ownership and the same sums as seam_grad_any_kernel; column sums stay in registers.  With one vector per thread so do the
+// parameters and, between the two passes over the row, its elements: 8192 x 4096 in BF16 takes ... us, with two vectors read twice from shared memory
+// 86 us.
 template <typename Y, typename H, int NV, int STAGES, int MODE>
-__global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 3 : 1) seam_grad_kernel(const SeamArgs a)
+__global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
 {
     extern __shared__ __align__(16) uint8_t stage_mem[];
     __shared__ float4 area[2][SEAM_MAX_WARPS];
@@ -675,16 +690,30 @@ __global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 3 : 1) seam_gra
             }
         copies_issued();
     };
+    constexpr bool KEEP = NV == 1;
     Eight pre[NV], post[NV], gates[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) pre[i] = post[i] = gates[i] = zero8();
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) issue(r0 + s, s);
+    Eight keep_pre, keep_post, keep_gate, keep_h, keep_dx, keep_dh, keep_y;
+    int64_t gate_kept = -1;
+    if (KEEP && t * 8 < a.cols) {
+        keep_pre = params8(a.gamma_pre, t * 8, known.bf16());
+        if (known.post()) keep_post = params8(a.gamma_post, t * 8, known.bf16());
+    }
+    auto gamma_pre = [&](int c) { return KEEP ? keep_pre : params8(a.gamma_pre, c, known.bf16()); };
+    auto gamma_post = [&](int c) { return KEEP ? keep_post : params8(a.gamma_post, c, known.bf16()); };
+    auto gate_at = [&](int64_t g, int c) { return KEEP ? keep_gate : params8(a.gate, g * a.cols + c, known.bf16()); };
     int stage = 0;
     for (int64_t r = r0; r < r1; ++r) {
         issue(r + STAGES - 1, (stage + STAGES - 1) % STAGES);
         const int64_t g = known.gate() ? gate_row(a, r) : 0;
         const float rn = a.rstd_pre[r], rp = known.post() ? a.rstd_post[r] : 1.f;
+        if (KEEP && known.gate() && g != gate_kept) {
+            if (t * 8 < a.cols) keep_gate = params8(a.gate, g * a.cols + t * 8, known.bf16());
+            gate_kept = g;
+        }
         copies_done<STAGES - 1>();
         const uint8_t* at = mine + stage * NV * Q * piece;
         // the sums without the factors that all their terms share
@@ -695,23 +724,27 @@ __global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 3 : 1) seam_gra
             if (c >= a.cols) break;
             const uint8_t* from = at + i * Q * piece;
             const Eight h = load_staged<H>(from + AT_H * piece, piece);
+            keep_h = h;
             Eight d = zero8();
             if (known.dx()) {
                 d = load_staged<Y>(from, piece);
-                const Eight w = params8(a.gamma_pre, c, known.bf16());
+                const Eight w = gamma_pre(c);
+                keep_dx = d;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) d.v[k] = mul2(d.v[k], w.v[k]);
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) s0 = fma2(d.v[k], h.v[k], s0);
             if (known.post()) {
-                Eight w = params8(a.gamma_post, c, known.bf16());
+                Eight w = gamma_post(c);
                 if (known.gate()) {
-                    const Eight q = params8(a.gate, g * a.cols + c, known.bf16());
+                    const Eight q = gate_at(g, c);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) w.v[k] = mul2(w.v[k], q.v[k]);
                 }
                 const Eight y = load_staged<Y>(from + AT_Y * piece, piece), e = known.dh() ? load_staged<H>(from + AT_DH * piece, piece) : zero8();
+                keep_y = y;
+                keep_dh = e;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     w.v[k] = mul2(w.v[k], y.v[k]);
@@ -722,18 +755,19 @@ __global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 3 : 1) seam_gra
         }
         float s[3] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y};
         cta_sums(s, area, turn);
-        // G = (dh + rn t) - k1 h;  dy = k G w - k2 y
-        const float c1 = rn * s[0] * inv_cols, k1 = rn * rn * c1, k = a.branch_scale * rp, c2 = (s[1] - rn * rn * c1 * s[2]) * k * inv_cols, k2 = rp * rp * c2;
+        // G = (dh + rn t) - k1 h;  dy = kb G w - k2 y
+        const float c1 = rn * s[0] * inv_cols, k1 = rn * rn * c1, kb = a.branch_scale * rp, c2 = (s[1] - rn * rn * c1 * s[2]) * kb * inv_cols, k2 = rp * rp * c2;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (t + i * T) * 8;
             if (c >= a.cols) break;
             const uint8_t* from = at + i * Q * piece;
             const int64_t to = r * a.cols + c;
-            const Eight h = load_staged<H>(from + AT_H * piece, piece);
-            Eight G = known.dh() ? load_staged<H>(from + AT_DH * piece, piece) : zero8();
+            const bool kept = KEEP && known.post();          // dh and y are looked at in the first pass then
+            const Eight h = KEEP ? keep_h : load_staged<H>(from + AT_H * piece, piece);
+            Eight G = kept ? keep_dh : (known.dh() ? load_staged<H>(from + AT_DH * piece, piece) : zero8());
             if (known.dx()) {
-                const Eight d = load_staged<Y>(from, piece), w = params8(a.gamma_pre, c, known.bf16());
+                const Eight d = KEEP ? keep_dx : load_staged<Y>(from, piece), w = gamma_pre(c);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const float2 scaled = mul2(d.v[k], both(rn));
@@ -748,26 +782,26 @@ __global__ void __launch_bounds__(NV == 1 ? 256 : 512, NV == 1 ? 3 : 1) seam_gra
                 out.v[k] = mul2(both(a.residual_scale), G.v[k]);
             }
             if (known.dh_in()) store8(static_cast<H*>(a.dh_in) + to, out);
-            const Eight y = load_staged<Y>(from + AT_Y * piece, piece);
-            const Eight w = known.post() ? params8(a.gamma_post, c, known.bf16()) : zero8();
+            const Eight y = kept ? keep_y : load_staged<Y>(from + AT_Y * piece, piece);
+            const Eight w = known.post() ? gamma_post(c) : zero8();
             if (known.d_gate())
 #pragma unroll
-                for (int k_ = 0; k_ < 4; ++k_) {
-                    const float2 n = mul2(both(k), y.v[k_]);
-                    gates[i].v[k_] = fma2(G.v[k_], known.post() ? mul2(n, w.v[k_]) : n, gates[i].v[k_]);
+                for (int k = 0; k < 4; ++k) {
+                    const float2 n = mul2(both(kb), y.v[k]);
+                    gates[i].v[k] = fma2(G.v[k], known.post() ? mul2(n, w.v[k]) : n, gates[i].v[k]);
                 }
             if (known.gate()) {
-                const Eight q = params8(a.gate, g * a.cols + c, known.bf16());
+                const Eight q = gate_at(g, c);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) G.v[k] = mul2(G.v[k], q.v[k]);
             }
 #pragma unroll
-            for (int k_ = 0; k_ < 4; ++k_) {
-                const float2 scaled = mul2(both(k), G.v[k_]);                  // without a norm after the block, dy
-                out.v[k_] = scaled;
+            for (int k = 0; k < 4; ++k) {
+                const float2 scaled = mul2(both(kb), G.v[k]);                  // without a norm after the block, dy
+                out.v[k] = scaled;
                 if (known.post()) {
-                    post[i].v[k_] = fma2(scaled, y.v[k_], post[i].v[k_]);
-                    out.v[k_] = fma2(scaled, w.v[k_], mul2(both(-k2), y.v[k_]));
+                    post[i].v[k] = fma2(scaled, y.v[k], post[i].v[k]);
+                    out.v[k] = fma2(scaled, w.v[k], mul2(both(-k2), y.v[k]));
                 }
             }
             if (known.dy()) store8(static_cast<Y*>(a.dy) + to, out);
@@ -949,7 +983,8 @@ cudaError_t launch_forward(const SeamArgs& a, cudaStream_t st)
 }
 
 // CTAs of the backward pass per multiprocessor, by the width alone (the workspace's size follows from it): as many as registers allow.
-int grad_ctas_per_sm(int64_t cols) { return cols > 4096 ? 1 : (cols > 2048 ? 2 : (cols > 1024 ? 3 : (cols > 512 ? 5 : 8))); }
+// (16 warps of 128 registers)
+int grad_ctas_per_sm(int64_t cols) { return cols > 2048 ? 1 : (cols > 1024 ? 2 : (cols > 512 ? 4 : 8)); }
 int64_t grad_chunk(int64_t rows, int64_t cols)
 {
     const int64_t ctas = (int64_t)grad_ctas_per_sm(cols) * multiprocessors();
@@ -978,8 +1013,7 @@ cudaError_t launch_grad(SeamArgs a, cudaStream_t st)
     if (rows_aligned(a, a.dx, a.dh, a.y, a.h, a.dy, a.dh_in, a.d_gate) && a.cols * 2 * (int)(sizeof(Y) + sizeof(H)) <= SMEM_PER_SM) {
         constexpr int Q = PIECES<Y> + PIECES<H>;
         const int warps = (a.cols / 8 + 31) / 32;
-        if (warps <= 8) rc = launch_grad_rows<Y, H, 1, Q == 4 ? 2 : 3>(a, 32 * warps, ctas, st);
-        else if (warps <= 16) rc = launch_grad_rows<Y, H, 2, Q == 2 ? 3 : (Q == 3 ? 2 : 1)>(a, 32 * ((warps + 1) / 2), ctas, st);
+        if (warps <= 16) rc = launch_grad_rows<Y, H, 1, Q == 2 ? 4 : (Q == 3 ? 4 : 3)>(a, 32 * warps, ctas, st);
         else if (warps <= 32) rc = launch_grad_rows<Y, H, 2, Q == 2 ? 3 : (Q == 3 ? 2 : 1)>(a, 32 * ((warps + 1) / 2), ctas, st);
         else rc = launch_grad_rows<Y, H, 4, 1>(a, 32 * ((warps + 3) / 4), ctas, st);
     } else if (a.cols <= 8192) {
