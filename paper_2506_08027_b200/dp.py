@@ -193,3 +193,43 @@ class DataParallelLinear:
                                     B.E4M3, B.E4M3, self.owners, p.first_owner())
         self._everyone_arrived()
         return self.y, self.dx, self.dw_shard
+
+
+class GradientClipping:
+    """The norm of a step's gradients over all ranks, and clipping by it: what follows the WGRAD products of a step.
+
+    `owned` are this rank's parts of sharded gradients (DataParallelLinear's dw_shard, say): every element lies on one rank.  `replicated` are
+    gradients that all ranks hold alike (norm weights, gates); they count once, and every rank scales its copy.  FP32 or BF16, dense, on the
+    current device.  Built once; clip() may be called every step while the tensors live.
+
+    clip(max_norm) scales in place and returns [norm, factor] (FP32, this object's, valid in stream order until the next call).  Ranks exchange one
+    FP64 number; a single rank launches the two kernels of mxfp8_grad_clip.  Every rank calls clip() the same number of times.
+    """
+
+    def __init__(self, owned, replicated=(), group=None):
+        self.group = group
+        self.world = dist.get_world_size(group) if dist.is_initialized() else 1
+        rank = dist.get_rank(group) if dist.is_initialized() else 0
+        owned, replicated = list(owned), list(replicated)
+        self.on_stream = not dist.is_initialized() or dist.get_backend(group) == "nccl"
+        self._all = B.make_grad_items(owned + replicated)
+        self._counted = self._all if rank == 0 else B.make_grad_items(owned)
+        like = (owned + replicated)[0] if owned or replicated else None
+        device = torch.device("cuda", torch.cuda.current_device()) if like is None else like.device
+        self._ws = torch.empty(max(8, B.mxfp8_grad_ws_bytes(self._all)), dtype=torch.uint8, device=device)
+        self._sumsq = torch.zeros(1, dtype=torch.float64, device=device)
+        self.norm = torch.zeros(2, dtype=torch.float32, device=device)
+
+    def clip(self, max_norm: float) -> torch.Tensor:
+        if self.world == 1:
+            B.mxfp8_grad_clip(self._all, max_norm, self.norm, self._ws)
+            return self.norm
+        B.mxfp8_grad_sumsq(self._counted, self._sumsq, self._ws)
+        if self.on_stream:
+            dist.all_reduce(self._sumsq, group=self.group)
+        else:                                    # through the host, as the other exchanges
+            total = self._sumsq.cpu()
+            dist.all_reduce(total, group=self.group)
+            self._sumsq.copy_(total)
+        B.mxfp8_grad_scale(self._all, self._sumsq, max_norm, self.norm)
+        return self.norm
