@@ -550,9 +550,9 @@ def run_case(args):
         for _ in range(reps):
             B.mxfp8_gemm_reduce_scatter(qdy[2], qdy[3], qx[2], qx[3], F, H, T, B.MN_MAJOR, B.MN_MAJOR, E, E, ptrs, 3)
     elif args.case == "operator":
-        # one listed case of perf/operators.py
-        ops = operator_cases()
-        state = ops.prepare(next(c for c in ops.listed() if c["name"] == args.operator), 5)
+        # one listed case of perf/operators.py or perf/more_operators.py
+        ops, case = next((m, c) for m in (operator_cases(), operator_cases("more_operators")) for c in m.listed() if c["name"] == args.operator)
+        state = ops.prepare(case, 5)
         for _ in range(reps):
             ops.run(state)
     elif args.case == "glu":
@@ -588,10 +588,11 @@ def run_case(args):
     print(json.dumps({"case": args.case, "launches": int(B.mxfp8_launch_count()), "device_status": B.mxfp8_device_status()}))
 
 
-def operator_cases():
-    """perf/operators.py (cases, inputs and plain forms of the mixture-of-experts calls and the 4-bit products), set to call the library."""
+def operator_cases(name="operators"):
+    """perf/operators.py (cases, inputs and plain forms of the mixture-of-experts calls and the 4-bit products) or perf/more_operators.py (the
+    block seam, gradient clipping, the few-token mixture-of-experts layer), set to call the library."""
     import importlib.util
-    spec = importlib.util.spec_from_file_location("operators", os.path.join(ROOT, "perf", "operators.py"))
+    spec = importlib.util.spec_from_file_location(name, os.path.join(ROOT, "perf", name + ".py"))
     ops = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(ops)
     ops.own = True
@@ -938,7 +939,7 @@ def run_sweep(args):
 
 
 def run_operator_sweep(peaks):
-    """The calls around the grouped products and the 4-bit products: the listed cases of perf/operators.py, the gathered conversion by
+    """The calls around the grouped products and the 4-bit products: the listed cases of perf/operators.py and perf/more_operators.py, the gathered conversion by
     orientation, the calls with and without what reads their results, and 4-bit products by number of tokens beside
     mxfp8_gemm.  Device times of captured graphs, inputs taken in turn."""
     import torch
@@ -953,13 +954,14 @@ def run_operator_sweep(peaks):
 
     print("| case | us | floor us | of the floor's rate |")
     print("|---|---|---|---|")
-    for case in ops.listed():
-        states = [ops.prepare(case, 5 + i) for i in range(3)]
-        nbytes = ops.work(case)["bytes"]
+    more = operator_cases("more_operators")
+    for mod, case in [(ops, c) for c in ops.listed()] + [(more, c) for c in more.listed()]:
+        states = [mod.prepare(case, 5 + i) for i in range(3)]
+        nbytes = mod.work(case)["bytes"]
         if case["op"] == "matvec" and case["chosen"]:            # the matrices that are chosen, not as many as could be
             used = sum(len(s["ids"].unique()) for s in states) / 3
             nbytes = used * case["rows"] * case["cols"] * 17 / 32 + 2 * case["tokens"] * case["cols"] + 4 * case["tokens"] * case["top_k"] * case["rows"]
-        t, floor = us(lambda i: ops.run(states[i]), 3), nbytes / peaks["hbm_gbs"] / 1e3
+        t, floor = us(lambda i: mod.run(states[i]), 3), nbytes / peaks["hbm_gbs"] / 1e3
         print("| %s | %.1f | %.2f | %.0f %% |" % (case["name"], t, floor, 100 * floor / t), flush=True)
         del states
     g = torch.Generator(device="cuda").manual_seed(7)
@@ -1051,7 +1053,7 @@ def main():
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--case", default=None, choices=["quantize", "dequantize", "fake_quantize", "gemm", "gemm8k", "gemm_fused", "step", "grouped", "grouped_wgrad", "glu", "scatter", "operator"],
                     help="run one kernel on one small case and exit (for profiler captures)")
-    ap.add_argument("--operator", default="dispatch layer", help="the listed case of perf/operators.py that --case operator runs")
+    ap.add_argument("--operator", default="dispatch layer", help="the listed case of perf/operators.py or perf/more_operators.py that --case operator runs")
     ap.add_argument("--sweep", default=None, choices=["cast", "gemm", "emu", "moe", "dp", "rules", "operators"],
                     help="print the cast-bandwidth, GEMM-shape or round-trip (emu) sweep as a markdown table and exit")
     args = ap.parse_args()
