@@ -7,6 +7,7 @@
 #include <cuda_bf16.h>
 
 #include <initializer_list>
+#include <type_traits>
 
 #include "mxfp8_device.cuh"
 #include "mxfp8_host.h"
@@ -182,13 +183,15 @@ __device__ __forceinline__ void params_few(const void* p, int64_t at, bool bf16,
     else load_few<float, V>(static_cast<const float*>(p) + at, v);
 }
 
-template <typename Y, typename H, int V, int NE>
-__global__ void __launch_bounds__(NE == 8 ? 256 : 1024, NE == 8 ? 6 : 1) seam_forward_any_kernel(const SeamArgs a)
+// T threads; SAME: the parameters have the stream's type.
+template <typename Y, typename H, int V, int NE, int T, bool SAME>
+__global__ void __launch_bounds__(T, NE == 16 ? 1024 / T : (T == 32 ? 24 : 1536 / T)) seam_forward_any_kernel(const SeamArgs a)
 {
     __shared__ float area[2][SEAM_MAX_WARPS];
     constexpr int NV = NE / V;
     int turn = 0;
-    const int T = blockDim.x, t = threadIdx.x;
+    const int t = threadIdx.x;
+    const bool bf16 = SAME ? sizeof(H) == 2 : a.bf16_params;
     const float n_cols = (float)a.cols;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const int64_t row = r * a.cols, gate = a.gate ? gate_row(a, r) * a.cols : 0;
@@ -218,12 +221,12 @@ __global__ void __launch_bounds__(NE == 8 ? 256 : 1024, NE == 8 ? 6 : 1) seam_fo
             if (c >= a.cols) break;
             float w[V];
             if (a.gamma_post) {
-                params_few<V>(a.gamma_post, c, a.bf16_params, w);
+                params_few<V>(a.gamma_post, c, bf16, w);
 #pragma unroll
                 for (int k = 0; k < V; ++k) n[i][k] = (n[i][k] * rp) * w[k];
             }
             if (a.gate) {
-                params_few<V>(a.gate, gate + c, a.bf16_params, w);
+                params_few<V>(a.gate, gate + c, bf16, w);
 #pragma unroll
                 for (int k = 0; k < V; ++k) n[i][k] *= w[k];
             }
@@ -241,7 +244,7 @@ __global__ void __launch_bounds__(NE == 8 ? 256 : 1024, NE == 8 ? 6 : 1) seam_fo
                 const int c = (t + i * T) * V;
                 if (c >= a.cols) break;
                 float w[V];
-                params_few<V>(a.gamma_pre, c, a.bf16_params, w);
+                params_few<V>(a.gamma_pre, c, bf16, w);
 #pragma unroll
                 for (int k = 0; k < V; ++k) w[k] = (h[i][k] * rn) * w[k];
                 store_few<Y, V>(static_cast<Y*>(a.x) + row + c, w);
@@ -269,13 +272,14 @@ __device__ __forceinline__ float* weights_part(const SeamArgs& a, bool post)
     return a.ws + ((int64_t)blockIdx.x + (post && a.d_gamma_pre ? gridDim.x : 0)) * a.cols;
 }
 
-template <typename Y, typename H, int V, int NE>
-__global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(const SeamArgs a)
+template <typename Y, typename H, int V, int NE, int T, bool SAME>
+__global__ void __launch_bounds__(T, (NE == 4 ? 1024 : 512) / T) seam_grad_few_kernel(const SeamArgs a)
 {
     __shared__ float4 area[2][SEAM_MAX_WARPS];
     constexpr int NV = NE / V;
     int turn = 0;
-    const int T = blockDim.x, t = threadIdx.x;
+    const int t = threadIdx.x;
+    const bool bf16 = SAME ? sizeof(H) == 2 : a.bf16_params;
     const int64_t r0 = blockIdx.x * a.chunk, r1 = min(r0 + a.chunk, a.rows);
     const float inv_cols = 1.0f / (float)a.cols;
     float pre[NV][V], post[NV][V], gates[NV][V];
@@ -283,9 +287,14 @@ __global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(con
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int k = 0; k < V; ++k) pre[i][k] = post[i][k] = gates[i][k] = 0.f;
+    float rn_next = a.rstd_pre[r0], rp_next = a.gamma_post ? a.rstd_post[r0] : 1.f;             // a row ahead
     for (int64_t r = r0; r < r1; ++r) {
         const int64_t row = r * a.cols, g = a.gate ? gate_row(a, r) : 0;
-        const float rn = a.rstd_pre[r], rp = a.gamma_post ? a.rstd_post[r] : 1.f;
+        const float rn = rn_next, rp = rp_next;
+        if (r + 1 < r1) {
+            rn_next = a.rstd_pre[r + 1];
+            if (a.gamma_post) rp_next = a.rstd_post[r + 1];
+        }
         float dx[NV][V], dh[NV][V], y[NV][V], h[NV][V], s[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -304,7 +313,7 @@ __global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(con
             const int c = (t + i * T) * V;
             if (c >= a.cols) break;
             float w[V], q[V];
-            params_few<V>(a.gamma_pre, c, a.bf16_params, w);
+            params_few<V>(a.gamma_pre, c, bf16, w);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 h[i][k] *= rn;
@@ -314,9 +323,9 @@ __global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(con
             }
             if (a.gamma_post) {
                 float u[V];
-                params_few<V>(a.gamma_post, c, a.bf16_params, u);
+                params_few<V>(a.gamma_post, c, bf16, u);
                 if (a.gate) {
-                    params_few<V>(a.gate, g * a.cols + c, a.bf16_params, q);
+                    params_few<V>(a.gate, g * a.cols + c, bf16, q);
 #pragma unroll
                     for (int k = 0; k < V; ++k) u[k] *= q[k];
                 }
@@ -335,7 +344,7 @@ __global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(con
             const int c = (t + i * T) * V;
             if (c >= a.cols) break;
             float w[V], G[V];
-            params_few<V>(a.gamma_pre, c, a.bf16_params, w);
+            params_few<V>(a.gamma_pre, c, bf16, w);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 pre[i][k] = fmaf(dx[i][k], h[i][k], pre[i][k]);
@@ -346,13 +355,13 @@ __global__ void __launch_bounds__(512, NE == 4 ? 2 : 1) seam_grad_few_kernel(con
             if (a.dh_in) store_few<H, V>(static_cast<H*>(a.dh_in) + row + c, w);
 #pragma unroll
             for (int k = 0; k < V; ++k) w[k] = 1.f;
-            if (a.gamma_post) params_few<V>(a.gamma_post, c, a.bf16_params, w);
+            if (a.gamma_post) params_few<V>(a.gamma_post, c, bf16, w);
             if (a.d_gate)
 #pragma unroll
                 for (int k = 0; k < V; ++k) gates[i][k] = fmaf(G[k], y[i][k] * w[k], gates[i][k]);
             if (a.gate) {
                 float q[V];
-                params_few<V>(a.gate, g * a.cols + c, a.bf16_params, q);
+                params_few<V>(a.gate, g * a.cols + c, bf16, q);
 #pragma unroll
                 for (int k = 0; k < V; ++k) G[k] *= q[k];
             }
@@ -706,10 +715,15 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
     auto gamma_post = [&](int c) { return KEEP ? keep_post : params8(a.gamma_post, c, known.bf16()); };
     auto gate_at = [&](int64_t g, int c) { return KEEP ? keep_gate : params8(a.gate, g * a.cols + c, known.bf16()); };
     int stage = 0;
+    float rn_next = a.rstd_pre[r0], rp_next = known.post() ? a.rstd_post[r0] : 1.f;             // a row ahead
     for (int64_t r = r0; r < r1; ++r) {
         issue(r + STAGES - 1, (stage + STAGES - 1) % STAGES);
         const int64_t g = known.gate() ? gate_row(a, r) : 0;
-        const float rn = a.rstd_pre[r], rp = known.post() ? a.rstd_post[r] : 1.f;
+        const float rn = rn_next, rp = rp_next;
+        if (r + 1 < r1) {
+            rn_next = a.rstd_pre[r + 1];
+            if (known.post()) rp_next = a.rstd_post[r + 1];
+        }
         if (KEEP && known.gate() && g != gate_kept) {
             if (t * 8 < a.cols) keep_gate = params8(a.gate, g * a.cols + t * 8, known.bf16());
             gate_kept = g;
@@ -960,15 +974,23 @@ template <typename Y, typename H>
 cudaError_t launch_forward(const SeamArgs& a, cudaStream_t st)
 {
     if (!rows_aligned(a, a.y, a.h_in, a.h, a.x)) {
-        const int few = a.cols <= 2048 ? 8 : 16, threads = (a.cols + 32 * few - 1) / (32 * few) * 32;
-        const int per_sm = 1536 / threads < 16 ? 1536 / threads : 16;
-        const int64_t most = (int64_t)multiprocessors() * (per_sm < 1 ? 1 : per_sm);
-        const unsigned ctas = (unsigned)(a.rows < most ? a.rows : most);
-        const bool two = even_rows<Y, H>(a, {a.y, a.x}, {a.h_in, a.h});
-        if (few == 8 && two) seam_forward_any_kernel<Y, H, 2, 8><<<ctas, threads, 0, st>>>(a);
-        else if (few == 8) seam_forward_any_kernel<Y, H, 1, 8><<<ctas, threads, 0, st>>>(a);
-        else if (two) seam_forward_any_kernel<Y, H, 2, 16><<<ctas, threads, 0, st>>>(a);
-        else seam_forward_any_kernel<Y, H, 1, 16><<<ctas, threads, 0, st>>>(a);
+        const bool two = even_rows<Y, H>(a, {a.y, a.x}, {a.h_in, a.h}), same = a.bf16_params == (sizeof(H) == 2);
+        auto go = [&](auto kernel, int threads) {
+            const int64_t most = (int64_t)multiprocessors() * (1536 / threads < 24 ? 1536 / threads : 24);
+            kernel<<<(unsigned)(a.rows < most ? a.rows : most), threads, 0, st>>>(a);
+        };
+        auto by_width = [&](auto v, auto s) {
+            constexpr int V = decltype(v)::value;
+            constexpr bool SAME = decltype(s)::value;
+            if (a.cols <= 256) go(seam_forward_any_kernel<Y, H, V, 8, 32, SAME>, 32);
+            else if (a.cols <= 2048) go(seam_forward_any_kernel<Y, H, V, 8, 256, SAME>, 256);
+            else if (a.cols <= 8192) go(seam_forward_any_kernel<Y, H, V, 16, 512, SAME>, 512);
+            else go(seam_forward_any_kernel<Y, H, V, 16, 1024, SAME>, 1024);
+        };
+        using one_t = std::integral_constant<int, 1>;
+        using two_t = std::integral_constant<int, 2>;
+        if (two) same ? by_width(two_t{}, std::true_type{}) : by_width(two_t{}, std::false_type{});
+        else same ? by_width(one_t{}, std::true_type{}) : by_width(one_t{}, std::false_type{});
         count_launch(1);
         return cudaGetLastError();
     }
@@ -1017,16 +1039,20 @@ cudaError_t launch_grad(SeamArgs a, cudaStream_t st)
         else if (warps <= 32) rc = launch_grad_rows<Y, H, 2, Q == 2 ? 3 : (Q == 3 ? 2 : 1)>(a, 32 * ((warps + 1) / 2), ctas, st);
         else rc = launch_grad_rows<Y, H, 4, 1>(a, 32 * ((warps + 3) / 4), ctas, st);
     } else if (a.cols <= 8192) {
-        const int few = a.cols <= 2048 ? 4 : 8, threads = (a.cols + 32 * few - 1) / (32 * few) * 32;
-        const bool two = even_rows<Y, H>(a, {a.dx, a.y, a.dy}, {a.dh, a.h, a.dh_in});
-        if (threads > 512) {
-            if (two) seam_grad_few_kernel<Y, H, 2, 16><<<ctas, (a.cols + 511) / 512 * 32, 0, st>>>(a);
-            else seam_grad_few_kernel<Y, H, 1, 16><<<ctas, (a.cols + 511) / 512 * 32, 0, st>>>(a);
-        } else if (few == 4) {
-            if (two) seam_grad_few_kernel<Y, H, 2, 4><<<ctas, threads, 0, st>>>(a);
-            else seam_grad_few_kernel<Y, H, 1, 4><<<ctas, threads, 0, st>>>(a);
-        } else if (two) seam_grad_few_kernel<Y, H, 2, 8><<<ctas, threads, 0, st>>>(a);
-        else seam_grad_few_kernel<Y, H, 1, 8><<<ctas, threads, 0, st>>>(a);
+        const bool two = even_rows<Y, H>(a, {a.dx, a.y, a.dy}, {a.dh, a.h, a.dh_in}), same = a.bf16_params == (sizeof(H) == 2);
+        auto by_width = [&](auto v, auto s) {
+            constexpr int V = decltype(v)::value;
+            constexpr bool SAME = decltype(s)::value;
+            if (a.cols <= 256) seam_grad_few_kernel<Y, H, V, 4, 64, SAME><<<ctas, 64, 0, st>>>(a);
+            else if (a.cols <= 1024) seam_grad_few_kernel<Y, H, V, 4, 256, SAME><<<ctas, 256, 0, st>>>(a);
+            else if (a.cols <= 2048) seam_grad_few_kernel<Y, H, V, 4, 512, SAME><<<ctas, 512, 0, st>>>(a);
+            else if (a.cols <= 4096) seam_grad_few_kernel<Y, H, V, 8, 512, SAME><<<ctas, 512, 0, st>>>(a);
+            else seam_grad_few_kernel<Y, H, V, 16, 512, SAME><<<ctas, 512, 0, st>>>(a);
+        };
+        using one_t = std::integral_constant<int, 1>;
+        using two_t = std::integral_constant<int, 2>;
+        if (two) same ? by_width(two_t{}, std::true_type{}) : by_width(two_t{}, std::false_type{});
+        else same ? by_width(one_t{}, std::true_type{}) : by_width(one_t{}, std::false_type{});
         rc = cudaGetLastError();
     } else {
         auto kernel = seam_grad_any_kernel<Y, H>;
