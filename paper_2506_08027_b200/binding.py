@@ -491,6 +491,22 @@ def mxfp8_glu_quantize(src: torch.Tensor, act: int, orientation: int, scale_rule
                                     _stream(stream)), "mxfp8_glu_quantize")
 
 
+def _addresses(*tensors):
+    """Addresses of a call's tensors (None for one that is left out), looked at once: they are dense and lie on the current device."""
+    device = _current_device()
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+        elif t.get_device() != device:                           # -1 for a host tensor
+            raise ValueError("a tensor of shape %s is on %s, the call runs on cuda:%d" % (tuple(t.shape), t.device, device))
+        elif not t.is_contiguous():
+            raise ValueError("the C entry points take dense row-major buffers: pass a contiguous tensor")
+        else:
+            out.append(t.data_ptr())
+    return out
+
+
 def _stream_for(stream, *tensors) -> int:
     """The call's stream, after a look at its tensors: all of them lie on the device that the stream belongs to and that
     is current (a launch elsewhere would read foreign addresses)."""
@@ -634,7 +650,7 @@ def mxfp8_e2m1_moe_ws_bytes(tokens: int, top_k: int, inner: int) -> int:
 
 
 def _nbytes(t) -> int:
-    return 0 if t is None else t.numel() * t.element_size()
+    return 0 if t is None else t.nbytes
 
 
 def mxfp8_e2m1_moe(x: torch.Tensor, logits: torch.Tensor, top_k: int, gate_up: torch.Tensor, down: torch.Tensor, inner: int, act: int, renormalize: bool,
@@ -646,14 +662,16 @@ def mxfp8_e2m1_moe(x: torch.Tensor, logits: torch.Tensor, top_k: int, gate_up: t
     if x.dtype is not torch.bfloat16 or logits.dtype is not torch.float32:
         raise TypeError("x must be bfloat16 and logits float32")
     _int32(ids)
-    st = _stream_for(stream, x, logits, gate_up, down, y, ids, weights, ws)
+    st = _stream_for(stream)
+    x_at, logits_at, gate_up_at, down_at, y_at, ids_at, weights_at, ws_at = _addresses(x, logits, gate_up, down, y, ids, weights, ws)
     _float_weights(weights, tokens, top_k)
     if logits.shape[0] != tokens or y.shape != x.shape or (ids is not None and ids.shape != (tokens, top_k)):
         raise ValueError("logits, y and ids hold one row per token")
-    if _nbytes(gate_up) < mxfp8_e2m1_packed_bytes(experts, 2 * inner, cols) or _nbytes(down) < mxfp8_e2m1_packed_bytes(experts, cols, inner):
+    # tiles of 16 rows x 128 columns, 1088 bytes each (mxfp8_e2m1_packed_bytes)
+    if _nbytes(gate_up) < experts * (-(-2 * inner // 16)) * (-(-cols // 128)) * 1088 or _nbytes(down) < experts * (-(-cols // 16)) * (-(-inner // 128)) * 1088:
         raise ValueError("gate_up or down is smaller than %d matrices of [%d, %d] and [%d, %d]" % (experts, 2 * inner, cols, cols, inner))
-    _check(lib().mxfp8_e2m1_moe(_ptr(x), _ptr(logits), tokens, cols, experts, top_k, _ptr(gate_up), _ptr(down), inner, act, int(renormalize), _ptr(y),
-                                _dtype_code(y), _ptr(ids), _ptr(weights), _ptr(ws), _nbytes(ws), st), "mxfp8_e2m1_moe")
+    _check(lib().mxfp8_e2m1_moe(x_at, logits_at, tokens, cols, experts, top_k, gate_up_at, down_at, inner, act, renormalize, y_at,
+                                _dtype_code(y), ids_at, weights_at, ws_at, _nbytes(ws), st), "mxfp8_e2m1_moe")
 
 
 class Seam:
@@ -700,14 +718,15 @@ def _alike(what: str, shape, dtype, *tensors) -> None:
 
 def mxfp8_residual_rmsnorm(seam: Seam, y: torch.Tensor, h_in: torch.Tensor, h: torch.Tensor, x, rstd_post, rstd_pre: torch.Tensor, stream=None) -> None:
     """y, x (or None): [rows, cols] of the block's type; h_in, h: of the stream's; rstd_post (or None), rstd_pre: FP32 [rows]."""
-    rows, cols = y.shape
-    st = _stream_for(stream, y, h_in, h, x, rstd_post, rstd_pre, seam.gamma_pre, seam.gamma_post, seam.gate)
+    rows, cols = shape = y.shape
+    st = _stream_for(stream, seam.gamma_pre, seam.gamma_post, seam.gate)
+    at = _addresses(y, h_in, h, x, rstd_post, rstd_pre)
     if x is not None:
-        _alike("y and x", y.shape, y.dtype, x)
-    _alike("y, h_in and h", y.shape, h_in.dtype, h_in, h)
+        _alike("y and x", shape, y.dtype, x)
+    _alike("y, h_in and h", shape, h_in.dtype, h_in, h)
     _row_statistics(rows, rstd_post, rstd_pre)
     c = seam.describe(rows, cols, _dtype_code(y), _dtype_code(h_in))
-    _check(lib().mxfp8_residual_rmsnorm(c, _ptr(y), _ptr(h_in), _ptr(h), _ptr(x), _ptr(rstd_post), _ptr(rstd_pre), st), "mxfp8_residual_rmsnorm")
+    _check(lib().mxfp8_residual_rmsnorm(c, *at, st), "mxfp8_residual_rmsnorm")
 
 
 def mxfp8_residual_rmsnorm_quantize(seam: Seam, y: torch.Tensor, h_in: torch.Tensor, h: torch.Tensor, rstd_post, rstd_pre: torch.Tensor,

@@ -114,6 +114,7 @@ def test_few_token_layer():
 @pytest.fixture
 def no_device(monkeypatch):
     monkeypatch.setattr(B, "_stream_for", lambda stream, *tensors: 5)
+    monkeypatch.setattr(B, "_current_device", lambda: -1)                 # what a host tensor says of itself
 
     class Nothing:
         def __getattr__(self, name):
