@@ -57,7 +57,8 @@ __device__ __forceinline__ float share_of(uint32_t o, uint32_t top) { return o =
 
 // Chooses for all tokens and makes the entries.  `keys`: shared memory for tokens * experts numbers.  An expert's place is the number of experts before
 // it: larger logits, and equal ones of a lower number.  That is tokens * experts^2 comparisons, all threads side by side; where they are many,
-// a warp per token takes the largest top_k times instead (16 tokens of 64 experts: ... ).  Ends with a barrier.
+// a warp per token takes the largest top_k times instead (one token of 64 experts: 4.4 thousand cycles for everything here, 7.0 the other way;
+// 16 tokens: 8.4 and 6.3).  Ends with a barrier.
 constexpr int MOE_COMPARISONS = 128 * 128;
 __device__ __forceinline__ void choose(const MoeArgs& a, Choice& choice, uint32_t* keys, int most)
 {

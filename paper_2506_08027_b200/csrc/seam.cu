@@ -36,6 +36,8 @@ struct SeamArgs {
     int64_t chunk;                               // rows of a CTA
     int64_t gates;
     uint32_t gate_magic;                         // of rows_per_gate, where rows fit 31 bits
+    uint8_t *q_row, *s_row;                      // forward: x converted with row blocks instead of stored
+    int elem, rule, layout;
 };
 
 __device__ __forceinline__ float to_float(float v) { return v; }
@@ -564,9 +566,73 @@ __device__ __forceinline__ Eight params8(const void* p, int64_t at, bool bf16)
     return unpack<float>(w);
 }
 
-// Forward.  WARP: rows of a warp each (the CTA has four), else of the CTA.  Rows go last to first: what reads h or x next begins with the first
-// rows, and finds them in L2 (the conversion behind the seam of 8192 x 4096 in BF16: 79 us for both that way, ... us the other way).
-template <typename Y, typename H, int NV, bool WARP, int STAGES, int MODE>
+// Largest magnitude of the finite elements as a bit pattern.  The maximum passes over NaN by itself; an infinity is looked at again.
+__device__ __forceinline__ uint32_t finite_peak(const Eight& e)
+{
+    float peak = fmaxf(fabsf(e.v[0].x), fabsf(e.v[0].y));
+#pragma unroll
+    for (int k = 1; k < 4; ++k) peak = fmaxf(fmaxf(peak, fabsf(e.v[k].x)), fabsf(e.v[k].y));
+    uint32_t bits = __float_as_uint(peak);
+    if (bits >= 0x7F800000u) {                       // an infinity, or nothing but NaN
+        bits = 0u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t a = __float_as_uint(e.v[k].x) & 0x7FFFFFFFu, b = __float_as_uint(e.v[k].y) & 0x7FFFFFFFu;
+            bits = max(bits, max(a < 0x7F800000u ? a : 0u, b < 0x7F800000u ? b : 0u));
+        }
+    }
+    return bits;
+}
+// Scale byte of a block with this peak, and the eight codes under it
+template <int ELEM>
+__device__ __forceinline__ uint2 codes8(const Eight& x, uint32_t peak, int rule, uint32_t& byte)
+{
+    byte = scale_byte_from_amax_bits<ELEM>(peak, rule);
+    const float2 inverse = both(inv_scale_from_byte(byte));
+    float2 v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = mul2(x.v[k], inverse);
+    return make_uint2(cvt_fp8x4<ELEM>(v[0].x, v[0].y, v[1].x, v[1].y), cvt_fp8x4<ELEM>(v[2].x, v[2].y, v[3].x, v[3].y));
+}
+
+// x of eight columns (c .. c + 7) rounded to the stream's type and converted: four lanes share a block, sixteen a word of four scale bytes.
+// `codes`, `scales`: the row's.  All lanes of the warp take part; those without columns (in == false) store nothing.
+template <typename H>
+__device__ __forceinline__ void convert_row(const SeamArgs& a, uint8_t* codes, uint8_t* scales, int c, bool in, Eight x)
+{
+    if constexpr (sizeof(H) == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x.v[k].x, x.v[k].y);
+            const uint32_t u = *reinterpret_cast<const uint32_t*>(&b);
+            x.v[k] = make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xFFFF0000u));
+        }
+    }
+    uint32_t peak = finite_peak(x), byte;                                   // columns behind the row: zeros
+    peak = max(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, 1));
+    peak = max(peak, __shfl_xor_sync(0xFFFFFFFFu, peak, 2));
+    const uint2 q = a.elem == MXFP8_E4M3 ? codes8<MXFP8_E4M3>(x, peak, a.rule, byte) : codes8<MXFP8_E5M2>(x, peak, a.rule, byte);
+    if (in) *reinterpret_cast<uint2*>(codes + c) = q;
+    const int lane = threadIdx.x & 31;
+    if (a.layout == MXFP8_SF_SWIZZLED) {                                    // whole words: the bytes behind the last block are zero
+        uint32_t word = in ? byte << (8 * (lane >> 2 & 3)) : 0u;          // c / 32 % 4 == lane / 4 % 4
+        word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
+        word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
+        if (in && (lane & 15) == 0) *reinterpret_cast<uint32_t*>(scales + (c >> 7) * 512) = word;
+    } else if (in && (lane & 3) == 0) scales[c >> 5] = (uint8_t)byte;
+}
+// The rows that pad a swizzled scale array to 128, by the threads that took the last row
+__device__ __forceinline__ void pad_scales(const SeamArgs& a, int t, int T)
+{
+    const int words = (a.cols / 32 + 3) / 4;
+    const int64_t rest = (128 - a.rows % 128) % 128 * words;
+    for (int64_t i = t; i < rest; i += T)
+        *reinterpret_cast<uint32_t*>(a.s_row + sf_swizzled_offset(a.rows + i / words, i % words * 4, words * 4)) = 0u;
+}
+
+// Forward.  WARP: rows of a warp each (the CTA has four), else of the CTA.  CONVERT: x is converted (see convert_row) instead of stored.  Rows go last to first: what reads h or x next begins with the first
+// rows, and finds them in L2 (8192 x 4096 in BF16 with the conversion in both orientations behind it: 76 us, first to last 79 us).
+template <typename Y, typename H, int NV, bool WARP, int STAGES, int MODE, bool CONVERT>
 __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 : 256)), WARP ? 8 : (NV == 1 ? 1 : (NV == 8 ? 2 : (NV == 2 ? 2 : 4)))) seam_forward_kernel(const SeamArgs a)
 {
     extern __shared__ __align__(16) uint8_t stage_mem[];
@@ -646,7 +712,24 @@ __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 
         }
         const float rn = rstd_of(WARP ? warp_sum(s.x + s.y) : cta_sum(s.x + s.y, area, turn), n_cols, a.eps);
         if (t == 0) a.rstd_pre[r] = rn;
-        if (a.x) {
+        if constexpr (CONVERT) {
+            uint8_t* codes = a.q_row + r * a.cols;
+            uint8_t* scales = a.s_row + (a.layout == MXFP8_SF_SWIZZLED ? sf_swizzled_offset(r, 0, a.cols / 32) : r * (a.cols / 32));
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (t + i * T) * 8;
+                if (c - t % 32 * 8 >= a.cols) break;                       // the whole warp is behind the row
+                const bool in = c < a.cols;
+                Eight x = zero8();
+                if (in) {
+                    const Eight w = params8(a.gamma_pre, c, known.bf16());
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x.v[k] = mul2(mul2(h[i].v[k], both(rn)), w.v[k]);
+                }
+                convert_row<H>(a, codes, scales, c, in, x);
+            }
+            if (r == a.rows - 1 && a.layout == MXFP8_SF_SWIZZLED) pad_scales(a, t, T);
+        } else if (a.x) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (t + i * T) * 8;
@@ -663,8 +746,7 @@ __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 
 }
 
 // Backward: same ownership and the same sums as seam_grad_any_kernel; column sums stay in registers.  With one vector per thread so do the
-// parameters and, between the two passes over the row, its elements: 8192 x 4096 in BF16 takes ... us, with two vectors read twice from shared memory
-// 86 us.
+// parameters and, between the two passes over the row, its elements: 8192 x 4096 in BF16 takes 80 us, with two vectors read twice from shared memory 86 us.
 template <typename Y, typename H, int NV, int STAGES, int MODE>
 __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
 {
@@ -954,11 +1036,12 @@ int mode_of(const SeamArgs& a, bool backward)
     return a.gate ? 2 : 1;
 }
 
-template <typename Y, typename H, int NV, bool WARP, int STAGES, int MODE = 0>
+template <typename Y, typename H, int NV, bool WARP, int STAGES, int MODE = 0, bool CONVERT = false>
 cudaError_t launch_forward_rows(const SeamArgs& a, int threads, cudaStream_t st)
 {
-    if (MODE == 0 && !WARP && mode_of<H>(a, false) == 1) return launch_forward_rows<Y, H, NV, WARP, STAGES, MODE == 0 && !WARP ? 1 : MODE>(a, threads, st);
-    auto kernel = seam_forward_kernel<Y, H, NV, WARP, STAGES, MODE>;
+    if (!CONVERT && a.q_row) return launch_forward_rows<Y, H, NV, WARP, STAGES, MODE, true>(a, threads, st);
+    if (MODE == 0 && !WARP && mode_of<H>(a, false) == 1) return launch_forward_rows<Y, H, NV, WARP, STAGES, MODE == 0 && !WARP ? 1 : MODE, CONVERT>(a, threads, st);
+    auto kernel = seam_forward_kernel<Y, H, NV, WARP, STAGES, MODE, CONVERT>;
     const int smem = STAGES * NV * (PIECES<Y> + PIECES<H>) * 16 * threads;
     static unsigned long long set = 0;
     const cudaError_t err = ensure_dynamic_smem(kernel, SMEM_PER_SM, set);
@@ -1079,10 +1162,12 @@ cudaError_t launch_grad(SeamArgs a, cudaStream_t st)
     return rc;
 }
 
-int seam_forward(const mxfp8_seam* s, const void* y, const void* h_in, void* h, void* x, float* rstd_post, float* rstd_pre, cudaStream_t st)
+int seam_forward(const mxfp8_seam* s, const void* y, const void* h_in, void* h, void* x, float* rstd_post, float* rstd_pre, cudaStream_t st,
+                 void* q_row = nullptr, void* s_row = nullptr, int elem = 0, int rule = 0, int layout = 0)
 {
     SeamArgs a = seam_args(s);
     a.y = y; a.h_in = h_in; a.h = h; a.x = x; a.rstd_post = rstd_post; a.rstd_pre = rstd_pre;
+    a.q_row = static_cast<uint8_t*>(q_row); a.s_row = static_cast<uint8_t*>(s_row); a.elem = elem; a.rule = rule; a.layout = layout;
     const cudaError_t err = by_types(s, [&](auto* yt, auto* ht) {
         return launch_forward<std::remove_pointer_t<decltype(yt)>, std::remove_pointer_t<decltype(ht)>>(a, st);
     });
@@ -1124,6 +1209,9 @@ extern "C" int mxfp8_residual_rmsnorm_quantize(const mxfp8_seam* seam, const voi
                         q_row, s_row, q_col, s_col, sf_layout);
     if (bad != MXFP8_OK) return bad;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    // row blocks alone, of 8-bit elements: converted where x is computed.  (Column blocks need 32 rows at a time: a second launch, which reads h.)
+    if (orientation == MXFP8_ROW && fp8_elem(elem) && aligned16(y) && aligned16(h_in) && aligned16(seam->gamma_post) && aligned16(seam->gate))
+        return seam_forward(seam, y, h_in, h, nullptr, rstd_post, rstd_pre, st, q_row, s_row, elem, scale_rule, sf_layout);
     bad = seam_forward(seam, y, h_in, h, nullptr, rstd_post, rstd_pre, st);
     if (bad != MXFP8_OK) return bad;
     const QuantizeItem item{h, seam->rows, seam->cols, q_row, s_row, q_col, s_col};

@@ -195,7 +195,9 @@ def test_backward_against_differences():
 def test_converted_output_is_that_of_the_separate_call():
     for rows, cols, stream, orientation, layout in ((64, 512, "bf16", B.BOTH, B.SF_SWIZZLED), (96, 160, "fp32", B.ROW, B.SF_LINEAR), (32, 4096, "bf16", B.COL, B.SF_SWIZZLED),
                                                     (1, 4096, "bf16", B.ROW, B.SF_SWIZZLED), (333, 1056, "bf16", B.ROW, B.SF_SWIZZLED),
-                                                    (130, 2048, "fp32", B.ROW, B.SF_SWIZZLED), (160, 96, "fp32", B.BOTH, B.SF_LINEAR)):
+                                                    (130, 2048, "fp32", B.ROW, B.SF_SWIZZLED), (160, 96, "fp32", B.BOTH, B.SF_LINEAR),
+                                                    (1300, 256, "bf16", B.ROW, B.SF_SWIZZLED), (1201, 416, "bf16", B.ROW, B.SF_LINEAR), (1190, 1024, "fp32", B.ROW, B.SF_SWIZZLED),
+                                                    (260, 6176, "bf16", B.ROW, B.SF_SWIZZLED), (2, 16384, "bf16", B.ROW, B.SF_LINEAR), (3, 16352, "fp32", B.ROW, B.SF_SWIZZLED)):
         for elem, rule in ((B.E4M3, B.RULE_PAPER), (B.E5M2, B.RULE_OCP), (B.E2M1, B.RULE_PAPER)):
             d = inputs(rows, cols, ("bf16", stream, stream), True, 0, seed=4)
             seam = B.make_seam(d["gamma_pre"], d["gamma_post"], None, 1, 1.0, 1.0, 1e-6)
@@ -211,6 +213,32 @@ def test_converted_output_is_that_of_the_separate_call():
             B.mxfp8_quantize(x, orientation, rule, elem, *want, layout)
             for got, w in zip(outs, want):
                 assert (got is None) == (w is None) and (got is None or torch.equal(got, w)), (rows, cols, stream, orientation, elem)
+
+
+@pytest.mark.parametrize("orientation", [B.ROW, B.BOTH])
+def test_conversion_of_infinities_nan_and_zero_rows(orientation):
+    """Infinities and NaN in x (from the weights) saturate and stay, and neither enters a block's largest magnitude."""
+    rows, cols = 64, 256
+    for elem in (B.E4M3, B.E5M2):
+        d = inputs(rows, cols, ("bf16", "bf16", "bf16"), True, 0, seed=9)
+        d["gamma_pre"][5], d["gamma_pre"][40], d["gamma_pre"][200] = float("inf"), float("nan"), float("-inf")
+        d["gamma_pre"][96:128] = float("inf")                        # a block without a finite element
+        d["y"][7] = 0
+        d["h_in"][7] = 0
+        seam = B.make_seam(d["gamma_pre"], d["gamma_post"])
+        h, rp, rn = torch.empty_like(d["h_in"]), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        outs, want = (B.alloc_quantize_outputs(rows, cols, orientation, B.SF_SWIZZLED) for _ in range(2))
+        B.mxfp8_residual_rmsnorm_quantize(seam, d["y"], d["h_in"], h, rp, rn, orientation, B.RULE_PAPER, elem, *outs, B.SF_SWIZZLED)
+        x = ((h.float() * rn.unsqueeze(1)) * d["gamma_pre"].float()).to(h.dtype)
+        B.mxfp8_quantize(x, orientation, B.RULE_PAPER, elem, *want, B.SF_SWIZZLED)
+        for k, (got, w) in enumerate(zip(outs, want)):
+            if got is None:
+                continue
+            if k % 2 == 0:                                            # codes: any NaN for a NaN
+                got, w = (t.view(torch.float8_e4m3fn if elem == B.E4M3 else torch.float8_e5m2).float() for t in (got, w))
+                assert torch.equal(got.isnan(), w.isnan())
+                got, w = got.nan_to_num(0.0), w.nan_to_num(0.0)
+            assert torch.equal(got, w)
 
 
 def test_zero_rows_and_special_values():
