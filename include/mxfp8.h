@@ -527,7 +527,7 @@ int mxfp8_residual_rmsnorm_grad(const mxfp8_seam* seam, const void* dx, const vo
  * S is FP64 (squares of eight neighbours at a time are added in FP32 where that loses no range), in a fixed order: the result is the same every
  * time.  A norm that is not finite leaves the values as they are (dst = src, factor = 1), so that the caller can skip the step.
  *   items   HOST array of `count` entries, read during the call (it may change afterwards).  src and dst are aligned to their elements; dst may be
- *           src, otherwise no dst may overlap another item.  numel may be 0; count may be 0 (norm 0).
+ *           its own src, and overlaps nothing else (no other item's src or dst).  numel may be 0; count may be 0 (norm 0).
  * mxfp8_grad_sumsq -- S alone, to `sumsq` (device, one FP64): ranks that hold parts of the gradients add theirs before
  * mxfp8_grad_scale -- computes norm and factor from *sumsq and scales; norm (device, two FP32): norm and factor.  With dst == src
  *           everywhere and factor 1 nothing is read or written.

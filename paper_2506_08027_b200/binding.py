@@ -692,7 +692,7 @@ class Seam:
 
 def make_seam(gamma_pre: torch.Tensor, gamma_post=None, gate=None, rows_per_gate: int = 1, branch_scale: float = 1.0, residual_scale: float = 1.0,
               eps: float = 1e-5) -> Seam:
-    """gamma_pre, gamma_post (or None): [cols]; gate (or None): [ceil(rows / rows_per_gate), cols]; all of one type."""
+    """gamma_pre, gamma_post (or None): [cols]; gate (or None): [ceil(rows / rows_per_gate), cols]; all of one type.  Their addresses are taken here."""
     given = [t for t in (gamma_pre, gamma_post, gate) if t is not None]
     if any(t.dtype is not gamma_pre.dtype or t.shape[-1] != gamma_pre.numel() for t in given) or gamma_pre.dim() != 1 or \
             (gamma_post is not None and gamma_post.dim() != 1) or (gate is not None and (gate.dim() != 2 or rows_per_gate < 1)):
@@ -776,7 +776,7 @@ class GradItems:
 
 def make_grad_items(grads, results=None) -> GradItems:
     """grads: FP32 / BF16 tensors of one device; results: where the scaled values go (None: in place).  Build it once and reuse it while the
-    tensors live; mxfp8_grad_sumsq needs no results."""
+    tensors keep their storage; mxfp8_grad_sumsq needs no results.  What is written may overlap no other gradient (the same one twice, say)."""
     grads, results = list(grads), None if results is None else list(results)
     if results is not None and (len(results) != len(grads) or any(r.dtype is not g.dtype or r.shape != g.shape for g, r in zip(grads, results))):
         raise ValueError("results have the gradients' shapes and types")
@@ -790,6 +790,14 @@ def make_grad_items(grads, results=None) -> GradItems:
                 raise ValueError("gradients lie on one CUDA device")
             items.device = t.get_device()
         items.c[k].src, items.c[k].dst, items.c[k].numel, items.c[k].dtype = _ptr(g), _ptr(to), g.numel(), _dtype_code(g)
+    # what is written overlaps nothing else, else a value would be scaled twice or read after it was
+    spans = sorted((c.dst, c.dst + t.nbytes, True, k) for k, (c, t) in enumerate(zip(items.c, grads)) if t.numel()) + \
+        sorted((c.src, c.src + t.nbytes, False, k) for k, (c, t) in enumerate(zip(items.c, grads)) if t.numel() and c.src != c.dst)
+    end, written_end = -1, -1                                # of all spans so far, of those that are written
+    for lo, hi, written, _ in sorted(spans):
+        if lo < (end if written else written_end):
+            raise ValueError("a gradient that is written overlaps another one")
+        end, written_end = max(end, hi), max(written_end, hi if written else -1)
     return items
 
 

@@ -294,8 +294,9 @@ __global__ void __launch_bounds__(32 * WARPS, 1) moe_gate_up_kernel(const MoeArg
     extern __shared__ __align__(16) uint8_t dynamic[];
     __shared__ Choice choice;
     constexpr int P = 8 * NT + 1, UNIT_SUMS = 2 * TILE_ROWS * P, STAGE = 2 * TILE_BYTES;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the second launch may choose, and fetch weights, beside this one
     asm volatile("griddepcontrol.wait;" ::: "memory");                    // all that was launched before this call is done
+    // only now: the second launch chooses and fetches weights beside this one, from inputs that those launches may have written
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* ring = dynamic + warp * STAGES * STAGE;
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;

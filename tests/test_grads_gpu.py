@@ -163,3 +163,15 @@ def test_offsets_beyond_32_bits():
     norm, factor = clip([g], None, 1.5)
     assert norm == 3.0 and abs(factor - 0.5) <= 1e-6
     assert float(g[0]) == 0.5 and float(g[n - 1]) == 1.0 and float(g[n // 2]) == 1.0 and int((g != 0).sum()) == 3
+
+
+def test_overlapping_gradients_are_refused():
+    flat = torch.zeros(100, device="cuda")
+    a, b, c = flat[:40], flat[40:80], flat[39:60]
+    out = torch.zeros(100, device="cuda")
+    B.make_grad_items([a, b])
+    B.make_grad_items([a, b], [out[:40], out[40:80]])
+    B.make_grad_items([a, c], [out[:40], out[40:61]])                  # read twice, written apart
+    for grads, results in (([a, a], None), ([a, c], None), ([a, b], [out[:40], out[:40]]), ([a, b], [b, out[:40]]), ([a, b], [out[:40], out[39:79]])):
+        with pytest.raises(ValueError):
+            B.make_grad_items(grads, results)
