@@ -925,10 +925,10 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
 }
 
 // Joins the CTAs' sums.  blockIdx.y: 0 / 1 the weights, then the rows of the gate that several CTAs hold.
-constexpr int JOIN_COLS = 32, JOIN_WARPS = 32;
+constexpr int JOIN_COLS = 32, JOIN_WARPS = 16;
 __global__ void __launch_bounds__(32 * JOIN_WARPS) seam_join_kernel(const SeamArgs a, int parts)
 {
-    __shared__ float area[JOIN_WARPS][JOIN_COLS + 1];
+    __shared__ float area[JOIN_WARPS][JOIN_COLS];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c = blockIdx.x * JOIN_COLS + lane, weights = (a.d_gamma_pre != nullptr) + (a.d_gamma_post != nullptr);
@@ -954,10 +954,12 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) seam_join_kernel(const SeamAr
         }
         area[warp][lane] = s;
         __syncthreads();
-        s = area[lane][warp];                               // warp w adds column w
+        if (warp == 0) {
+            s = 0.f;
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, off);
-        if (lane == 0 && blockIdx.x * JOIN_COLS + warp < a.cols) to[blockIdx.x * JOIN_COLS + warp] = s;
+            for (int w = 0; w < JOIN_WARPS; ++w) s += area[w][lane];
+            if (c < a.cols) to[c] = s;
+        }
         __syncthreads();
     }
 }
