@@ -277,13 +277,14 @@ __device__ __forceinline__ void run_tiles(const __nv_bfloat16* const (&from)[NX]
     }
 }
 
-// m of one (slot, row of the matrix)
+// m of one (slot, row of the matrix).  The second part of an infinity is zero, not infinity less infinity.
 __device__ __forceinline__ void put_m(const MoeArgs& a, int64_t row, int n, float gate, float up)
 {
     const float m = activate(gate, a.act) * up;
     const __nv_bfloat16 hi = __float2bfloat16_rn(m);
     a.m_hi[row * a.inner + n] = hi;
-    a.m_lo[row * a.inner + n] = __float2bfloat16_rn(m - __bfloat162float(hi));
+    const float rest = m - __bfloat162float(hi);
+    a.m_lo[row * a.inner + n] = __float2bfloat16_rn(isinf(__bfloat162float(hi)) ? 0.f : rest);
 }
 
 // ---- first launch.  A unit is 16 gate rows and the 16 up rows that belong to them, for the slots of one entry.  The CTAs take the units in
@@ -504,6 +505,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * WARPS, 1) moe_d
                 }
             __syncwarp();
         }
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         // a thread per output: the sums of the warps of both CTAs
         const int half = a.tokens * (DOWN_ROWS / 2);
@@ -528,6 +530,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * WARPS, 1) moe_d
             if (a.bf16_out) static_cast<__nv_bfloat16*>(a.y)[to] = __float2bfloat16_rn(s);
             else static_cast<float*>(a.y)[to] = s;
         }
+        __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
     copies_done<0>();

@@ -631,8 +631,8 @@ __device__ __forceinline__ void pad_scales(const SeamArgs& a, int t, int T)
         *reinterpret_cast<uint32_t*>(a.s_row + sf_swizzled_offset(a.rows + i / words, i % words * 4, words * 4)) = 0u;
 }
 
-// Forward.  WARP: rows of a warp each (the CTA has four), else of the CTA.  CONVERT: x is converted (see convert_row) instead of stored.  Rows go last to first: what reads h or x next begins with the first
-// rows, and finds them in L2 (8192 x 4096 in BF16 with the conversion in both orientations behind it: 76 us, first to last 79 us).
+// Forward.  WARP: rows of a warp each (the CTA has four), else of the CTA.  CONVERT: x is converted (see convert_row) instead of stored.
+// Rows go last to first: what reads h or x next begins with the first rows, and finds them in L2 (8192 x 4096 in BF16 with the conversion in both orientations behind it: 76 us, first to last 79 us).
 template <typename Y, typename H, int NV, bool WARP, int STAGES, int MODE, bool CONVERT>
 __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 : 256)), WARP ? 8 : (NV == 1 ? 1 : (NV == 8 ? 2 : (NV == 2 ? 2 : 4)))) seam_forward_kernel(const SeamArgs a)
 {
@@ -926,7 +926,8 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
     }
 }
 
-// Joins the CTAs' sums; 16 warps because the chain of dependent loads is what it waits for (3065 x 2048 with gates: 39.5 us, 41.1 with 8).  blockIdx.y: 0 / 1 the weights, then the rows of the gate that several CTAs hold.
+// Joins the CTAs' sums; 16 warps because the latency of the loads is what it waits for (3065 x 2048 with gates: 39.5 us, 41.1 with 8).
+// blockIdx.y: 0 / 1 the weights, then the rows of the gate that several CTAs hold.
 constexpr int JOIN_COLS = 32, JOIN_WARPS = 16;
 __global__ void __launch_bounds__(32 * JOIN_WARPS) seam_join_kernel(const SeamArgs a, int parts)
 {

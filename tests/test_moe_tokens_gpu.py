@@ -184,6 +184,28 @@ def test_wide_scales():
     assert bool(((y.double() - want).abs() <= slack + 2.0 ** -20 * want.abs() + floor).all())
 
 
+@pytest.mark.parametrize("sign", [1, -1])
+def test_an_infinite_intermediate_stays_infinite(sign):
+    """The first token's m overflows FP32 (2^100 * 2^100); with weights that are all 1 the formula gives an infinity of its sign, and the second
+    token, whose m is 64 * 64, must not notice.  All of the second token's numbers are powers of two, so its outputs are exact."""
+    cols, inner = 64, 96
+    packed = []
+    for rows, c in ((2 * inner, cols), (cols, inner)):
+        q = torch.empty(rows, c, dtype=torch.uint8, device="cuda")
+        s = torch.empty(rows * (c // 32), dtype=torch.uint8, device="cuda")
+        B.mxfp8_quantize(torch.ones(rows, c, device="cuda"), B.ROW, B.RULE_PAPER, B.E2M1, q, s, None, None, B.SF_LINEAR)
+        packed.append(torch.empty(B.mxfp8_e2m1_packed_bytes(1, rows, c), dtype=torch.uint8, device="cuda"))
+        B.mxfp8_e2m1_pack(q, s, 1, packed[-1])
+    x = torch.zeros(2, cols, dtype=torch.bfloat16, device="cuda")
+    x[0, 0] = sign * 2.0 ** 100
+    x[1] = 1.0
+    logits = torch.zeros(2, 1, device="cuda")
+    kind = B.ACT_RELU if sign > 0 else B.ACT_NONE
+    y, _, _ = run(x, logits, 1, packed, inner, kind, True, torch.float32)
+    assert bool((y[0] == float("inf")).all())                            # (-2^100)^2 as well
+    assert bool((y[1] == inner * 64.0 * 64.0).all())
+
+
 def test_graph_streams_and_two_calls_at_once():
     tokens, top_k, experts, cols, inner = 6, 3, 16, 512, 256
     g = torch.Generator(device="cuda").manual_seed(4)
