@@ -22,6 +22,8 @@
 //   optional store mode that writes the decoded values back instead of the codes (round trip).
 #pragma once
 
+#include <type_traits>
+
 #include <cuda.h>
 
 #include "mxfp8_device.cuh"
@@ -111,7 +113,7 @@ __device__ __forceinline__ void act_slab(uint8_t* mine)
 // normalisation y = ((x - mean[row]) * rstd[row]) * gamma[col] + beta[col], four FP32 operations
 // in that order, rounded once to the source dtype.  Rows and columns beyond the tensor hold TMA's zero fill and
 // are left alone (their statistics and weights do not exist).
-template <bool BF>
+template <bool BF, bool LAYER>
 __device__ __forceinline__ void norm_slab(uint8_t* mine, const float* __restrict__ rstd, const void* __restrict__ gamma_col,
                                           int rows_here, bool col_ok, const float* __restrict__ mean, const void* __restrict__ beta_col)
 {
@@ -128,28 +130,38 @@ __device__ __forceinline__ void norm_slab(uint8_t* mine, const float* __restrict
     };
     float g[4], b[4] = {0.f, 0.f, 0.f, 0.f};
     weights(gamma_col, g);
-    const bool layer = mean != nullptr;      // layer normalisation: subtract the row mean first, add the per-column bias last
-    if (layer) weights(beta_col, b);
-    // one value: a subtraction (layer normalisation only), two products and an addition (layer normalisation only),
+    if constexpr (LAYER) weights(beta_col, b);      // layer normalisation: subtract the row mean first, add the per-column bias last
+    // two values: a subtraction (layer normalisation only), two products and an addition (layer normalisation only),
     // each rounded to FP32 on its own (no fused multiply-add: the definition has four roundings)
-    auto one = [&](float x, float m, float r, int i) {
-        const float t = __fmul_rn(__fmul_rn(layer ? __fsub_rn(x, m) : x, r), g[i]);
-        return layer ? __fadd_rn(t, b[i]) : t;
+    auto two = [&](float& v0, float& v1, float m, uint64_t r, int i) {
+        if constexpr (LAYER) v0 = __fsub_rn(v0, m), v1 = __fsub_rn(v1, m);
+        uint64_t v, w;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(v0), "f"(v1));
+        asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(g[i]), "f"(g[i + 1]));
+        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(r));
+        asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(w));
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(v0), "=f"(v1) : "l"(v));
+        if constexpr (LAYER) v0 = __fadd_rn(v0, b[i]), v1 = __fadd_rn(v1, b[i + 1]);
     };
 #pragma unroll 8
     for (int j = 0; j < 32; ++j) {
         if (j >= rows_here) break;
-        const float r = rstd[j];
-        const float m = layer ? mean[j] : 0.f;
+        uint64_t r;
+        asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(rstd[j]));
+        const float m = LAYER ? mean[j] : 0.f;
         uint2 w = *reinterpret_cast<const uint2*>(mine + j * T_BYTES);
         if constexpr (BF) {
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(one(__uint_as_float(w.x << 16), m, r, 0), one(__uint_as_float(w.x & 0xFFFF0000u), m, r, 1));
-            const __nv_bfloat162 hi = __floats2bfloat162_rn(one(__uint_as_float(w.y << 16), m, r, 2), one(__uint_as_float(w.y & 0xFFFF0000u), m, r, 3));
+            float v[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u)};
+            two(v[0], v[1], m, r, 0);
+            two(v[2], v[3], m, r, 2);
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(v[0], v[1]), hi = __floats2bfloat162_rn(v[2], v[3]);
             w.x = *reinterpret_cast<const uint32_t*>(&lo);
             w.y = *reinterpret_cast<const uint32_t*>(&hi);
         } else {
-            w.x = __float_as_uint(one(__uint_as_float(w.x), m, r, 0));
-            w.y = __float_as_uint(one(__uint_as_float(w.y), m, r, 1));
+            float v0 = __uint_as_float(w.x), v1 = __uint_as_float(w.y);
+            two(v0, v1, m, r, 0);
+            w.x = __float_as_uint(v0);
+            w.y = __float_as_uint(v1);
         }
         *reinterpret_cast<uint2*>(mine + j * T_BYTES) = w;
     }
@@ -667,10 +679,15 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
             const int64_t row_first = grow0 + warp * 32;
             const int rows_in = (int)max((int64_t)0, min((int64_t)32, p.rows - row_first));
             const int64_t col_first = gcol0 + lane * VEC;
-            norm_slab<BF>(in_tile + warp * 32 * T_BYTES + lane * 8, batch.rstd + row_first,
-                          static_cast<const uint8_t*>(batch.gamma) + col_first * (BF ? 2 : 4), rows_in, col_first < p.cols,
-                          batch.mean ? batch.mean + row_first : nullptr,
-                          batch.beta ? static_cast<const uint8_t*>(batch.beta) + col_first * (BF ? 2 : 4) : nullptr);
+            auto norm = [&](auto layer) {
+                constexpr bool LAYER = decltype(layer)::value;
+                norm_slab<BF, LAYER>(in_tile + warp * 32 * T_BYTES + lane * 8, batch.rstd + row_first,
+                                     static_cast<const uint8_t*>(batch.gamma) + col_first * (BF ? 2 : 4), rows_in, col_first < p.cols,
+                                     LAYER ? batch.mean + row_first : nullptr,
+                                     LAYER ? static_cast<const uint8_t*>(batch.beta) + col_first * (BF ? 2 : 4) : nullptr);
+            };
+            if (batch.mean) norm(std::true_type{});
+            else norm(std::false_type{});
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         if (PRO == PRO_ELEMENTWISE && batch.act != MXFP8_ACT_NONE) {
