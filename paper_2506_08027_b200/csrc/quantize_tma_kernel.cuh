@@ -113,24 +113,25 @@ __device__ __forceinline__ void act_slab(uint8_t* mine)
 // normalisation y = ((x - mean[row]) * rstd[row]) * gamma[col] + beta[col], four FP32 operations
 // in that order, rounded once to the source dtype.  Rows and columns beyond the tensor hold TMA's zero fill and
 // are left alone (their statistics and weights do not exist).
+// What a warp needs for its slab besides the tile: a row's statistics per lane, the weights of the lane's own columns.
+struct SlabNorm {
+    float rstd, mean;
+    uint2 gamma, beta;
+};
 template <bool BF, bool LAYER>
-__device__ __forceinline__ void norm_slab(uint8_t* mine, const float* __restrict__ rstd, const void* __restrict__ gamma_col,
-                                          int rows_here, bool col_ok, const float* __restrict__ mean, const void* __restrict__ beta_col)
+__device__ __forceinline__ void norm_slab(uint8_t* mine, const SlabNorm& n, int rows_here, bool col_ok)
 {
-    if (!col_ok) return;
-    auto weights = [](const void* ptr, float (&g)[4]) {
+    auto weights = [](uint2 w, float (&g)[4]) {
         if constexpr (BF) {
-            const uint2 w = *reinterpret_cast<const uint2*>(ptr);
             g[0] = __uint_as_float(w.x << 16); g[1] = __uint_as_float(w.x & 0xFFFF0000u);
             g[2] = __uint_as_float(w.y << 16); g[3] = __uint_as_float(w.y & 0xFFFF0000u);
         } else {
-            const float2 w = *reinterpret_cast<const float2*>(ptr);
-            g[0] = w.x; g[1] = w.y; g[2] = 0.f; g[3] = 0.f;
+            g[0] = __uint_as_float(w.x); g[1] = __uint_as_float(w.y); g[2] = 0.f; g[3] = 0.f;
         }
     };
     float g[4], b[4] = {0.f, 0.f, 0.f, 0.f};
-    weights(gamma_col, g);
-    if constexpr (LAYER) weights(beta_col, b);      // layer normalisation: subtract the row mean first, add the per-column bias last
+    weights(n.gamma, g);
+    if constexpr (LAYER) weights(n.beta, b);      // layer normalisation: subtract the row mean first, add the per-column bias last
     // two values: a subtraction (layer normalisation only), two products and an addition (layer normalisation only),
     // each rounded to FP32 on its own (no fused multiply-add: the definition has four roundings)
     auto two = [&](float& v0, float& v1, float m, uint64_t r, int i) {
@@ -147,8 +148,8 @@ __device__ __forceinline__ void norm_slab(uint8_t* mine, const float* __restrict
     for (int j = 0; j < 32; ++j) {
         if (j >= rows_here) break;
         uint64_t r;
-        asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(rstd[j]));
-        const float m = LAYER ? mean[j] : 0.f;
+        asm("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(__shfl_sync(0xFFFFFFFFu, n.rstd, j)));
+        const float m = LAYER ? __shfl_sync(0xFFFFFFFFu, n.mean, j) : 0.f;
         uint2 w = *reinterpret_cast<const uint2*>(mine + j * T_BYTES);
         if constexpr (BF) {
             float v[4] = {__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xFFFF0000u)};
@@ -163,7 +164,7 @@ __device__ __forceinline__ void norm_slab(uint8_t* mine, const float* __restrict
             w.x = __float_as_uint(v0);
             w.y = __float_as_uint(v1);
         }
-        *reinterpret_cast<uint2*>(mine + j * T_BYTES) = w;
+        if (col_ok) *reinterpret_cast<uint2*>(mine + j * T_BYTES) = w;
     }
 }
 
@@ -637,6 +638,21 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
         divmod((uint32_t)(tile - batch.tile_start[ti]), (uint32_t)p.tiles_x, p.tiles_x_magic, tile_y, tile_x);
         const int64_t gcol0 = (int64_t)tile_x * T_COLS, grow0 = (int64_t)tile_y * T_ROWS;
 
+        // statistics and weights of a normalisation come while the tile does (asked for after it, they cost a trip to L2 per tile)
+        SlabNorm slab_norm{};
+        const int64_t row_first = grow0 + warp * 32, col_first = gcol0 + lane * VEC;
+        const int rows_in = (int)max((int64_t)0, min((int64_t)32, p.rows - row_first));
+        if (PRO == PRO_ELEMENTWISE && batch.rstd != nullptr) {
+            if (lane < rows_in) {
+                slab_norm.rstd = batch.rstd[row_first + lane];
+                if (batch.mean) slab_norm.mean = batch.mean[row_first + lane];
+            }
+            if (col_first < p.cols) {
+                slab_norm.gamma = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(batch.gamma) + col_first * (BF ? 2 : 4));
+                if (batch.beta) slab_norm.beta = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(batch.beta) + col_first * (BF ? 2 : 4));
+            }
+        }
+
         // wait for the tile (bounded: on expiry report through the status word and leave).  A warp needs nothing from the
         // other warps to start on its slab, so the CTA meets only once per tile, at the barrier that frees the ring slot:
         // a warp whose wait ran out skips the tile and says so there.  (The gated mode meets in between for the up tile,
@@ -676,15 +692,8 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
         }
         if (PRO == PRO_ELEMENTWISE && batch.rstd != nullptr) {
             // RMS normalisation in place (single-tensor launches only), then the unchanged conversion
-            const int64_t row_first = grow0 + warp * 32;
-            const int rows_in = (int)max((int64_t)0, min((int64_t)32, p.rows - row_first));
-            const int64_t col_first = gcol0 + lane * VEC;
             auto norm = [&](auto layer) {
-                constexpr bool LAYER = decltype(layer)::value;
-                norm_slab<BF, LAYER>(in_tile + warp * 32 * T_BYTES + lane * 8, batch.rstd + row_first,
-                                     static_cast<const uint8_t*>(batch.gamma) + col_first * (BF ? 2 : 4), rows_in, col_first < p.cols,
-                                     LAYER ? batch.mean + row_first : nullptr,
-                                     LAYER ? static_cast<const uint8_t*>(batch.beta) + col_first * (BF ? 2 : 4) : nullptr);
+                norm_slab<BF, decltype(layer)::value>(in_tile + warp * 32 * T_BYTES + lane * 8, slab_norm, rows_in, col_first < p.cols);
             };
             if (batch.mean) norm(std::true_type{});
             else norm(std::false_type{});
