@@ -520,7 +520,8 @@ __device__ __noinline__ void slab_careful(const uint8_t* __restrict__ my_in, uin
 
 // PRO: what runs on a tile before the conversion.  Separate instantiations, so that the plain conversion carries
 // none of the prologue code (folding the prologues in at run time cost the plain kernels 2-5 %).
-enum { PRO_NONE = 0, PRO_ELEMENTWISE = 1 /* activation or RMS normalisation */, PRO_GLU = 2 /* gated activation */ };
+// (And activations and norms in one kernel cost the activations up to 2 %: the statistics of a norm stay in registers while its tile comes.)
+enum { PRO_NONE = 0, PRO_ACT = 1 /* activation */, PRO_GLU = 2 /* gated activation */, PRO_NORM = 3 /* RMS or layer normalisation */ };
 
 template <int DTYPE, int ELEM, bool DO_ROW, bool DO_COL, bool EMU, int PRO>
 __global__ void __launch_bounds__(QT_THREADS, QT_CTAS_PER_SM)
@@ -642,7 +643,7 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
         SlabNorm slab_norm{};
         const int64_t row_first = grow0 + warp * 32, col_first = gcol0 + lane * VEC;
         const int rows_in = (int)max((int64_t)0, min((int64_t)32, p.rows - row_first));
-        if (PRO == PRO_ELEMENTWISE && batch.rstd != nullptr) {
+        if constexpr (PRO == PRO_NORM) {
             if (lane < rows_in) {
                 slab_norm.rstd = batch.rstd[row_first + lane];
                 if (batch.mean) slab_norm.mean = batch.mean[row_first + lane];
@@ -690,7 +691,7 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
             __syncthreads();                     // every warp has consumed the up tile: fetch the next one under the conversion
             if (tid == 0 && slot_tile[(it + 1) % RING] < num_tiles) issue_up(slot_tile[(it + 1) % RING]);
         }
-        if (PRO == PRO_ELEMENTWISE && batch.rstd != nullptr) {
+        if constexpr (PRO == PRO_NORM) {
             // RMS normalisation in place (single-tensor launches only), then the unchanged conversion
             auto norm = [&](auto layer) {
                 norm_slab<BF, decltype(layer)::value>(in_tile + warp * 32 * T_BYTES + lane * 8, slab_norm, rows_in, col_first < p.cols);
@@ -699,7 +700,7 @@ quantize_tma_kernel(const __grid_constant__ QMaps maps, const __grid_constant__ 
             else norm(std::false_type{});
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
-        if (PRO == PRO_ELEMENTWISE && batch.act != MXFP8_ACT_NONE) {
+        if constexpr (PRO == PRO_ACT) {
             // activation in place: every lane rewrites exactly the 8 bytes per row it reads below, rounded once
             // to the source dtype, so what follows equals the conversion of a tensor that holds act(x)
             uint8_t* mine = in_tile + warp * 32 * T_BYTES + lane * 8;
@@ -842,9 +843,10 @@ cudaError_t quantize_tma_launch(bool bf16_src, int orientation, bool emulate, co
 {
     if (p.glu_cols || p.up_map)
         return bf16_src ? launch_o<MXFP8_BF16, ELEM, false, PRO_GLU>(orientation, ms, p, st) : launch_o<MXFP8_FP32, ELEM, false, PRO_GLU>(orientation, ms, p, st);
-    if (p.rstd != nullptr || p.act != MXFP8_ACT_NONE)
-        return bf16_src ? launch_o<MXFP8_BF16, ELEM, false, PRO_ELEMENTWISE>(orientation, ms, p, st)
-                        : launch_o<MXFP8_FP32, ELEM, false, PRO_ELEMENTWISE>(orientation, ms, p, st);
+    if (p.rstd != nullptr)
+        return bf16_src ? launch_o<MXFP8_BF16, ELEM, false, PRO_NORM>(orientation, ms, p, st) : launch_o<MXFP8_FP32, ELEM, false, PRO_NORM>(orientation, ms, p, st);
+    if (p.act != MXFP8_ACT_NONE)
+        return bf16_src ? launch_o<MXFP8_BF16, ELEM, false, PRO_ACT>(orientation, ms, p, st) : launch_o<MXFP8_FP32, ELEM, false, PRO_ACT>(orientation, ms, p, st);
     if (emulate)
         return bf16_src ? launch_o<MXFP8_BF16, ELEM, true>(orientation, ms, p, st) : launch_o<MXFP8_FP32, ELEM, true>(orientation, ms, p, st);
     return bf16_src ? launch_o<MXFP8_BF16, ELEM, false>(orientation, ms, p, st) : launch_o<MXFP8_FP32, ELEM, false>(orientation, ms, p, st);
