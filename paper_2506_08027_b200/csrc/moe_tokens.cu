@@ -3,7 +3,8 @@
 //   2. the down products of the chosen experts and their weighted sum, straight into y
 // Every CTA of both launches chooses for itself (a few hundred logits, cheaper than a launch in between).  Bound by the
 // weights of the experts that are used, 17/32 byte each, which are read once, and by the instructions that decode them (210 per tile of 16 x 128 in launch 1).
-// One token with 8 of 64 experts of 2048 x 1408: 23 us; 16 tokens with 6: 69 us; 32 tokens with 2 of 8 experts of 4096 x 14336: 280 us.
+// One token with 8 of 64 experts of 2048 x 1408: 23 us; 16 tokens with 6: 68 to 73 us; 32 tokens with 2 of 8 experts of 4096 x 14336: 280 to
+// 317 us from run to run.
 #include "e2m1_tiles.cuh"
 #include "mxfp8_host.h"
 

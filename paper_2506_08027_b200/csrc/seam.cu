@@ -4,7 +4,7 @@
 //   rstd_pre  = 1 / sqrt(mean h^2 + eps);  x = (h rstd_pre) gamma_pre
 //
 // Bound by memory: forward y, h_in -> h, x; backward dx, dh, y, h -> dy, dh_in, each element once.  8192 x 4096 in BF16: forward
-// 49.5 us, backward 76 us, 83 and 81 % of the measured copy rate.
+// 49.5 us, backward 76 to 80 us, 83 and 77 to 81 % of the measured copy rate.
 #include <cuda_bf16.h>
 
 #include <initializer_list>
@@ -749,7 +749,7 @@ __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 
 
 // Backward: same ownership and the same sums as seam_grad_any_kernel; column sums stay in registers.  With one vector per thread so do the
 // parameters and, between the two passes over the row, its elements: 8192 x 4096 in BF16 took 82 us that
-// way and 86 us with two vectors read twice from shared memory; it takes 76 us (81 % of the copy rate) since statistics are read a row ahead and 16 warps join.
+// way and 86 us with two vectors read twice from shared memory; it takes 76 to 80 us since statistics are read a row ahead and 16 warps join.
 template <typename Y, typename H, int NV, int STAGES, int MODE>
 __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
 {
