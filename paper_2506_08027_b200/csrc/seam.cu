@@ -514,6 +514,13 @@ __device__ __forceinline__ Eight zero8()
     return e;
 }
 
+__device__ __forceinline__ Eight times(Eight e, float by)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e.v[k] = mul2(e.v[k], both(by));
+    return e;
+}
+
 // Eight elements from 16-byte pieces, `apart` bytes from one another in shared memory / side by side in global memory
 template <typename T>
 __device__ __forceinline__ Eight unpack(const uint4 (&w)[PIECES<T>])
@@ -785,12 +792,12 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
         copies_issued();
     };
     constexpr bool KEEP = NV == 1;
-    Eight pre[NV], post[NV], gates[NV];
+    Eight pre[NV], post[NV], gates[NV];                      // those of gamma_post and the gate without branch_scale
 #pragma unroll
     for (int i = 0; i < NV; ++i) pre[i] = post[i] = gates[i] = zero8();
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) issue(r0 + s, s);
-    Eight keep_pre, keep_post, keep_gate, keep_h, keep_dx, keep_dh, keep_y;
+    Eight keep_pre, keep_post, keep_gate, keep_xh, keep_dx, keep_sum, keep_yh;
     int64_t gate_kept = -1;
     if (KEEP && t * 8 < a.cols) {
         keep_pre = params8(a.gamma_pre, t * 8, known.bf16());
@@ -815,15 +822,15 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
         }
         copies_done<STAGES - 1>();
         const uint8_t* at = mine + stage * NV * Q * piece;
-        // the sums without the factors that all their terms share
+        // sums of products of normalised elements: with both statistics left out until the end, their squares leave FP32's range for small rows
         float2 s0 = make_float2(0.f, 0.f), s1 = s0, s2 = s0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (t + i * T) * 8;
             if (c >= a.cols) break;
             const uint8_t* from = at + i * Q * piece;
-            const Eight h = load_staged<H>(from + AT_H * piece, piece);
-            keep_h = h;
+            const Eight xh = times(load_staged<H>(from + AT_H * piece, piece), rn);
+            keep_xh = xh;
             Eight d = zero8();
             if (known.dx()) {
                 d = load_staged<Y>(from, piece);
@@ -832,8 +839,13 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) d.v[k] = mul2(d.v[k], w.v[k]);
             }
+            Eight e = known.dh() ? load_staged<H>(from + AT_DH * piece, piece) : zero8();
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s0 = fma2(d.v[k], h.v[k], s0);
+            for (int k = 0; k < 4; ++k) {
+                s0 = fma2(d.v[k], xh.v[k], s0);
+                e.v[k] = fma2(both(rn), d.v[k], e.v[k]);
+            }
+            keep_sum = e;
             if (known.post()) {
                 Eight w = gamma_post(c);
                 if (known.gate()) {
@@ -841,54 +853,52 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) w.v[k] = mul2(w.v[k], q.v[k]);
                 }
-                const Eight y = load_staged<Y>(from + AT_Y * piece, piece), e = known.dh() ? load_staged<H>(from + AT_DH * piece, piece) : zero8();
-                keep_y = y;
-                keep_dh = e;
+                const Eight yh = times(load_staged<Y>(from + AT_Y * piece, piece), rp);
+                keep_yh = yh;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    w.v[k] = mul2(w.v[k], y.v[k]);
-                    s1 = fma2(w.v[k], fma2(both(rn), d.v[k], e.v[k]), s1);
-                    s2 = fma2(w.v[k], h.v[k], s2);
+                    w.v[k] = mul2(w.v[k], yh.v[k]);
+                    s1 = fma2(w.v[k], e.v[k], s1);
+                    s2 = fma2(w.v[k], xh.v[k], s2);
                 }
             }
         }
         float s[3] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y};
         cta_sums(s, area, turn);
-        // G = (dh + rn t) - k1 h;  dy = kb G w - k2 y
-        const float c1 = rn * s[0] * inv_cols, k1 = rn * rn * c1, kb = a.branch_scale * rp, c2 = (s[1] - rn * rn * c1 * s[2]) * kb * inv_cols, k2 = rp * rp * c2;
+        // G = (dh + rn t) - k1 xh;  dy = kb G w - k2 yh
+        const float k1 = rn * (s[0] * inv_cols), kb = a.branch_scale * rp, k2 = rp * ((s[1] - k1 * s[2]) * a.branch_scale * inv_cols);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (t + i * T) * 8;
             if (c >= a.cols) break;
             const uint8_t* from = at + i * Q * piece;
             const int64_t to = r * a.cols + c;
-            const bool kept = KEEP && known.post();          // dh and y are looked at in the first pass then
-            const Eight h = KEEP ? keep_h : load_staged<H>(from + AT_H * piece, piece);
-            Eight G = kept ? keep_dh : (known.dh() ? load_staged<H>(from + AT_DH * piece, piece) : zero8());
+            const bool kept = KEEP && known.post();          // y is looked at in the first pass then
+            const Eight xh = KEEP ? keep_xh : times(load_staged<H>(from + AT_H * piece, piece), rn);
+            Eight G = KEEP ? keep_sum : (known.dh() ? load_staged<H>(from + AT_DH * piece, piece) : zero8());
             if (known.dx()) {
-                const Eight d = KEEP ? keep_dx : load_staged<Y>(from, piece), w = gamma_pre(c);
+                const Eight d = KEEP ? keep_dx : load_staged<Y>(from, piece);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 scaled = mul2(d.v[k], both(rn));
-                    pre[i].v[k] = fma2(scaled, h.v[k], pre[i].v[k]);
-                    G.v[k] = fma2(scaled, w.v[k], G.v[k]);
+                for (int k = 0; k < 4; ++k) pre[i].v[k] = fma2(d.v[k], xh.v[k], pre[i].v[k]);
+                if (!KEEP) {
+                    const Eight w = gamma_pre(c);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) G.v[k] = fma2(both(rn), mul2(d.v[k], w.v[k]), G.v[k]);
                 }
             }
             Eight out;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                G.v[k] = fma2(both(-k1), h.v[k], G.v[k]);
+                G.v[k] = fma2(both(-k1), xh.v[k], G.v[k]);
                 out.v[k] = mul2(both(a.residual_scale), G.v[k]);
             }
             if (known.dh_in()) store8(static_cast<H*>(a.dh_in) + to, out);
-            const Eight y = kept ? keep_y : load_staged<Y>(from + AT_Y * piece, piece);
+            Eight yh = kept ? keep_yh : load_staged<Y>(from + AT_Y * piece, piece);
+            if (known.post() && !kept) yh = times(yh, rp);
             const Eight w = known.post() ? gamma_post(c) : zero8();
             if (known.d_gate())
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 n = mul2(both(kb), y.v[k]);
-                    gates[i].v[k] = fma2(G.v[k], known.post() ? mul2(n, w.v[k]) : n, gates[i].v[k]);
-                }
+                for (int k = 0; k < 4; ++k) gates[i].v[k] = fma2(G.v[k], known.post() ? mul2(yh.v[k], w.v[k]) : yh.v[k], gates[i].v[k]);
             if (known.gate()) {
                 const Eight q = gate_at(g, c);
 #pragma unroll
@@ -899,8 +909,8 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
                 const float2 scaled = mul2(both(kb), G.v[k]);                  // without a norm after the block, dy
                 out.v[k] = scaled;
                 if (known.post()) {
-                    post[i].v[k] = fma2(scaled, y.v[k], post[i].v[k]);
-                    out.v[k] = fma2(scaled, w.v[k], mul2(both(-k2), y.v[k]));
+                    post[i].v[k] = fma2(G.v[k], yh.v[k], post[i].v[k]);
+                    out.v[k] = fma2(scaled, w.v[k], mul2(both(-k2), yh.v[k]));
                 }
             }
             if (known.dy()) store8(static_cast<Y*>(a.dy) + to, out);
@@ -911,7 +921,7 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
             for (int i = 0; i < NV; ++i) {
                 const int c = (t + i * T) * 8;
                 if (c >= a.cols) break;
-                store8(part + c, gates[i]);
+                store8(part + c, times(gates[i], a.branch_scale));
                 gates[i] = zero8();
             }
         }
@@ -923,7 +933,7 @@ __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
         const int c = (t + i * T) * 8;
         if (c >= a.cols) break;
         if (a.d_gamma_pre) store8(weights_part(a, false) + c, pre[i]);
-        if (a.d_gamma_post) store8(weights_part(a, true) + c, post[i]);
+        if (a.d_gamma_post) store8(weights_part(a, true) + c, times(post[i], a.branch_scale));
     }
 }
 
