@@ -642,7 +642,7 @@ __device__ __forceinline__ void pad_scales(const SeamArgs& a, int t, int T)
 // Rows go last to first: what reads h or x next begins with the first rows, and finds them in L2 (8192 x 4096 in BF16 with the conversion in
 // both orientations behind it took 76 us that way and 79 us first to last; it takes 72 us now).
 template <typename Y, typename H, int NV, bool WARP, int STAGES, int MODE, bool CONVERT>
-__global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 : 256)), WARP ? 8 : (NV == 1 ? 1 : (NV == 8 ? 2 : (NV == 2 ? 2 : 4)))) seam_forward_kernel(const SeamArgs a)
+__global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 : 256)), WARP ? 8 : (NV == 1 ? 1 : 2)) seam_forward_kernel(const SeamArgs a)
 {
     extern __shared__ __align__(16) uint8_t stage_mem[];
     __shared__ float area[2][SEAM_MAX_WARPS];
@@ -1094,10 +1094,13 @@ cudaError_t launch_forward(const SeamArgs& a, cudaStream_t st)
         return cudaGetLastError();
     }
     const int vectors = a.cols / 8, warps = (vectors + 31) / 32;
+    // Rows of one warp's width: a warp each (8192 x 256 BF16 6.0 us, 6.7 with a CTA each).
+    // Wider ones, as long as CTAs of one vector per thread hold all rows at once: those (1184 x 1024 4.3 us, 5.0 with two vectors; 296 x 4096 4.7 and
+    // 5.6).  With more rows two vectors per thread pay (2368 x 1024 6.6 us, 6.9 with one; 592 x 4096 6.6 and 7.0), up to 512 columns in a
+    // warp per row (4736 x 512 6.5 us, 7.6 in a CTA per row; 8192 x 512 9.8 and 9.7; wider rows lose that way, 8192 x 1024 21 and 15).
     if (warps == 1) return launch_forward_rows<Y, H, 1, true, 4>(a, 128, st);
-    if (warps <= 4 && a.rows >= 8 * multiprocessors())
-        return warps <= 2 ? launch_forward_rows<Y, H, 2, true, 3>(a, 128, st) : launch_forward_rows<Y, H, 4, true, 3>(a, 128, st);
-    if (a.rows <= multiprocessors() && warps <= 32) return launch_forward_rows<Y, H, 1, false, 2>(a, 32 * warps, st);
+    if (warps <= 32 && a.rows <= (int64_t)multiprocessors() * (32 / warps)) return launch_forward_rows<Y, H, 1, false, 2>(a, 32 * warps, st);
+    if (warps == 2) return launch_forward_rows<Y, H, 2, true, 3>(a, 128, st);
     if (warps <= 32) return launch_forward_rows<Y, H, 2, false, 2>(a, 32 * ((warps + 1) / 2), st);
     // 16384 columns of two FP32 inputs leave room for one row at a time
     return launch_forward_rows<Y, H, 8, false, PIECES<Y> + PIECES<H> == 4 ? 1 : 2>(a, 32 * ((warps + 7) / 8), st);
