@@ -961,7 +961,12 @@ def run_operator_sweep(peaks):
         if case["op"] == "matvec" and case["chosen"]:            # the matrices that are chosen, not as many as could be
             used = sum(len(s["ids"].unique()) for s in states) / 3
             nbytes = used * case["rows"] * case["cols"] * 17 / 32 + 2 * case["tokens"] * case["cols"] + 4 * case["tokens"] * case["top_k"] * case["rows"]
-        t, floor = us(lambda i: mod.run(states[i]), 3), nbytes / peaks["hbm_gbs"] / 1e3
+        t = us(lambda i: mod.run(states[i]), 3)
+        if case["op"] == "moe":                                  # the same for a layer's experts, which its run has chosen
+            used = sum(len(s["ids"][s["ids"] >= 0].unique()) for s in states) / 3
+            row = (2 + mod.BYTES[case["out"]]) * case["cols"] + 4 * case["experts"]
+            nbytes = used * 3 * case["inner"] * case["cols"] * 17 / 32 + case["tokens"] * row
+        floor = nbytes / peaks["hbm_gbs"] / 1e3
         print("| %s | %.1f | %.2f | %.0f %% |" % (case["name"], t, floor, 100 * floor / t), flush=True)
         del states
     g = torch.Generator(device="cuda").manual_seed(7)
