@@ -2,7 +2,8 @@
 //   1. the choice of the experts from the router's logits, their gate / up products, m = act(gate) * up
 //   2. the down products of the chosen experts and their weighted sum, straight into y
 // Every CTA of both launches chooses for itself (a few hundred logits, cheaper than a launch in between).  Bound by the
-// weights of the experts that are used, 17/32 byte each, which are read once, and by the instructions that decode them (210 per tile of 16 x 128 in launch 1).
+// weights of the experts that are used, 17/32 byte each, and by the instructions that decode them (210 per tile of 16 x 128 in launch 1).  Both are done once
+// for every entry of an expert: ceil(slots / 8 or 16) times in launch 1, ceil(slots / 4 or 8) times in launch 2.
 // One token with 8 of 64 experts of 2048 x 1408: 23 us; 16 tokens with 6: 68 to 73 us; 32 tokens with 2 of 8 experts of 4096 x 14336: 280 to
 // 317 us from run to run.
 #include "e2m1_tiles.cuh"
@@ -278,7 +279,9 @@ __device__ __forceinline__ void run_tiles(const __nv_bfloat16* const (&from)[NX]
     }
 }
 
-// m of one (slot, row of the matrix).  The second part of an infinity is zero, not infinity less infinity.
+// m of one (slot, row of the matrix), rounded to 16 bits: two BF16 numbers are what the tensor instructions of the second launch take.  One alone costs
+// up to 2^-8 of each element, two up to 2^-16, about what the FP32 sums of the products cost (32 tokens of 4096 x 14336: y is 2.4e-6 from 64 bits
+// altogether, 2.0e-6 with FP32 throughout in PyTorch).  The second part of an infinity is zero, not infinity less infinity.
 __device__ __forceinline__ void put_m(const MoeArgs& a, int64_t row, int n, float gate, float up)
 {
     const float m = activate(gate, a.act) * up;
@@ -621,9 +624,11 @@ extern "C" int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens
     a.col_tiles = (int)((cols + TILE_COLS - 1) / TILE_COLS); a.inner_tiles = (int)((inner + TILE_COLS - 1) / TILE_COLS);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     a.units_magic = div_magic((uint32_t)(a.inner / TILE_ROWS)); a.top_k_magic = div_magic((uint32_t)a.top_k); a.experts_magic = div_magic((uint32_t)a.experts);
-    // slots of an expert that are worked on together: by how many are expected of one
+    // Slots of an expert that are worked on together: by how many are expected of one (all of an expert's tiles are copied and decoded again for the next entry).
+    // First launch, 8 or 16: 24 tokens with 2 of 8 experts of 4096 x 4096 93.1 us, 95.6 with 16; 32 tokens 107.8 and 105.2; 64 with 6 of 64 of 2048 x 1408 147.9 and 149.2.
+    // Second launch, 4 or 8: 8 tokens with 2 of 8 66.5 us, 68.2 with 8; 12 tokens 74.0 and 73.3; 16 with 6 of 64 69.6 and 71.7, 32 97.9 and 96.3.
     const int slots = a.tokens * a.top_k;
-    cudaError_t err = a.tokens <= 8 || slots <= 4 * num_experts ? launch_gate_up<1, 16, 4>(a, st) : launch_gate_up<2, 16, 3>(a, st);
+    cudaError_t err = a.tokens <= 8 || slots <= 6 * num_experts ? launch_gate_up<1, 16, 4>(a, st) : launch_gate_up<2, 16, 3>(a, st);
     if (err == cudaSuccess) {
         if (a.tokens <= 4 || slots <= 2 * num_experts) err = a.tokens <= 32 ? launch_down<1, 16, 3, 32>(a, st) : launch_down<1, 12, 3, 64>(a, st);
         else err = a.tokens <= 32 ? launch_down<2, 16, 3, 32>(a, st) : launch_down<2, 12, 3, 64>(a, st);
