@@ -281,14 +281,16 @@ __device__ __forceinline__ void run_tiles(const __nv_bfloat16* const (&from)[NX]
 
 // m of one (slot, row of the matrix), rounded to 16 bits: two BF16 numbers are what the tensor instructions of the second launch take.  One alone costs
 // up to 2^-8 of each element, two up to 2^-16, about what the FP32 sums of the products cost (32 tokens of 4096 x 14336: y is 2.4e-6 from 64 bits
-// altogether, 2.0e-6 with FP32 throughout in PyTorch).  The second part of an infinity is zero, not infinity less infinity.
+// altogether, 2.0e-6 with FP32 throughout in PyTorch).  A finite m whose first part would round to infinity takes the
+// largest BF16 number; the second part of an infinity is zero, not infinity less infinity.
 __device__ __forceinline__ void put_m(const MoeArgs& a, int64_t row, int n, float gate, float up)
 {
     const float m = activate(gate, a.act) * up;
-    const __nv_bfloat16 hi = __float2bfloat16_rn(m);
+    __nv_bfloat16 hi = __float2bfloat16_rn(m);
+    if (isinf(__bfloat162float(hi))) hi = __float2bfloat16_rz(m);
     a.m_hi[row * a.inner + n] = hi;
     const float rest = m - __bfloat162float(hi);
-    a.m_lo[row * a.inner + n] = __float2bfloat16_rn(isinf(__bfloat162float(hi)) ? 0.f : rest);
+    a.m_lo[row * a.inner + n] = __float2bfloat16_rn(isinf(m) ? 0.f : rest);
 }
 
 // ---- first launch.  A unit is 16 gate rows and the 16 up rows that belong to them, for the slots of one entry.  The CTAs take the units in

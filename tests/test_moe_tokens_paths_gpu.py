@@ -91,3 +91,25 @@ def test_choice_of_many_tokens_at_ties_zeros_infinities_and_nan(experts, top_k, 
     assert torch.equal(ids.cpu(), want_ids)
     assert bool(((weights.cpu().double() - want).abs() <= 300 * 2.0 ** -23 * want + 1e-38).all())
     assert bool((y[3] == 0).all()) and bool((y[8] == 0).all()) and bool(y.isfinite().all())
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_an_intermediate_between_the_largest_numbers_of_bf16_and_fp32(sign):
+    """m = (2^64 (1 - 2^-12))^2 = 2^128 (1 - 2^-11 + 2^-24) is an FP32 number that BF16 rounds to infinity.  Times 2^-30 it is in range; the other columns of the down
+    matrix are zero.  m is kept to 2^-16 of itself, everything else here is exact."""
+    cols, inner = 64, 64
+    packed = []
+    down = torch.zeros(cols, inner, device="cuda")
+    down[:, 0] = sign * 2.0 ** -30
+    for w in (torch.ones(2 * inner, cols, device="cuda"), down):
+        q = torch.empty(w.shape, dtype=torch.uint8, device="cuda")
+        s = torch.empty(w.numel() // 32, dtype=torch.uint8, device="cuda")
+        B.mxfp8_quantize(w, B.ROW, B.RULE_PAPER, B.E2M1, q, s, None, None, B.SF_LINEAR)
+        packed.append(torch.empty(B.mxfp8_e2m1_packed_bytes(1, *w.shape), dtype=torch.uint8, device="cuda"))
+        B.mxfp8_e2m1_pack(q, s, 1, packed[-1])
+    x = torch.zeros(1, cols, dtype=torch.bfloat16, device="cuda")
+    x[0, 0], x[0, 1], x[0, 2] = 2.0 ** 63, 2.0 ** 63 * (1 - 2.0 ** -8), 2.0 ** 55 * 0.875
+    assert float(x.double().sum()) == 2.0 ** 64 * (1 - 2.0 ** -12)
+    y, _, _ = run(x, torch.zeros(1, 1, device="cuda"), 1, packed, inner, B.ACT_NONE, True, torch.float32)
+    want = sign * 2.0 ** 98 * (1 - 2.0 ** -11 + 2.0 ** -24)
+    assert bool(((y.double() - want).abs() <= 2.0 ** -16 * abs(want)).all())
