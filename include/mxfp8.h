@@ -465,8 +465,10 @@ int mxfp8_e2m1_matvec(const void* x, int64_t tokens, int64_t cols, const void* p
  *   y         [tokens, cols] FP32 or BF16, zeros for a token without experts.
  *   ids, weights  [tokens, top_k] int32 / FP32 outputs, or NULL: the choice, best first, -1 / 0 where there is none.
  *   ws        mxfp8_e2m1_moe_ws_bytes() bytes, 16-byte aligned; calls that may overlap need their own.
- *   Products and sums as mxfp8_e2m1_matvec; m is kept as the sum of two BF16 numbers (16 bits), the rest in FP32, in a fixed order.
- *   cols and inner multiples of 32; at least one token (ERR_SHAPE); at most 64 tokens, 256 experts, top_k 16 (ERR_UNSUPPORTED).
+ *   Products and sums as mxfp8_e2m1_matvec; m is kept as the sum of two BF16 numbers (to 2^-16 of itself), the rest in FP32, in a fixed
+ *   order.
+ *   cols and inner multiples of 32; at least one token (ERR_SHAPE); at most 64 tokens, 256 experts, top_k 16,
+ *   2^20 columns and 2^20 inner rows (ERR_UNSUPPORTED).
  */
 size_t mxfp8_e2m1_moe_ws_bytes(int64_t tokens, int top_k, int64_t inner);
 int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens, int64_t cols, int num_experts, int top_k,
@@ -480,7 +482,8 @@ int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens, int64_t c
  *     h[r, c]      = residual_scale * h_in[r, c] + (branch_scale * gate[r / rows_per_gate, c]) * n    rounded once to the stream's type
  *     rstd_pre[r]  = 1 / sqrt(mean_c h[r, c]^2 + eps)                                            of h as stored
  *     x[r, c]      = (h[r, c] * rstd_pre[r]) * gamma_pre[c]                                       rounded once to the block's type
- * Everything between the roundings is FP32.  Since the second norm reads h as it is stored, x can be computed again from h alone.
+ * Everything between the roundings is FP32, the sums of squares too: a row whose squares leave its range has the statistic 0 or 1 / sqrt(eps).
+ * Since the second norm reads h as it is stored, x can be computed again from h alone.
  *
  * The description of a seam (host memory, read during the call; its pointers are device pointers):
  */
@@ -508,7 +511,9 @@ typedef struct mxfp8_seam {
  *     dy    = rstd_post (w gamma_post G - yh mean_c(w gamma_post G yh))      rounded once to the block's type; w G without gamma_post
  *     d_gamma_pre = sum_r dx xh,  d_gamma_post = sum_r w G yh,  d_gate[g] = sum over the rows of g of branch_scale G n     FP32
  *   The FP32 sums over rows have a fixed order.  dh_in may be dh.  dy, dh_in and each of the parameters' gradients may be NULL when they are not wanted.
- *   ws: mxfp8_residual_rmsnorm_grad_ws_bytes() bytes, 16-byte aligned; calls that may overlap need their own.
+ *   ws: mxfp8_residual_rmsnorm_grad_ws_bytes() bytes (by the current device's multiprocessors), 16-byte aligned; calls that may overlap need their own.
+ * Errors: ERR_NULL, ERR_ENUM (types), ERR_SHAPE (rows, cols or, with a gate, rows_per_gate below 1; eps negative or NaN), ERR_ALIGN, ERR_UNSUPPORTED (more than
+ *   16384 columns or 2^40 rows), ERR_WORKSPACE, ERR_CUDA.
  */
 int mxfp8_residual_rmsnorm(const mxfp8_seam* seam, const void* y, const void* h_in, void* h, void* x,
                            float* rstd_post, float* rstd_pre, void* stream);
@@ -525,7 +530,7 @@ int mxfp8_residual_rmsnorm_grad(const mxfp8_seam* seam, const void* dx, const vo
  *     S = sum over all items and elements of src^2;   norm = sqrt(S);   factor = min(1, max_norm / (norm + 1e-6))
  *     dst = factor * src   one FP32 product, rounded once to the item's type
  * S is FP64 (squares of eight neighbours at a time are added in FP32 where that loses no range), in a fixed order: the result is the same every
- * time.  A norm that is not finite leaves the values as they are (dst = src, factor = 1), so that the caller can skip the step.
+ * time.  A norm that is not a finite FP32 number leaves the values as they are (dst = src, factor = 1), so that the caller can skip the step.
  *   items   HOST array of `count` entries, read during the call (it may change afterwards).  src and dst are aligned to their elements; dst may be
  *           its own src, and overlaps nothing else (no other item's src or dst).  numel may be 0; count may be 0 (norm 0).
  * mxfp8_grad_sumsq -- S alone, to `sumsq` (device, one FP64): ranks that hold parts of the gradients add theirs before
@@ -533,7 +538,8 @@ int mxfp8_residual_rmsnorm_grad(const mxfp8_seam* seam, const void* dx, const vo
  *           everywhere and factor 1 nothing is read or written.
  * mxfp8_grad_clip  -- both, without the detour over sumsq.
  *   ws: mxfp8_grad_ws_bytes(items, count) bytes, 8-byte aligned; calls that may overlap need their own.
- *   Errors: ERR_NULL, ERR_ENUM (dtype), ERR_SHAPE (negative count or numel, max_norm negative or NaN), ERR_ALIGN, ERR_WORKSPACE, ERR_CUDA.
+ *   Errors: ERR_NULL, ERR_ENUM (dtype), ERR_SHAPE (negative count or numel, max_norm negative or NaN), ERR_ALIGN, ERR_UNSUPPORTED (numel above
+ *           2^34), ERR_WORKSPACE, ERR_CUDA.
  */
 typedef struct mxfp8_grad_item {
     const void* src;

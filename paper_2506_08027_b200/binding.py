@@ -776,7 +776,8 @@ class GradItems:
 
 def make_grad_items(grads, results=None) -> GradItems:
     """grads: FP32 / BF16 tensors of one device; results: where the scaled values go (None: in place).  Build it once and reuse it while the
-    tensors keep their storage; mxfp8_grad_sumsq needs no results.  What is written may overlap no other gradient (the same one twice, say)."""
+    tensors keep their storage: it takes 2 to 3 us of host time per tensor, more than clipping many short ones does.  mxfp8_grad_sumsq needs no
+    results.  What is written may overlap no other gradient (the same one twice, say)."""
     grads, results = list(grads), None if results is None else list(results)
     if results is not None and (len(results) != len(grads) or any(r.dtype is not g.dtype or r.shape != g.shape for g, r in zip(grads, results))):
         raise ValueError("results have the gradients' shapes and types")

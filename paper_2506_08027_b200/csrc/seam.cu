@@ -4,7 +4,8 @@
 //   rstd_pre  = 1 / sqrt(mean h^2 + eps);  x = (h rstd_pre) gamma_pre
 //
 // Bound by memory: forward y, h_in -> h, x; backward dx, dh, y, h -> dy, dh_in, each element once.  8192 x 4096 in BF16: forward
-// 49.5 us, backward 76 to 80 us, 83 and 77 to 81 % of the measured copy rate.
+// 49.5 us, backward 76 to 81 us, 83 and 76 to 81 % of the measured copy rate.  Further from it: FP32 streams (forward 91 us, 68 %; backward 142 us,
+// 65 %), backward rows above 4096 columns (65 % in BF16, 44 % in FP32) and rows off 16-byte boundaries (8192 x 4095 BF16: 147 and 463 us).
 #include <cuda_bf16.h>
 
 #include <initializer_list>
@@ -466,7 +467,8 @@ __global__ void __launch_bounds__(SEAM_THREADS) seam_grad_any_kernel(const SeamA
 // ---------------------------------------------------------------------------------------------------------------------
 // Rows that start on 16-byte boundaries.  A thread owns the vectors of eight columns threadIdx.x + i T of every row that its group
 // takes (a warp for short rows, else the CTA of T threads).  It copies them itself, asynchronously, into places of shared memory that no other
-// thread touches, STAGES rows ahead: no barrier guards them, only the thread's own wait for its copies.
+// thread touches, STAGES - 1 rows ahead: no barrier guards them, only the thread's own wait for its copies.  Where shared memory holds one row of a CTA,
+// STAGES is 1 and a row's loads are waited for (backward above 8192 columns, and above 4096 with FP32 on both sides; forward above 8192 with FP32 on both).
 template <typename T> constexpr int PIECES = sizeof(T) / 2;            // 16-byte pieces of eight elements
 
 __device__ __forceinline__ void copy16(uint32_t to, const void* from)
@@ -756,7 +758,7 @@ __global__ void __launch_bounds__(WARP ? 128 : (NV == 1 ? 1024 : (NV == 2 ? 512 
 
 // Backward: same ownership and the same sums as seam_grad_any_kernel; column sums stay in registers.  With one vector per thread so do the
 // parameters and, between the two passes over the row, its elements: 8192 x 4096 in BF16 took 82 us that
-// way and 86 us with two vectors read twice from shared memory; it takes 76 to 80 us since statistics are read a row ahead and 16 warps join.
+// way and 86 us with two vectors read twice from shared memory; it takes 76 to 81 us since statistics are read a row ahead and 16 warps join.
 template <typename Y, typename H, int NV, int STAGES, int MODE>
 __global__ void __launch_bounds__(512, 1) seam_grad_kernel(const SeamArgs a)
 {
