@@ -465,8 +465,8 @@ int mxfp8_e2m1_matvec(const void* x, int64_t tokens, int64_t cols, const void* p
  *   y         [tokens, cols] FP32 or BF16, zeros for a token without experts.
  *   ids, weights  [tokens, top_k] int32 / FP32 outputs, or NULL: the choice, best first, -1 / 0 where there is none.
  *   ws        mxfp8_e2m1_moe_ws_bytes() bytes, 16-byte aligned; calls that may overlap need their own.
- *   Products and sums as mxfp8_e2m1_matvec; m is kept as the sum of two BF16 numbers (to 2^-16 of itself), the rest in FP32, in a fixed
- *   order.
+ *   Products and sums as mxfp8_e2m1_matvec; with BF16 y, m is kept as the sum of two BF16 numbers (to 2^-16 of itself), with FP32 y in
+ *   FP32, as the rest is; everything in a fixed order.
  *   cols and inner multiples of 32; at least one token (ERR_SHAPE); at most 64 tokens, 256 experts, top_k 16,
  *   2^20 columns and 2^20 inner rows (ERR_UNSUPPORTED).
  */

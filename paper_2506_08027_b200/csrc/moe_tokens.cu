@@ -4,8 +4,10 @@
 // Every CTA of both launches chooses for itself (a few hundred logits, cheaper than a launch in between).  Bound by the
 // weights of the experts that are used, 17/32 byte each, and by the instructions that decode them (210 per tile of 16 x 128 in launch 1).  Both are done once
 // for every entry of an expert: ceil(slots / 8 or 16) times in launch 1, ceil(slots / 4 or 8) times in launch 2.
-// One token with 8 of 64 experts of 2048 x 1408: 23 us; 16 tokens with 6: 68 to 73 us; 32 tokens with 2 of 8 experts of 4096 x 14336: 280 to
-// 317 us from run to run.
+// One token with 8 of 64 experts of 2048 x 1408: 23 us; 16 tokens with 6: 68 to 73 us; 32 tokens with 2 of 8 experts of 4096 x 14336: 269 to
+// 317 us from run to run with BF16 outputs, 35 us more with FP32 ones.
+#include <type_traits>
+
 #include "e2m1_tiles.cuh"
 #include "mxfp8_host.h"
 
@@ -26,7 +28,7 @@ struct MoeArgs {
     bool bf16_out;
     int32_t* ids;
     float* weights;
-    __nv_bfloat16 *m_hi, *m_lo;      // [slots, inner]: m = m_hi + m_lo
+    __nv_bfloat16 *m_hi, *m_lo, *m_rest;      // [slots, inner]: m = m_hi + m_lo (+ m_rest; null for BF16 outputs)
     int tokens, experts, top_k, act, renormalize;
     int cols, inner;
     int col_tiles, inner_tiles;      // column tiles of gate_up and of down
@@ -279,10 +281,10 @@ __device__ __forceinline__ void run_tiles(const __nv_bfloat16* const (&from)[NX]
     }
 }
 
-// m of one (slot, row of the matrix), rounded to 16 bits: two BF16 numbers are what the tensor instructions of the second launch take.  One alone costs
-// up to 2^-8 of each element, two up to 2^-16, about what the FP32 sums of the products cost (32 tokens of 4096 x 14336: y is 2.4e-6 from 64 bits
-// altogether, 2.0e-6 with FP32 throughout in PyTorch).  A finite m whose first part would round to infinity takes the
-// largest BF16 number; the second part of an infinity is zero, not infinity less infinity.
+// m of one (slot, row of the matrix) as BF16 numbers, which the tensor instructions of the second launch take.  FP32 outputs get three, which hold all of its 24
+// bits (with two, y was 2.3e-6 from 64 bits where FP32 throughout is 2e-7 from it); BF16 outputs get two, 2^-16 of m beside
+// their own rounding of 2^-8.  A finite m whose first part would round to infinity takes the largest BF16 number; the other parts
+// of an infinity are zero, not infinity less infinity.
 __device__ __forceinline__ void put_m(const MoeArgs& a, int64_t row, int n, float gate, float up)
 {
     const float m = activate(gate, a.act) * up;
@@ -290,7 +292,9 @@ __device__ __forceinline__ void put_m(const MoeArgs& a, int64_t row, int n, floa
     if (isinf(__bfloat162float(hi))) hi = __float2bfloat16_rz(m);
     a.m_hi[row * a.inner + n] = hi;
     const float rest = m - __bfloat162float(hi);
-    a.m_lo[row * a.inner + n] = __float2bfloat16_rn(isinf(m) ? 0.f : rest);
+    const __nv_bfloat16 lo = __float2bfloat16_rn(isinf(m) ? 0.f : rest);
+    a.m_lo[row * a.inner + n] = lo;
+    if (a.m_rest) a.m_rest[row * a.inner + n] = __float2bfloat16_rn(isinf(m) ? 0.f : rest - __bfloat162float(lo));
 }
 
 // ---- first launch.  A unit is 16 gate rows and the 16 up rows that belong to them, for the slots of one entry.  The CTAs take the units in
@@ -421,14 +425,15 @@ __global__ void __launch_bounds__(32 * WARPS, 1) moe_gate_up_kernel(const MoeArg
 // ---- second launch.  A cluster of two CTAs takes two row tiles of all entries' down projections at a time, and its warps split the entries'
 // column tiles evenly: m, read from L2 by everybody, serves 32 rows (each CTA reads half of it).  A warp holds the weighted sums of
 // its share for all tokens; at the end they are gathered through the cluster's shared memory, half of the outputs by each CTA.
-// A block of eight columns of the tensor instructions takes the two parts of m of four slots: entries have 4 NB slots at most.
+// A block of eight columns of the tensor instructions takes the first two parts of m of four slots: entries have 4 NB slots at most.  Their third parts, where
+// there are any, fill the columns of further blocks, eight slots to each.
 constexpr int DOWN_ROWS = 2 * TILE_ROWS, DOWN_PITCH = DOWN_ROWS + 1;
-template <int NB, int WARPS, int STAGES>
+template <int NB, int PARTS, int WARPS, int STAGES>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * WARPS, 1) moe_down_kernel(const MoeArgs a)
 {
     extern __shared__ __align__(16) uint8_t dynamic[];
     __shared__ Choice choice;
-    constexpr int STAGE = 2 * TILE_BYTES, P = DOWN_PITCH;
+    constexpr int STAGE = 2 * TILE_BYTES, P = DOWN_PITCH, NX = PARTS == 2 ? NB : NB + (NB + 1) / 2;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = blockIdx.x & 1, cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
     uint8_t* ring = dynamic + warp * STAGES * STAGE;
@@ -483,15 +488,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * WARPS, 1) moe_d
             const short* slot = choice.slot + v * 4 * NB;
             const int rows = choice.entry_rows[v], here = min(left, a.inner_tiles - kt);
             left -= here;
-            const __nv_bfloat16* from[NB];
+            const __nv_bfloat16* from[NX];
 #pragma unroll
-            for (int t = 0; t < NB; ++t) {               // columns 0 .. 3: the first parts of four slots, 4 .. 7: their second parts
-                const int i = 4 * t + ((lane >> 2) & 3);
-                from[t] = (lane & 16 ? a.m_lo : a.m_hi) + (int64_t)slot[i < rows ? i : 0] * a.inner + (lane & 3) * 8;
+            for (int t = 0; t < NX; ++t) {               // columns 0 .. 3: the first parts of four slots, 4 .. 7: their second parts
+                const int i = t < NB ? 4 * t + ((lane >> 2) & 3) : 8 * (t - NB) + (lane >> 2);
+                from[t] = (t < NB ? (lane & 16 ? a.m_lo : a.m_hi) : a.m_rest) + (int64_t)slot[i < rows ? i : 0] * a.inner + (lane & 3) * 8;
             }
-            float acc[2][NB][4];
+            float acc[2][NX][4];
             clear(acc);
-            run_tiles<NB, STAGES>(from, kt, kt + here, a.inner, ring, stage, fetch, acc);
+            run_tiles<NX, STAGES>(from, kt, kt + here, a.inner, ring, stage, fetch, acc);
 #pragma unroll
             for (int t = 0; t < NB; ++t)
 #pragma unroll
@@ -505,8 +510,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * WARPS, 1) moe_d
                     for (int r = 0; r < 2; ++r)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            const float part = acc[r][t][2 * h + c], both = part + __shfl_xor_sync(0xFFFFFFFFu, part, 2);
-                            if (in) to[r * TILE_ROWS + 8 * h] = fmaf(weight, both, to[r * TILE_ROWS + 8 * h]);
+                            // the third part lies in this lane for even blocks, in the lane of the second part for odd ones; the smaller two are added first
+                            const float part = acc[r][t][2 * h + c], third = PARTS == 2 ? 0.f : acc[r][PARTS == 2 ? t : NB + t / 2][2 * h + c];
+                            const float other = __shfl_xor_sync(0xFFFFFFFFu, t % 2 ? part + third : part, 2);
+                            const float all = part + (t % 2 ? other : other + third);
+                            if (in) to[r * TILE_ROWS + 8 * h] = fmaf(weight, all, to[r * TILE_ROWS + 8 * h]);
                         }
                 }
             __syncwarp();
@@ -580,14 +588,14 @@ cudaError_t launch_gate_up(const MoeArgs& a, cudaStream_t st)
     return launch_early(moe_gate_up_kernel<NT, WARPS, STAGES>, multiprocessors(), 32 * WARPS, SMEM, set, a, st);
 }
 
-template <int NB, int WARPS, int STAGES, int TOKENS>
+template <int NB, int PARTS, int WARPS, int STAGES, int TOKENS>
 cudaError_t launch_down(const MoeArgs& a, cudaStream_t st)
 {
     constexpr int RING = WARPS * STAGES * 2 * TILE_BYTES, PER_TOKEN = WARPS * DOWN_PITCH * (int)sizeof(float);
     static_assert(RING + TOKENS * PER_TOKEN <= MOE_DYNAMIC_SMEM, "ring and sums fit");
     static unsigned long long set = 0;
     const int groups = a.cols / DOWN_ROWS, most = multiprocessors() / 2;
-    return launch_early(moe_down_kernel<NB, WARPS, STAGES>, 2 * (groups < most ? groups : most), 32 * WARPS, RING + a.tokens * PER_TOKEN, set, a, st);
+    return launch_early(moe_down_kernel<NB, PARTS, WARPS, STAGES>, 2 * (groups < most ? groups : most), 32 * WARPS, RING + a.tokens * PER_TOKEN, set, a, st);
 }
 
 }  // namespace
@@ -598,7 +606,7 @@ using namespace mxfp8;
 extern "C" size_t mxfp8_e2m1_moe_ws_bytes(int64_t tokens, int top_k, int64_t inner)
 {
     if (tokens <= 0 || top_k <= 0 || inner <= 0 || tokens > MOE_MAX_TOKENS || top_k > MOE_MAX_TOP_K) return 0;
-    return (size_t)tokens * top_k * (size_t)inner * 2 * sizeof(__nv_bfloat16);
+    return (size_t)tokens * top_k * (size_t)inner * 3 * sizeof(__nv_bfloat16);
 }
 
 extern "C" int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens, int64_t cols, int num_experts, int top_k,
@@ -621,6 +629,7 @@ extern "C" int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens
     a.gate_up = static_cast<const uint8_t*>(gate_up); a.down = static_cast<const uint8_t*>(down);
     a.y = y; a.bf16_out = y_dtype == MXFP8_BF16; a.ids = ids; a.weights = weights;
     a.m_hi = static_cast<__nv_bfloat16*>(ws); a.m_lo = a.m_hi + tokens * top_k * inner;
+    a.m_rest = a.bf16_out ? nullptr : a.m_lo + tokens * top_k * inner;
     a.tokens = (int)tokens; a.experts = num_experts; a.top_k = top_k; a.act = act; a.renormalize = renormalize != 0;
     a.cols = (int)cols; a.inner = (int)inner;
     a.col_tiles = (int)((cols + TILE_COLS - 1) / TILE_COLS); a.inner_tiles = (int)((inner + TILE_COLS - 1) / TILE_COLS);
@@ -628,12 +637,18 @@ extern "C" int mxfp8_e2m1_moe(const void* x, const float* logits, int64_t tokens
     a.units_magic = div_magic((uint32_t)(a.inner / TILE_ROWS)); a.top_k_magic = div_magic((uint32_t)a.top_k); a.experts_magic = div_magic((uint32_t)a.experts);
     // Slots of an expert that are worked on together: by how many are expected of one (all of an expert's tiles are copied and decoded again for the next entry).
     // First launch, 8 or 16: 24 tokens with 2 of 8 experts of 4096 x 4096 93.1 us, 95.6 with 16; 32 tokens 107.8 and 105.2; 64 with 6 of 64 of 2048 x 1408 147.9 and 149.2.
-    // Second launch, 4 or 8: 8 tokens with 2 of 8 66.5 us, 68.2 with 8; 12 tokens 74.0 and 73.3; 16 with 6 of 64 69.6 and 71.7, 32 97.9 and 96.3.
+    // Second launch, 4 or 8: 8 tokens with 2 of 8 66.5 us, 68.2 with 8; 12 tokens 74.0 and 73.3; 16 with 6 of 64 69.6 and 71.7, 32 97.9 and 96.3;
+    // with FP32 outputs 70.5 and 72.3, 78.8 and 77.6, 73.4 and 77.6, 103.6 and 104.5.
     const int slots = a.tokens * a.top_k;
     cudaError_t err = a.tokens <= 8 || slots <= 6 * num_experts ? launch_gate_up<1, 16, 4>(a, st) : launch_gate_up<2, 16, 3>(a, st);
     if (err == cudaSuccess) {
-        if (a.tokens <= 4 || slots <= 2 * num_experts) err = a.tokens <= 32 ? launch_down<1, 16, 3, 32>(a, st) : launch_down<1, 12, 3, 64>(a, st);
-        else err = a.tokens <= 32 ? launch_down<2, 16, 3, 32>(a, st) : launch_down<2, 12, 3, 64>(a, st);
+        auto down = [&](auto nb) {
+            constexpr int NB = decltype(nb)::value;
+            // three blocks of activations need the registers of 12 warps (32 tokens with 2 of 8 experts of 4096 x 14336 363 us with 16, 315 with 12)
+            if (a.m_rest) return NB == 1 && a.tokens <= 32 ? launch_down<NB, 3, NB == 1 ? 16 : 12, 3, 32>(a, st) : launch_down<NB, 3, 12, 3, 64>(a, st);
+            return a.tokens <= 32 ? launch_down<NB, 2, 16, 3, 32>(a, st) : launch_down<NB, 2, 12, 3, 64>(a, st);
+        };
+        err = a.tokens <= 4 || slots <= 2 * num_experts ? down(std::integral_constant<int, 1>{}) : down(std::integral_constant<int, 2>{});
     }
     return err == cudaSuccess ? MXFP8_OK : MXFP8_ERR_CUDA;
 }

@@ -113,3 +113,32 @@ def test_an_intermediate_between_the_largest_numbers_of_bf16_and_fp32(sign):
     y, _, _ = run(x, torch.zeros(1, 1, device="cuda"), 1, packed, inner, B.ACT_NONE, True, torch.float32)
     want = sign * 2.0 ** 98 * (1 - 2.0 ** -11 + 2.0 ** -24)
     assert bool(((y.double() - want).abs() <= 2.0 ** -16 * abs(want)).all())
+
+
+@pytest.mark.parametrize("tokens,top_k,experts", [(1, 1, 1), (3, 2, 2), (4, 4, 4), (7, 1, 1), (16, 2, 8), (23, 3, 4), (33, 2, 40), (64, 1, 1), (64, 4, 5)])
+def test_an_intermediate_is_held_in_32_bits_where_the_outputs_are(tokens, top_k, experts):
+    """m = s^2 of a 12-bit s needs all 24 bits of an FP32 number.  With one column of the down matrices 1 and the others zero, and choices of equal weight (a half or a quarter
+    of m each, exactly; with three, a third is rounded twice), y is m to the last bit."""
+    cols, inner = 64, 96
+    packed = []
+    down = torch.zeros(experts, cols, inner, device="cuda")
+    down[:, :, 5] = 1.0
+    for w in (torch.ones(experts, 2 * inner, cols, device="cuda"), down):
+        q = torch.empty(experts * w.shape[1], w.shape[2], dtype=torch.uint8, device="cuda")
+        s = torch.empty(w.numel() // 32, dtype=torch.uint8, device="cuda")
+        B.mxfp8_quantize(w.reshape(q.shape), B.ROW, B.RULE_PAPER, B.E2M1, q, s, None, None, B.SF_LINEAR)
+        packed.append(torch.empty(B.mxfp8_e2m1_packed_bytes(*w.shape), dtype=torch.uint8, device="cuda"))
+        B.mxfp8_e2m1_pack(q, s, experts, packed[-1])
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    a, b = (torch.randint(0, n, (tokens,), generator=g, device="cuda") for n in (128, 16))
+    x = torch.zeros(tokens, cols, dtype=torch.bfloat16, device="cuda")
+    x[:, 0], x[:, 33] = (1 + a / 128.0).to(torch.bfloat16), (b * 2.0 ** -11).to(torch.bfloat16)
+    m = x.double().sum(dim=1).square()
+    logits = torch.zeros(tokens, experts, device="cuda")
+    y, _, _ = run(x, logits, top_k, packed, inner, B.ACT_NONE, True, torch.float32)
+    off = (y.double() - m.unsqueeze(1)).abs() / m.unsqueeze(1)
+    # three times a rounded third, three roundings of the sum
+    assert float(off.max()) <= (5 * 2.0 ** -24 if top_k == 3 else 0.0)
+    # two parts, to 2^-16, and the outputs' rounding
+    y, _, _ = run(x, logits, top_k, packed, inner, B.ACT_NONE, True, torch.bfloat16)
+    assert float(((y.double() - m.unsqueeze(1)).abs() / m.unsqueeze(1)).max()) <= 2.0 ** -8 + 2.0 ** -15
